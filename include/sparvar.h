@@ -493,6 +493,131 @@ int sparvar_kv_compact(const sparvar_geometry_t* g, int32_t n_keep, const int32_
                        const void* v_src, int64_t src_bh_stride, void* k_dst, void* v_dst,
                        int64_t dst_bh_stride, hipStream_t stream);
 
+/*
+ * ---- 8-bit key/value cache, and the step that fills a cache.
+ *
+ * An 8-bit cache holds K and V as e4m3 codes (1 + 4 + 3 bits, no infinity) with
+ * one power-of-two scale for each block of `block` consecutive tokens of a head,
+ * K and V apart: value = code * 2^(scale byte - 127) (E8M0 bytes). A block's
+ * exponent is the smallest e with max|x| <= 448 * 2^e over the block's tokens,
+ * clamped to [-100, 112]; codes are x * 2^-e rounded to nearest even, saturated
+ * at 448 (so magnitudes of 448 * 2^112 and above saturate, infinities too; a
+ * NaN stays a NaN and does not count for the exponent). Every value is exact in
+ * bf16. Tokens are counted from the start of the plane, as everywhere.
+ *
+ * Rows are appended at any token t0. The block that t0 lies in is encoded again,
+ * with the values its tokens before t0 hold and the new ones: its exponent may
+ * grow, which only moves codes towards the subnormals of the format. Tokens from
+ * t0 + n on in the last block are not counted and their codes stay as they were
+ * (their values change with the block's scale): append in ascending order.
+ *
+ * The struct is host memory read during the call; k, v and the scales are device
+ * memory. H_kv planes a batch entry; a call's H (query heads) is a multiple of
+ * H_kv, and query heads [g H / H_kv, (g + 1) H / H_kv) read key head g.
+ */
+typedef struct sparvar_q8_cache {
+  int32_t block;           /* tokens of one scale: 16, 32, 64 or 128 */
+  int32_t capacity;        /* tokens a plane holds */
+  void* k;                 /* codes [B,H_kv,capacity,d], plane stride bh_stride */
+  void* v;
+  int64_t bh_stride;       /* >= capacity * d, a multiple of 16 */
+  uint8_t* k_scale;        /* E8M0 bytes [B,H_kv,ceil(capacity / block)] */
+  uint8_t* v_scale;
+  int64_t scale_bh_stride; /* >= ceil(capacity / block) */
+} sparvar_q8_cache_t;
+
+/* Norm of a head's vector: none; x / sqrt(mean(x^2) + eps); x / max(|x|, eps). */
+typedef enum sparvar_norm { SPARVAR_NORM_NONE = 0, SPARVAR_NORM_RMS = 1, SPARVAR_NORM_L2 = 2 } sparvar_norm_t;
+/* Channels that pair i < d/2 of the rotation turns: (2i, 2i+1), or (i, i + d/2). */
+typedef enum sparvar_rope_layout { SPARVAR_ROPE_PAIRS = 0, SPARVAR_ROPE_HALVES = 1 } sparvar_rope_layout_t;
+
+/* What happens to a query or key vector on its way: norm, weight, rotation. The
+ * struct is host memory read during the call, its pointers are device memory. */
+typedef struct sparvar_norm_rope {
+  int32_t norm;           /* sparvar_norm_t */
+  int32_t layout;         /* sparvar_rope_layout_t */
+  float eps;              /* finite, >= 0 */
+  int32_t table_rows;     /* rows of cos_sin */
+  const float* q_weight;  /* nullable: [H, d], times the normed vector */
+  const float* k_weight;  /* nullable: [H_kv, d] */
+  const float* cos_sin;   /* nullable (no rotation): [table_rows, d/2, 2], row = cache token */
+} sparvar_norm_rope_t;
+
+/*
+ * Appends n tokens of one step to a cache: for every token i < n and head,
+ *   y = x * r(x) * weight, r as sparvar_norm_t says;
+ *   (y_a, y_b) -> (y_a cos - y_b sin, y_a sin + y_b cos) for every pair of the
+ *   layout, with cos and sin of row t0 + i of the table;
+ * for queries (to q_out) and keys (to cache token t0 + i); values are copied. In
+ * 32 bits from the inputs on, rounded once, to the output's type or to the codes
+ * of an 8-bit cache.
+ *   q: [B,n,H,d], k, v: [B,n,H_kv,d] of `dtype`, the layout of a fused
+ *   projection: heads contiguous, tokens and batch entries at strides of their
+ *   own (elements, multiples of 16 bytes; k and v share theirs).
+ *   q_out: [B,H,n,d] contiguous, `dtype`.
+ *   k_cache, v_cache: [B,H_kv,>= t0+n,d] of `dtype`, plane stride cache_bh_stride,
+ *   or NULL and q8 an 8-bit cache (exactly one of the two).
+ *   heads (nullable): neither norm nor rotation. table_rows >= t0 + n.
+ * No output may overlap an input. |x| below 2^60 (sums of squares in 32 bits).
+ */
+int sparvar_qkv_append(int32_t B, int32_t H, int32_t H_kv, int32_t d, sparvar_dtype_t dtype, int32_t n,
+                       int32_t t0, const void* q, int64_t q_batch_stride, int64_t q_token_stride,
+                       const void* k, const void* v, int64_t kv_batch_stride, int64_t kv_token_stride,
+                       const sparvar_norm_rope_t* heads, void* q_out, void* k_cache, void* v_cache,
+                       int64_t cache_bh_stride, const sparvar_q8_cache_t* q8, hipStream_t stream);
+
+/*
+ * Writes rows [0, n) of k_src and v_src ([B,H_kv,n,d] of `dtype`, plane stride
+ * src_bh_stride) to tokens [t0, t0 + n) of an 8-bit cache.
+ */
+int sparvar_kv_quantize(int32_t B, int32_t H_kv, int32_t d, sparvar_dtype_t dtype, int32_t n, int32_t t0,
+                        const void* k_src, const void* v_src, int64_t src_bh_stride,
+                        const sparvar_q8_cache_t* q8, hipStream_t stream);
+
+/*
+ * Reads tokens [t0, t0 + n) of an 8-bit cache back to rows [0, n) of k_dst and
+ * v_dst ([B,H_kv,n,d] of `dtype`, plane stride dst_bh_stride). Exact in both
+ * types. The decision step, whose pooled scores take 16-bit keys, reads the
+ * cache up to its scale this way.
+ */
+int sparvar_kv_dequantize(int32_t B, int32_t H_kv, int32_t d, sparvar_dtype_t dtype, int32_t n, int32_t t0,
+                          const sparvar_q8_cache_t* q8, void* k_dst, void* v_dst, int64_t dst_bh_stride,
+                          hipStream_t stream);
+
+/*
+ * Dense attention over the first n_kv tokens of an 8-bit cache: the definition
+ * of sparvar_dense_attn_fwd on the values that the codes stand for (bf16 only).
+ *   q: [B,H,n_q,d] (plane stride q_bh_stride); o: [B,H,n_q,d] contiguous;
+ *   lse (nullable): [B,H,n_q] fp32.
+ *   kv_len (nullable): device int32 [B]; entry b attends to its first
+ *   min(max(kv_len[b], 0), n_kv) tokens. With none, o = 0 and lse = -inf.
+ *   workspace (nullable, 16-byte aligned): workspace_bytes of device memory, at
+ *   least what sparvar_dense_attn_q8_workspace gives for the same sizes on this
+ *   device (0: none is used). With it, calls of few rows cut the keys into parts
+ *   that run side by side and are joined in order by a second launch; without
+ *   it, every row is walked in one part. The last bits of o and lse may depend
+ *   on that. A workspace serves one call at a time: calls that may overlap,
+ *   replays of captured graphs among them, need one each.
+ */
+int64_t sparvar_dense_attn_q8_workspace(int32_t B, int32_t H, int32_t H_kv, int32_t n_q, int32_t n_kv,
+                                        int32_t d); /* bytes, < 0 on error */
+int sparvar_dense_attn_q8_fwd(int32_t B, int32_t H, int32_t H_kv, int32_t n_q, int32_t n_kv, int32_t d,
+                              sparvar_dtype_t dtype, const void* q, int64_t q_bh_stride,
+                              const sparvar_q8_cache_t* q8, const int32_t* kv_len, void* o, float* lse,
+                              float softmax_scale, void* workspace, int64_t workspace_bytes,
+                              hipStream_t stream);
+
+/*
+ * sparvar_block_sparse_attn_fwd over an 8-bit cache (bf16 queries and outputs):
+ * the same rows, launch orders of rows and outputs, on the values that the codes
+ * stand for. CSR rows stay per query head; an order of groups is not used.
+ */
+int sparvar_block_sparse_attn_q8_fwd(const sparvar_geometry_t* g, int32_t k, int32_t B, int32_t H,
+                                     int32_t H_kv, int32_t d, sparvar_dtype_t dtype, const void* q_k,
+                                     int64_t q_bh_stride, const sparvar_q8_cache_t* q8, void* o, float* lse,
+                                     float softmax_scale, const int32_t* row_ptr, const int32_t* col_idx,
+                                     const int32_t* schedule, hipStream_t stream);
+
 /* Static description of a status code. */
 const char* sparvar_status_string(int status);
 /* Message of the last failed call on this thread ("" if none). */

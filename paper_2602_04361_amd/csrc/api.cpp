@@ -298,6 +298,77 @@ int map_steps(const sparvar_geometry_t* g, int32_t S, int32_t n_steps, const int
                     "launch order launch");
 }
 
+// An 8-bit cache: the struct's own consistency, and room for `tokens` tokens.
+int check_q8(const sparvar_q8_cache_t* c, int32_t d, int64_t tokens, Q8View* v) {
+  if (!c) return fail(SPARVAR_ERR_INVALID, "the 8-bit cache is NULL");
+  if (c->block != 16 && c->block != 32 && c->block != 64 && c->block != 128)
+    return fail(SPARVAR_ERR_INVALID, "scale block %d is not 16, 32, 64 or 128", c->block);
+  if (c->capacity < 1) return fail(SPARVAR_ERR_INVALID, "cache capacity %d < 1", c->capacity);
+  if ((int64_t)c->capacity * d >= (int64_t(1) << 31))
+    return fail(SPARVAR_ERR_INVALID, "8-bit cache of %d tokens x %d exceeds 2^31 codes a plane", c->capacity, d);
+  if (tokens > c->capacity)
+    return fail(SPARVAR_ERR_CAPACITY, "%lld tokens exceed the cache's capacity %d", (long long)tokens, c->capacity);
+  if (!c->k || !c->v || !c->k_scale || !c->v_scale) return fail(SPARVAR_ERR_INVALID, "a pointer of the 8-bit cache is NULL");
+  if (!aligned16(c->k) || !aligned16(c->v)) return fail(SPARVAR_ERR_INVALID, "cache codes are not 16-byte aligned");
+  if (c->bh_stride < (int64_t)c->capacity * d || c->bh_stride % 16 != 0)
+    return fail(SPARVAR_ERR_INVALID, "code plane stride %lld < %lld or not a multiple of 16", (long long)c->bh_stride,
+                (long long)c->capacity * d);
+  const int64_t blocks = ((int64_t)c->capacity + c->block - 1) / c->block;
+  if (c->scale_bh_stride < blocks)
+    return fail(SPARVAR_ERR_INVALID, "scale plane stride %lld < %lld blocks", (long long)c->scale_bh_stride, (long long)blocks);
+  v->k = static_cast<uint8_t*>(c->k);
+  v->v = static_cast<uint8_t*>(c->v);
+  v->ks = c->k_scale;
+  v->vs = c->v_scale;
+  v->bh_stride = c->bh_stride;
+  v->sc_stride = c->scale_bh_stride;
+  v->lg = 0;
+  while ((1 << v->lg) < c->block) ++v->lg;
+  return SPARVAR_OK;
+}
+
+// Batch, heads and appended tokens: every count of planes, rows and workgroups below 2^31.
+int check_tokens(int32_t B, int32_t H, int32_t H_kv, int32_t d, int32_t n, int32_t t0) {
+  if (B < 1 || H < 1 || H_kv < 1 || n < 1) return fail(SPARVAR_ERR_INVALID, "B, heads and n must be >= 1");
+  if (t0 < 0 || (int64_t)t0 + n >= (int64_t(1) << 31)) return fail(SPARVAR_ERR_INVALID, "tokens [%d, %d + %d) out of range", t0, t0, n);
+  if ((int64_t)B * H >= (int64_t(1) << 31) || (int64_t)B * H_kv >= (int64_t(1) << 31) ||
+      (int64_t)B * H * n >= (int64_t(1) << 31) || (int64_t)B * H_kv * n >= (int64_t(1) << 31))
+    return fail(SPARVAR_ERR_INVALID, "B * heads * n too large");
+  if ((int64_t)n * d >= (int64_t(1) << 31)) return fail(SPARVAR_ERR_INVALID, "n x d exceeds 2^31");
+  // a workgroup takes at least a sixteenth of a block, a token group or 4096 codes, K and V apart
+  if (((int64_t)B * H + 2 * (int64_t)B * H_kv) * ((int64_t)n / 16 + 2) >= (int64_t(1) << 31))
+    return fail(SPARVAR_ERR_INVALID, "too many rows for one launch");
+  return SPARVAR_OK;
+}
+
+int check_heads(int32_t B, int32_t H, int32_t H_kv) {
+  if (B < 1 || H < 1 || H_kv < 1) return fail(SPARVAR_ERR_INVALID, "B, H and H_kv must be >= 1");
+  if (H % H_kv != 0) return fail(SPARVAR_ERR_INVALID, "H = %d is not a multiple of H_kv = %d", H, H_kv);
+  return SPARVAR_OK;
+}
+
+// A token-major tensor [B, n, heads, d]: heads contiguous, tokens and entries at strides.
+int check_rows(const void* p, int64_t batch, int64_t token, int64_t row, int32_t B, int32_t n, int elem, const char* name) {
+  if (!p) return fail(SPARVAR_ERR_INVALID, "%s is NULL", name);
+  if (!aligned16(p)) return fail(SPARVAR_ERR_INVALID, "%s is not 16-byte aligned", name);
+  if ((n > 1 && token < row) || token < 0) return fail(SPARVAR_ERR_INVALID, "%s token stride %lld < heads * d = %lld", name,
+                                                       (long long)token, (long long)row);
+  if (batch < 0 || (B > 1 && batch < row)) return fail(SPARVAR_ERR_INVALID, "%s batch stride %lld", name, (long long)batch);
+  if (token * elem % 16 != 0 || batch * elem % 16 != 0)
+    return fail(SPARVAR_ERR_INVALID, "%s strides are not multiples of 16 bytes", name);
+  return SPARVAR_OK;
+}
+
+int check_dense_q8(int32_t B, int32_t H, int32_t H_kv, int32_t n_q, int32_t n_kv, int32_t d) {
+  int st = check_dtype_d(SPARVAR_BF16, d);
+  if (st) return st;
+  if ((st = check_heads(B, H, H_kv))) return st;
+  if (n_q < 1 || n_kv < 1) return fail(SPARVAR_ERR_INVALID, "n_q and n_kv must be >= 1");
+  // (the parts of a call are at most 64 and only taken by calls of few rows)
+  if ((int64_t)B * H * n_q >= (int64_t(1) << 31)) return fail(SPARVAR_ERR_INVALID, "B*H*n_q too large");
+  return SPARVAR_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -897,6 +968,193 @@ int sparvar_block_sparse_attn_fwd(const sparvar_geometry_t* g, int32_t k, int32_
   a.group_stages = opt(SPARVAR_OPT_SPARSE_GROUP_STAGES);
   a.num_cu = device_cus();
   return hip_status(launch_sparse_attn(a, stream), "block-sparse attention launch");
+}
+
+int sparvar_qkv_append(int32_t B, int32_t H, int32_t H_kv, int32_t d, sparvar_dtype_t dtype, int32_t n,
+                       int32_t t0, const void* q, int64_t q_batch_stride, int64_t q_token_stride,
+                       const void* k, const void* v, int64_t kv_batch_stride, int64_t kv_token_stride,
+                       const sparvar_norm_rope_t* heads, void* q_out, void* k_cache, void* v_cache,
+                       int64_t cache_bh_stride, const sparvar_q8_cache_t* q8, hipStream_t stream) {
+  int st = check_dtype_d(dtype, d);
+  if (st) return st;
+  if ((st = check_heads(B, H, H_kv))) return st;
+  if ((st = check_tokens(B, H, H_kv, d, n, t0))) return st;
+  const int elem = dtype == SPARVAR_BF16 ? 2 : 4;
+  if ((st = check_rows(q, q_batch_stride, q_token_stride, (int64_t)H * d, B, n, elem, "q"))) return st;
+  if ((st = check_rows(k, kv_batch_stride, kv_token_stride, (int64_t)H_kv * d, B, n, elem, "k"))) return st;
+  if ((st = check_rows(v, kv_batch_stride, kv_token_stride, (int64_t)H_kv * d, B, n, elem, "v"))) return st;
+  if ((st = check_plane(q_out, (int64_t)n * d, n, d, elem, "q_out"))) return st;
+  AppendArgs a;
+  a.map = HeadMap{SPARVAR_NORM_NONE, SPARVAR_ROPE_PAIRS, 0.f, nullptr, nullptr, nullptr};
+  if (heads) {
+    if (heads->norm < SPARVAR_NORM_NONE || heads->norm > SPARVAR_NORM_L2)
+      return fail(SPARVAR_ERR_INVALID, "norm %d unknown", heads->norm);
+    if (heads->layout != SPARVAR_ROPE_PAIRS && heads->layout != SPARVAR_ROPE_HALVES)
+      return fail(SPARVAR_ERR_INVALID, "rotation layout %d unknown", heads->layout);
+    if (!std::isfinite(heads->eps) || heads->eps < 0.f) return fail(SPARVAR_ERR_INVALID, "eps %g is not finite and >= 0", heads->eps);
+    if (heads->cos_sin && heads->table_rows < t0 + n)
+      return fail(SPARVAR_ERR_CAPACITY, "rotation table of %d rows ends before token %d", heads->table_rows, t0 + n);
+    if (!aligned16(heads->q_weight) || !aligned16(heads->k_weight) || !aligned16(heads->cos_sin))
+      return fail(SPARVAR_ERR_INVALID, "weights and the rotation table must be 16-byte aligned");
+    a.map = HeadMap{heads->norm, heads->layout, heads->eps, heads->q_weight, heads->k_weight, heads->cos_sin};
+  }
+  if ((k_cache || v_cache) == (q8 != nullptr))
+    return fail(SPARVAR_ERR_INVALID, "either k_cache and v_cache or an 8-bit cache is required");
+  a.q8 = q8 != nullptr;
+  a.c8 = Q8View{};
+  if (q8) {
+    if ((st = check_q8(q8, d, (int64_t)t0 + n, &a.c8))) return st;
+  } else {
+    if ((st = check_plane(k_cache, cache_bh_stride, (int64_t)t0 + n, d, elem, "k_cache"))) return st;
+    if ((st = check_plane(v_cache, cache_bh_stride, (int64_t)t0 + n, d, elem, "v_cache"))) return st;
+  }
+  a.B = B;
+  a.H = H;
+  a.H_kv = H_kv;
+  a.d = d;
+  a.n = n;
+  a.t0 = t0;
+  a.bf16 = dtype == SPARVAR_BF16;
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.q_batch = q_batch_stride;
+  a.q_token = q_token_stride;
+  a.kv_batch = kv_batch_stride;
+  a.kv_token = kv_token_stride;
+  a.q_out = q_out;
+  a.k_cache = k_cache;
+  a.v_cache = v_cache;
+  a.cache_bh_stride = cache_bh_stride;
+  return hip_status(launch_qkv_append(a, stream), "append launch");
+}
+
+int sparvar_kv_quantize(int32_t B, int32_t H_kv, int32_t d, sparvar_dtype_t dtype, int32_t n, int32_t t0,
+                        const void* k_src, const void* v_src, int64_t src_bh_stride,
+                        const sparvar_q8_cache_t* q8, hipStream_t stream) {
+  int st = check_dtype_d(dtype, d);
+  if (st) return st;
+  if ((st = check_tokens(B, H_kv, H_kv, d, n, t0))) return st;
+  const int elem = dtype == SPARVAR_BF16 ? 2 : 4;
+  if ((st = check_plane(k_src, src_bh_stride, n, d, elem, "k_src"))) return st;
+  if ((st = check_plane(v_src, src_bh_stride, n, d, elem, "v_src"))) return st;
+  KvQuantizeArgs a;
+  if ((st = check_q8(q8, d, (int64_t)t0 + n, &a.c8))) return st;
+  a.planes = B * H_kv;
+  a.d = d;
+  a.n = n;
+  a.t0 = t0;
+  a.bf16 = dtype == SPARVAR_BF16;
+  a.k = k_src;
+  a.v = v_src;
+  a.bh_stride = src_bh_stride;
+  return hip_status(launch_kv_quantize(a, stream), "kv quantize launch");
+}
+
+int sparvar_kv_dequantize(int32_t B, int32_t H_kv, int32_t d, sparvar_dtype_t dtype, int32_t n, int32_t t0,
+                          const sparvar_q8_cache_t* q8, void* k_dst, void* v_dst, int64_t dst_bh_stride,
+                          hipStream_t stream) {
+  int st = check_dtype_d(dtype, d);
+  if (st) return st;
+  if ((st = check_tokens(B, H_kv, H_kv, d, n, t0))) return st;
+  const int elem = dtype == SPARVAR_BF16 ? 2 : 4;
+  if ((st = check_plane(k_dst, dst_bh_stride, n, d, elem, "k_dst"))) return st;
+  if ((st = check_plane(v_dst, dst_bh_stride, n, d, elem, "v_dst"))) return st;
+  KvDequantizeArgs a;
+  if ((st = check_q8(q8, d, (int64_t)t0 + n, &a.c8))) return st;
+  a.planes = B * H_kv;
+  a.d = d;
+  a.n = n;
+  a.t0 = t0;
+  a.bf16 = dtype == SPARVAR_BF16;
+  a.k = k_dst;
+  a.v = v_dst;
+  a.bh_stride = dst_bh_stride;
+  return hip_status(launch_kv_dequantize(a, stream), "kv dequantize launch");
+}
+
+int64_t sparvar_dense_attn_q8_workspace(int32_t B, int32_t H, int32_t H_kv, int32_t n_q, int32_t n_kv,
+                                        int32_t d) {
+  const int st = check_dense_q8(B, H, H_kv, n_q, n_kv, d);
+  if (st) return st;
+  ok();
+  return dense_q8_workspace(B, H, H_kv, n_q, n_kv, d, device_cus());
+}
+
+int sparvar_dense_attn_q8_fwd(int32_t B, int32_t H, int32_t H_kv, int32_t n_q, int32_t n_kv, int32_t d,
+                              sparvar_dtype_t dtype, const void* q, int64_t q_bh_stride,
+                              const sparvar_q8_cache_t* q8, const int32_t* kv_len, void* o, float* lse,
+                              float softmax_scale, void* workspace, int64_t workspace_bytes,
+                              hipStream_t stream) {
+  if (dtype != SPARVAR_BF16) return fail(SPARVAR_ERR_UNSUPPORTED, "attention over an 8-bit cache takes bf16 queries only");
+  int st = check_dense_q8(B, H, H_kv, n_q, n_kv, d);
+  if (st) return st;
+  if ((st = check_softmax_scale(softmax_scale))) return st;
+  if ((st = check_plane(q, q_bh_stride, n_q, d, 2, "q"))) return st;
+  if ((st = check_plane(o, (int64_t)n_q * d, n_q, d, 2, "o"))) return st;
+  DenseQ8Args a;
+  if ((st = check_q8(q8, d, n_kv, &a.c8))) return st;
+  a.num_cu = device_cus();
+  const int64_t need = workspace ? dense_q8_workspace(B, H, H_kv, n_q, n_kv, d, a.num_cu) : 0;
+  if (need > 0) {
+    if (workspace_bytes < need)
+      return fail(SPARVAR_ERR_CAPACITY, "workspace of %lld bytes < %lld", (long long)workspace_bytes, (long long)need);
+    if (!aligned16(workspace)) return fail(SPARVAR_ERR_INVALID, "workspace is not 16-byte aligned");
+  }
+  a.B = B;
+  a.H = H;
+  a.H_kv = H_kv;
+  a.n_q = n_q;
+  a.n_kv = n_kv;
+  a.d = d;
+  a.q = q;
+  a.o = o;
+  a.lse = lse;
+  a.q_bh_stride = q_bh_stride;
+  a.kv_len = kv_len;
+  a.softmax_scale = softmax_scale;
+  a.workspace = need > 0 ? static_cast<float*>(workspace) : nullptr;
+  a.swizzle = opt(SPARVAR_OPT_SWIZZLE);
+  return hip_status(launch_dense_attn_q8(a, stream), "dense 8-bit attention launch");
+}
+
+int sparvar_block_sparse_attn_q8_fwd(const sparvar_geometry_t* g, int32_t k, int32_t B, int32_t H,
+                                     int32_t H_kv, int32_t d, sparvar_dtype_t dtype, const void* q_k,
+                                     int64_t q_bh_stride, const sparvar_q8_cache_t* q8, void* o, float* lse,
+                                     float softmax_scale, const int32_t* row_ptr, const int32_t* col_idx,
+                                     const int32_t* schedule, hipStream_t stream) {
+  GeoTable T;
+  int st = build_table(g, &T);
+  if (st) return st;
+  if (k < 1 || k > T.L) return fail(SPARVAR_ERR_INVALID, "scale %d outside [1, %d]", k, T.L);
+  if (dtype != SPARVAR_BF16) return fail(SPARVAR_ERR_UNSUPPORTED, "attention over an 8-bit cache takes bf16 queries only");
+  if ((st = check_dtype_d(dtype, d))) return st;
+  if ((st = check_heads(B, H, H_kv))) return st;
+  const int32_t Nk = T.h[k - 1] * T.w[k - 1];
+  if ((int64_t)B * H * Nk >= (int64_t(1) << 31)) return fail(SPARVAR_ERR_INVALID, "B*H*N_k too large");
+  if ((st = check_softmax_scale(softmax_scale))) return st;
+  if (!row_ptr || !col_idx) return fail(SPARVAR_ERR_INVALID, "row_ptr/col_idx is NULL");
+  if ((st = check_plane(q_k, q_bh_stride, Nk, d, 2, "q_k"))) return st;
+  if ((st = check_plane(o, (int64_t)Nk * d, Nk, d, 2, "o"))) return st;
+  SparseQ8Args a;
+  if ((st = check_q8(q8, d, T.C[k], &a.c8))) return st;
+  a.G = &T;
+  a.k = k;
+  a.BH = B * H;
+  a.H = H;
+  a.H_kv = H_kv;
+  a.d = d;
+  a.q = q_k;
+  a.o = o;
+  a.lse = lse;
+  a.q_bh_stride = q_bh_stride;
+  a.softmax_scale = softmax_scale;
+  a.row_ptr = row_ptr;
+  a.col_idx = col_idx;
+  a.schedule = schedule;
+  a.swizzle = opt(SPARVAR_OPT_SWIZZLE);
+  a.num_cu = device_cus();
+  return hip_status(launch_sparse_attn_q8(a, stream), "block-sparse 8-bit attention launch");
 }
 
 }  // extern "C"

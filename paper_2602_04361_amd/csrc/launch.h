@@ -132,6 +132,83 @@ struct KvCompactArgs {
 };
 hipError_t launch_kv_compact(const KvCompactArgs& a, hipStream_t stream);
 
+// An 8-bit cache: e4m3 codes and E8M0 scale bytes, one a block of 1 << lg tokens.
+struct Q8View {
+  uint8_t *k, *v, *ks, *vs;
+  int64_t bh_stride, sc_stride;  // bytes between planes of codes, of scales
+  int32_t lg;
+};
+
+struct HeadMap {  // norm, weight and rotation of query and key vectors
+  int32_t norm, layout;
+  float eps;
+  const float *q_weight, *k_weight, *cos_sin;
+};
+
+struct AppendArgs {
+  int32_t B, H, H_kv, d, n, t0;
+  bool bf16;
+  const void *q, *k, *v;
+  int64_t q_batch, q_token, kv_batch, kv_token;  // elements
+  HeadMap map;
+  void *q_out, *k_cache, *v_cache;
+  int64_t cache_bh_stride;
+  bool q8;
+  Q8View c8;
+  int num_cu;
+};
+hipError_t launch_qkv_append(const AppendArgs& a, hipStream_t stream);
+
+struct KvQuantizeArgs {
+  int32_t planes, d, n, t0;
+  bool bf16;
+  const void *k, *v;
+  int64_t bh_stride;  // elements
+  Q8View c8;
+};
+hipError_t launch_kv_quantize(const KvQuantizeArgs& a, hipStream_t stream);
+
+struct KvDequantizeArgs {
+  int32_t planes, d, n, t0;
+  bool bf16;
+  void *k, *v;
+  int64_t bh_stride;  // elements
+  Q8View c8;
+};
+hipError_t launch_kv_dequantize(const KvDequantizeArgs& a, hipStream_t stream);
+
+struct DenseQ8Args {
+  int32_t B, H, H_kv, n_q, n_kv, d;
+  const void* q;
+  void* o;
+  float* lse;
+  int64_t q_bh_stride;
+  Q8View c8;
+  const int32_t* kv_len;
+  float softmax_scale;
+  float* workspace;  // nullable: one part
+  int swizzle;
+  int num_cu;
+};
+// Bytes of workspace that a call of these sizes takes (0: it walks its keys in one part).
+int64_t dense_q8_workspace(int32_t B, int32_t H, int32_t H_kv, int32_t n_q, int32_t n_kv, int32_t d, int num_cu);
+hipError_t launch_dense_attn_q8(const DenseQ8Args& a, hipStream_t stream);
+
+struct SparseQ8Args {
+  const GeoTable* G;
+  int32_t k, BH, H, H_kv, d;
+  const void* q;
+  void* o;
+  float* lse;
+  int64_t q_bh_stride;
+  Q8View c8;
+  float softmax_scale;
+  const int32_t *row_ptr, *col_idx, *schedule;
+  int swizzle;
+  int num_cu;
+};
+hipError_t launch_sparse_attn_q8(const SparseQ8Args& a, hipStream_t stream);
+
 // Work items of the bf16 block-sparse launch at scale k (with the default
 // waves, chunk and stages): one query tile per workgroup (gh = gw = 0), or groups
 // of gh x gw neighbouring tiles per workgroup. group_waves: as in SparseAttnArgs.

@@ -11,6 +11,7 @@ current stream:
   map_all():  the rows of every step in one sparvar_map_index_steps launch
               (they depend only on the selection at S).
 Local rows are geometry-only and built once per step by build_local().
+Q8SparsePath runs the same steps from the projections on, over an 8-bit cache.
 All arithmetic runs in libsparvar.so; this module only allocates and calls.
 """
 from __future__ import annotations
@@ -223,3 +224,69 @@ class CslaPath:
                                  K_all[:, :, :i["n_tokens_le"]], V_all[:, :, :i["n_tokens_le"]], self.out[k],
                                  self.block_rows[k], softmax_scale=self.scale)
         return self.out[k]
+
+
+class Q8SparsePath(SparsePath):
+    """One layer over an 8-bit cache that grows scale by scale, as C-ABI calls.
+
+    step(l, q, k, v) takes scale l's projections [B, N_l, heads, d], scales in order:
+      append:    norms, rotation and the scale's tokens into the cache
+                 (sparvar_qkv_append);
+      l < S:     dense attention over the cache (sparvar_dense_attn_q8_fwd);
+      l == S:    the cache up to S read back to 16 bits (sparvar_kv_dequantize), the
+                 decision step on it, and the rows of every later step;
+      l in steps: block-sparse attention over the cache
+                 (sparvar_block_sparse_attn_q8_fwd); any other l > S: dense.
+    heads: a NormRope whose table has a row for every cache token, or None.
+    block: tokens of a scale of the cache.
+    """
+
+    def __init__(self, geom: sv.Geometry, S, steps, B, H, d, topk, radius, heads=None, block=64, device="cuda", **kw):
+        super().__init__(geom, S, steps, B, H, d, topk, radius, device=device, **kw)
+        self.heads = heads
+        bf = dict(dtype=torch.bfloat16, device=device)
+        total = self.info[len(geom.h)]["n_tokens_le"]
+        self.q8 = sv.Q8Cache.empty(B, H, total, d, block, device)
+        self.kv_S = [torch.empty(B, H, self.info[S]["n_tokens_le"], d, **bf) for _ in range(2)]
+        self.q = {l: torch.empty(B, H, i["n_tokens"], d, **bf) for l, i in self.info.items()}
+        self.out[self.S] = self.o_S
+        need = 0
+        for l, i in self.info.items():
+            if l != self.S and l not in self.steps:
+                self.out[l] = torch.empty(B, H, i["n_tokens"], d, **bf)
+                need = max(need, sv.sparvar_dense_attn_q8_workspace(B, H, H, i["n_tokens"], i["n_tokens_le"], d))
+        self.workspace = torch.empty(need, dtype=torch.uint8, device=device) if need else None
+
+    def append(self, l, q, k, v):
+        sv.sparvar_qkv_append(q, k, v, self.info[l]["token_offset"], self.heads, self.q[l], q8=self.q8)
+
+    def dense(self, l):
+        sv.sparvar_dense_attn_q8_fwd(self.q[l], self.q8, self.info[l]["n_tokens_le"], self.out[l],
+                                     softmax_scale=self.scale, workspace=self.workspace)
+
+    def decision(self):
+        k, v = self.kv_S
+        sv.sparvar_kv_dequantize(self.q8, 0, k, v)
+        sv.sparvar_decision_step(self.g, self.S, self.q[self.S], k, v, self.o_S, self.lse_S, self.scores, self.topk,
+                                 self.topk_idx, softmax_scale=self.scale)
+        self.map_all()
+
+    def attn_step(self, k):
+        rp, ci, _ = self.csr[k]
+        sv.sparvar_block_sparse_attn_q8_fwd(self.g, k, self.q[k], self.q8, self.out[k], rp, ci, softmax_scale=self.scale)
+
+    def step(self, l, q, k, v):
+        """Scale l from its projections to its attention output."""
+        self.append(l, q, k, v)
+        if l == self.S:
+            self.decision()
+        elif l in self.steps:
+            self.attn_step(l)
+        else:
+            self.dense(l)
+        return self.out[l]
+
+    def run(self, projections):
+        """Every scale in order; projections: (q, k, v) of each."""
+        for l, (q, k, v) in enumerate(projections, 1):
+            self.step(l, q, k, v)

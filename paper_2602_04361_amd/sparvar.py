@@ -43,6 +43,12 @@ EXPORTS = [
     "sparvar_map_index_capacity",
     "sparvar_map_index",
     "sparvar_block_sparse_attn_fwd",
+    "sparvar_qkv_append",
+    "sparvar_kv_quantize",
+    "sparvar_kv_dequantize",
+    "sparvar_dense_attn_q8_workspace",
+    "sparvar_dense_attn_q8_fwd",
+    "sparvar_block_sparse_attn_q8_fwd",
     "sparvar_status_string",
     "sparvar_last_error",
     "sparvar_set_launch_option",
@@ -58,6 +64,10 @@ OPT_DEFAULT = -(1 << 31)
 PROJECT_POINT, PROJECT_COVER = 0, 1
 PROJECTIONS = {"point": PROJECT_POINT, "cover": PROJECT_COVER, PROJECT_POINT: PROJECT_POINT,
                PROJECT_COVER: PROJECT_COVER}
+
+# sparvar_norm_t, sparvar_rope_layout_t
+NORMS = {None: 0, "rms": 1, "l2": 2}
+ROPE_LAYOUTS = {"pairs": 0, "halves": 1}
 
 
 class SparvarError(RuntimeError):
@@ -82,6 +92,31 @@ class _CScaleInfo(ctypes.Structure):
         "tiles_h", "tiles_w", "block_offset", "n_blocks_le")]
 
 
+class _CQ8Cache(ctypes.Structure):
+    _fields_ = [
+        ("block", ctypes.c_int32),
+        ("capacity", ctypes.c_int32),
+        ("k", ctypes.c_void_p),
+        ("v", ctypes.c_void_p),
+        ("bh_stride", ctypes.c_int64),
+        ("k_scale", ctypes.c_void_p),
+        ("v_scale", ctypes.c_void_p),
+        ("scale_bh_stride", ctypes.c_int64),
+    ]
+
+
+class _CNormRope(ctypes.Structure):
+    _fields_ = [
+        ("norm", ctypes.c_int32),
+        ("layout", ctypes.c_int32),
+        ("eps", ctypes.c_float),
+        ("table_rows", ctypes.c_int32),
+        ("q_weight", ctypes.c_void_p),
+        ("k_weight", ctypes.c_void_p),
+        ("cos_sin", ctypes.c_void_p),
+    ]
+
+
 _lib = None
 
 
@@ -95,6 +130,7 @@ def load_library(path: str = LIB_PATH):
     lib = ctypes.CDLL(path)
     i32, i64, f32, vp = ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_void_p
     G = ctypes.POINTER(_CGeometry)
+    Q8, NR = ctypes.POINTER(_CQ8Cache), ctypes.POINTER(_CNormRope)
     sig = {
         "sparvar_scale_info": (ctypes.c_int, [G, i32, ctypes.POINTER(_CScaleInfo)]),
         "sparvar_dense_attn_fwd": (ctypes.c_int, [i32, i32, i32, i32, i32, ctypes.c_int, vp, i64, vp, vp, i64, vp,
@@ -126,6 +162,15 @@ def load_library(path: str = LIB_PATH):
                                              vp, vp]),
         "sparvar_block_sparse_attn_fwd": (ctypes.c_int, [G, i32, i32, i32, i32, ctypes.c_int, vp, i64, vp, vp, i64,
                                                          vp, vp, f32, vp, vp, vp, vp]),
+        "sparvar_qkv_append": (ctypes.c_int, [i32, i32, i32, i32, ctypes.c_int, i32, i32, vp, i64, i64, vp, vp, i64, i64,
+                                              NR, vp, vp, vp, i64, Q8, vp]),
+        "sparvar_kv_quantize": (ctypes.c_int, [i32, i32, i32, ctypes.c_int, i32, i32, vp, vp, i64, Q8, vp]),
+        "sparvar_kv_dequantize": (ctypes.c_int, [i32, i32, i32, ctypes.c_int, i32, i32, Q8, vp, vp, i64, vp]),
+        "sparvar_dense_attn_q8_workspace": (i64, [i32, i32, i32, i32, i32, i32]),
+        "sparvar_dense_attn_q8_fwd": (ctypes.c_int, [i32, i32, i32, i32, i32, i32, ctypes.c_int, vp, i64, Q8, vp, vp, vp,
+                                                     f32, vp, i64, vp]),
+        "sparvar_block_sparse_attn_q8_fwd": (ctypes.c_int, [G, i32, i32, i32, i32, i32, ctypes.c_int, vp, i64, Q8, vp, vp,
+                                                            f32, vp, vp, vp, vp]),
         "sparvar_status_string": (ctypes.c_char_p, [ctypes.c_int]),
         "sparvar_last_error": (ctypes.c_char_p, []),
         "sparvar_set_launch_option": (ctypes.c_int, [i32, i32]),
@@ -460,4 +505,233 @@ def sparvar_block_sparse_attn_fwd(geom, k, q_k, k_lek, v_lek, o, row_ptr, col_id
                                              _plane_stride(k_lek, "k_lek"), _ptr(o), _ptr(lse),
                                              _scale(softmax_scale, d), _ptr(row_ptr), _ptr(col_idx),
                                              _ptr(schedule), _stream(stream)))
+    return o, lse
+
+
+# ---------------------------------------------------------------- 8-bit cache
+def _here(*tensors):
+    """Every tensor is on the current device (None: not given)."""
+    torch = _torch()
+    dev = None
+    for t in tensors:
+        if t is None:
+            continue
+        if dev is None:
+            if not t.is_cuda:
+                raise SparvarError(ERR_INVALID, f"a tensor is on {t.device}, not on a GPU")
+            dev = torch.cuda.current_device()
+        if t.get_device() != dev:
+            raise SparvarError(ERR_INVALID, f"a tensor is on {t.device}, the current device is cuda:{dev}")
+
+
+def _same(name, t, shape, dtype):
+    """t is a contiguous tensor of that shape and dtype."""
+    if t.dtype != dtype:
+        raise SparvarError(ERR_INVALID, f"{name} is {t.dtype}, {dtype} is required")
+    if t.shape != shape or not t.is_contiguous():
+        raise SparvarError(ERR_INVALID, f"{name} must be a contiguous {list(shape)} tensor")
+
+
+class Q8Cache:
+    """Host-side sparvar_q8_cache_t over device tensors: codes k, v [B,H_kv,capacity,d] (float8_e4m3fn, or their bytes as
+    uint8) and scale bytes k_scale, v_scale [B,H_kv,ceil(capacity / block)] (uint8 or float8_e8m0fnu)."""
+
+    def __init__(self, k, v, k_scale, v_scale, block):
+        torch = _torch()
+        for name, t, types in (("k", k, (torch.float8_e4m3fn, torch.uint8)), ("v", v, (torch.float8_e4m3fn, torch.uint8)),
+                               ("k_scale", k_scale, (torch.uint8, torch.float8_e8m0fnu)),
+                               ("v_scale", v_scale, (torch.uint8, torch.float8_e8m0fnu))):
+            if t.dtype not in types:
+                raise SparvarError(ERR_UNSUPPORTED, f"{name} is {t.dtype}")
+        if block not in (16, 32, 64, 128):
+            raise SparvarError(ERR_INVALID, f"scale block {block} is not 16, 32, 64 or 128")
+        self.bh_stride = _plane_stride(k, "k")
+        self.B, self.H_kv, self.capacity, self.d = k.shape
+        if k.shape != v.shape or _plane_stride(v, "v") != self.bh_stride:
+            raise SparvarError(ERR_INVALID, "k and v must share their shape and plane stride")
+        blocks = -(-self.capacity // block)
+        for name, t in (("k_scale", k_scale), ("v_scale", v_scale)):
+            if t.dim() != 3 or t.shape[:2] != k.shape[:2] or t.shape[2] < blocks or t.stride(2) != 1 or \
+                    t.stride(1) != k_scale.stride(1) or (self.B > 1 and t.stride(0) != self.H_kv * t.stride(1)):
+                raise SparvarError(ERR_INVALID, f"{name} must be [B,H_kv,>= {blocks}] with evenly spaced planes, as the other's")
+        self.block, self.k, self.v, self.k_scale, self.v_scale = int(block), k, v, k_scale, v_scale
+        self.c = _CQ8Cache(self.block, self.capacity, k.data_ptr(), v.data_ptr(), self.bh_stride, k_scale.data_ptr(),
+                           v_scale.data_ptr(), k_scale.stride(1))
+        self.ref = ctypes.byref(self.c)
+
+    @classmethod
+    def empty(cls, B, H_kv, capacity, d, block=64, device="cuda"):
+        """A cache of unwritten tokens."""
+        torch = _torch()
+        code = dict(dtype=torch.float8_e4m3fn, device=device)
+        scale = dict(dtype=torch.uint8, device=device)
+        blocks = -(-capacity // block)
+        return cls(torch.empty(B, H_kv, capacity, d, **code), torch.empty(B, H_kv, capacity, d, **code),
+                   torch.empty(B, H_kv, blocks, **scale), torch.empty(B, H_kv, blocks, **scale), block)
+
+
+class NormRope:
+    """Host-side sparvar_norm_rope_t: norm None, "rms" or "l2"; fp32 weights [H,d] and [H_kv,d]; cos_sin fp32
+    [rows, d/2, 2], a row for each cache token; layout "pairs" (2i, 2i+1) or "halves" (i, i + d/2)."""
+
+    def __init__(self, norm=None, eps=0.0, q_weight=None, k_weight=None, cos_sin=None, layout="pairs"):
+        torch = _torch()
+        if norm not in NORMS:
+            raise SparvarError(ERR_INVALID, f"norm {norm!r} unknown")
+        if layout not in ROPE_LAYOUTS:
+            raise SparvarError(ERR_INVALID, f"rotation layout {layout!r} unknown")
+        for name, t, dim in (("q_weight", q_weight, 2), ("k_weight", k_weight, 2), ("cos_sin", cos_sin, 3)):
+            if t is not None and (t.dtype != torch.float32 or t.dim() != dim or not t.is_contiguous()):
+                raise SparvarError(ERR_INVALID, f"{name} must be contiguous fp32 with {dim} axes")
+        if cos_sin is not None and cos_sin.shape[2] != 2:
+            raise SparvarError(ERR_INVALID, "cos_sin must be [rows, d/2, 2]")
+        self.q_weight, self.k_weight, self.cos_sin = q_weight, k_weight, cos_sin
+        self.c = _CNormRope(NORMS[norm], ROPE_LAYOUTS[layout], float(eps), 0 if cos_sin is None else cos_sin.shape[0],
+                            _ptr(q_weight), _ptr(k_weight), _ptr(cos_sin))
+        self.ref = ctypes.byref(self.c)
+
+
+def _token_strides(t, name):
+    """Batch and token stride of a [B,n,heads,d] tensor whose heads are contiguous."""
+    if t.dim() != 4:
+        raise SparvarError(ERR_INVALID, f"{name} must be [B,n,heads,d]")
+    stride = t.stride()
+    if stride[3] != 1 or (stride[2] != t.shape[3] and t.shape[2] > 1):
+        raise SparvarError(ERR_INVALID, f"{name} heads must be contiguous")
+    # (an axis of one has no stride of its own; any multiple of 16 bytes will do)
+    return stride[0] if t.shape[0] > 1 else 0, stride[1] if t.shape[1] > 1 else t.shape[2] * t.shape[3]
+
+
+def sparvar_qkv_append(q, k, v, t0, heads, q_out, k_cache=None, v_cache=None, q8=None, stream=None):
+    """Norms, rotation (heads, a NormRope or None) and the append of tokens [t0, t0 + n): queries to q_out [B,H,n,d], keys
+    and values to k_cache, v_cache or to an 8-bit cache q8; see sparvar.h."""
+    lib = load_library()
+    B, n, H, d = q.shape
+    H_kv = k.shape[2]
+    qb, qt = _token_strides(q, "q")
+    kb, kt = _token_strides(k, "k")
+    if v.shape != k.shape or _token_strides(v, "v") != (kb, kt):
+        raise SparvarError(ERR_INVALID, "k and v must share their shape and strides")
+    if k.shape != (B, n, H_kv, d):
+        raise SparvarError(ERR_INVALID, "q and k must share batch, tokens and d")
+    dt = _dtype_code(q)
+    if k.dtype != q.dtype or v.dtype != q.dtype:
+        raise SparvarError(ERR_INVALID, "q, k and v must share a dtype")
+    _same("q_out", q_out, (B, H, n, d), q.dtype)
+    _here(q, k, v, q_out, k_cache, v_cache)
+    if heads is not None:
+        for name, t, shape in (("q_weight", heads.q_weight, (H, d)), ("k_weight", heads.k_weight, (H_kv, d))):
+            if t is not None and t.shape != shape:
+                raise SparvarError(ERR_INVALID, f"{name} must be {list(shape)}")
+        if heads.cos_sin is not None and heads.cos_sin.shape[1] * 2 != d:
+            raise SparvarError(ERR_INVALID, "cos_sin must be [rows, d/2, 2]")
+        _here(heads.q_weight, heads.k_weight, heads.cos_sin)
+    cs = 0
+    if k_cache is not None and v_cache is not None:
+        cs = _plane_stride(k_cache, "k_cache")
+        if v_cache.shape != k_cache.shape or _plane_stride(v_cache, "v_cache") != cs:
+            raise SparvarError(ERR_INVALID, "k_cache and v_cache must share their shape and plane stride")
+        if k_cache.dtype != q.dtype or v_cache.dtype != q.dtype or k_cache.shape[:2] != (B, H_kv) or k_cache.shape[3] != d:
+            raise SparvarError(ERR_INVALID, f"the caches must be [{B},{H_kv},tokens,{d}] of {q.dtype}")
+        if t0 + n > k_cache.shape[2]:
+            raise SparvarError(ERR_CAPACITY, f"tokens up to {t0 + n} exceed the cache's {k_cache.shape[2]}")
+    if q8 is not None:
+        _check_q8(q8, B, H_kv, d)
+    _check(lib.sparvar_qkv_append(B, H, H_kv, d, dt, n, t0, _ptr(q), qb, qt, _ptr(k), _ptr(v), kb, kt,
+                                  None if heads is None else heads.ref, _ptr(q_out), _ptr(k_cache), _ptr(v_cache), cs,
+                                  None if q8 is None else q8.ref, _stream(stream)))
+    return q_out
+
+
+def _check_q8(q8, B, H_kv, d):
+    if (q8.B, q8.H_kv, q8.d) != (B, H_kv, d):
+        raise SparvarError(ERR_INVALID, f"the cache is [{q8.B},{q8.H_kv},{q8.capacity},{q8.d}], not of [{B},{H_kv},.,{d}]")
+    _here(q8.k, q8.v, q8.k_scale, q8.v_scale)
+
+
+def _kv_planes(k, v):
+    stride = _plane_stride(k, "k")
+    if v.shape != k.shape or v.dtype != k.dtype or _plane_stride(v, "v") != stride:
+        raise SparvarError(ERR_INVALID, "k and v must share their shape, dtype and plane stride")
+    _here(k, v)
+    return stride
+
+
+def sparvar_kv_quantize(k_src, v_src, t0, q8, stream=None):
+    """Write rows of k_src, v_src [B,H_kv,n,d] to tokens [t0, t0 + n) of an 8-bit cache; see sparvar.h."""
+    lib = load_library()
+    B, H_kv, n, d = k_src.shape
+    stride = _kv_planes(k_src, v_src)
+    _check_q8(q8, B, H_kv, d)
+    _check(lib.sparvar_kv_quantize(B, H_kv, d, _dtype_code(k_src), n, t0, _ptr(k_src), _ptr(v_src), stride, q8.ref,
+                                   _stream(stream)))
+    return q8
+
+
+def sparvar_kv_dequantize(q8, t0, k_dst, v_dst, stream=None):
+    """Read tokens [t0, t0 + n) of an 8-bit cache back to k_dst, v_dst [B,H_kv,n,d]; see sparvar.h."""
+    lib = load_library()
+    B, H_kv, n, d = k_dst.shape
+    stride = _kv_planes(k_dst, v_dst)
+    _check_q8(q8, B, H_kv, d)
+    _check(lib.sparvar_kv_dequantize(B, H_kv, d, _dtype_code(k_dst), n, t0, q8.ref, _ptr(k_dst), _ptr(v_dst), stride,
+                                     _stream(stream)))
+    return k_dst, v_dst
+
+
+def sparvar_dense_attn_q8_workspace(B, H, H_kv, n_q, n_kv, d):
+    """Bytes of workspace with which a dense call of these sizes cuts its keys into parts (0: it does not)."""
+    n = load_library().sparvar_dense_attn_q8_workspace(B, H, H_kv, n_q, n_kv, d)
+    if n < 0:
+        _check(int(n))
+    return int(n)
+
+
+def _q8_attn(q, q8, o, lse):
+    """The checks that both attention calls over an 8-bit cache share."""
+    B, H, n_q, d = q.shape
+    dt = _dtype_code(q)
+    _same("o", o, q.shape, q.dtype)
+    if lse is not None:
+        _same("lse", lse, (B, H, n_q), _torch().float32)
+    _here(q, o, lse)
+    _check_q8(q8, B, q8.H_kv, d)
+    return dt
+
+
+def sparvar_dense_attn_q8_fwd(q, q8, n_kv, o, lse=None, kv_len=None, softmax_scale=None, workspace=None, stream=None):
+    """Dense attention over the first n_kv tokens (kv_len[b] of them, int32, for entry b) of an 8-bit cache; workspace: a
+    contiguous tensor of at least sparvar_dense_attn_q8_workspace() bytes, or None; see sparvar.h."""
+    lib = load_library()
+    B, H, n_q, d = q.shape
+    dt = _q8_attn(q, q8, o, lse)
+    if kv_len is not None:
+        _same("kv_len", kv_len, (B,), _torch().int32)
+    size = 0
+    if workspace is not None:
+        if not workspace.is_contiguous():
+            raise SparvarError(ERR_INVALID, "workspace must be contiguous")
+        size = workspace.numel() * workspace.element_size()
+    _here(kv_len, workspace)
+    _check(lib.sparvar_dense_attn_q8_fwd(B, H, q8.H_kv, n_q, n_kv, d, dt, _ptr(q), _plane_stride(q, "q"), q8.ref,
+                                         _ptr(kv_len), _ptr(o), _ptr(lse), _scale(softmax_scale, d), _ptr(workspace), size,
+                                         _stream(stream)))
+    return o, lse
+
+
+def sparvar_block_sparse_attn_q8_fwd(geom, k, q_k, q8, o, row_ptr, col_idx, lse=None, schedule=None, softmax_scale=None,
+                                     stream=None):
+    """Block-sparse attention of scale-k queries over the kept blocks of an 8-bit cache; see sparvar.h."""
+    lib = load_library()
+    B, H, n, d = q_k.shape
+    if 1 <= k <= len(geom.h) and n != geom.h[k - 1] * geom.w[k - 1]:
+        raise SparvarError(ERR_INVALID, f"q_k has {n} rows, scale {k} has {geom.h[k - 1] * geom.w[k - 1]} tokens")
+    dt = _q8_attn(q_k, q8, o, lse)
+    i32 = _torch().int32
+    if row_ptr.dtype != i32 or col_idx.dtype != i32 or (schedule is not None and schedule.dtype != i32):
+        raise SparvarError(ERR_INVALID, "row_ptr, col_idx and schedule must be int32")
+    _here(row_ptr, col_idx, schedule)
+    _check(lib.sparvar_block_sparse_attn_q8_fwd(geom.ref, k, B, H, q8.H_kv, d, dt, _ptr(q_k), _plane_stride(q_k, "q_k"),
+                                                q8.ref, _ptr(o), _ptr(lse), _scale(softmax_scale, d), _ptr(row_ptr),
+                                                _ptr(col_idx), _ptr(schedule), _stream(stream)))
     return o, lse

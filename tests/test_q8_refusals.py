@@ -1,0 +1,178 @@
+"""Refusals of the 8-bit cache calls and of the append, before anything reaches a GPU (host only)."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_2602_04361_amd import sparvar as sv
+
+FAKE = 1 << 20  # never dereferenced: validation fails first
+SIDES = [1, 2, 4, 8]
+
+
+def cache(**kw):
+    a = dict(block=64, capacity=1000, k=FAKE, v=FAKE, bh_stride=1000 * 64, k_scale=FAKE, v_scale=FAKE, scale_bh_stride=16)
+    a.update(kw)
+    return sv._CQ8Cache(*[a[n] for n, _ in sv._CQ8Cache._fields_])
+
+
+def heads(**kw):
+    a = dict(norm=1, layout=0, eps=1e-6, table_rows=1000, q_weight=FAKE, k_weight=FAKE, cos_sin=FAKE)
+    a.update(kw)
+    return sv._CNormRope(*[a[n] for n, _ in sv._CNormRope._fields_])
+
+
+def append(c=None, h=None, **kw):
+    a = dict(B=2, H=4, Hkv=2, d=64, dt=sv.BF16, n=10, t0=5, q=FAKE, qb=10 * 512, qt=512, k=FAKE, v=FAKE, kb=10 * 512, kt=512,
+             out=FAKE, kc=None, vc=None, cs=0, q8=True)
+    a.update(kw)
+    return sv.load_library().sparvar_qkv_append(
+        a["B"], a["H"], a["Hkv"], a["d"], a["dt"], a["n"], a["t0"], a["q"], a["qb"], a["qt"], a["k"], a["v"], a["kb"], a["kt"],
+        ctypes.byref(h or heads()), a["out"], a["kc"], a["vc"], a["cs"], ctypes.byref(c or cache()) if a["q8"] else None, None)
+
+
+BAD_CACHES = [dict(block=8), dict(block=48), dict(block=256), dict(capacity=0), dict(capacity=1 << 26, bh_stride=1 << 40),
+              dict(k=None), dict(v=None), dict(k_scale=None), dict(v_scale=None), dict(k=FAKE + 8), dict(v=FAKE + 4),
+              dict(bh_stride=999 * 64), dict(bh_stride=1000 * 64 + 8), dict(scale_bh_stride=15)]
+
+
+@pytest.mark.parametrize("bad", BAD_CACHES)
+def test_cache_struct(bad):
+    lib, c = sv.load_library(), cache(**bad)
+    assert append(c=c) == sv.ERR_INVALID
+    assert lib.sparvar_kv_quantize(2, 2, 64, sv.BF16, 10, 5, FAKE, FAKE, 640, ctypes.byref(c), None) == sv.ERR_INVALID
+    assert lib.sparvar_kv_dequantize(2, 2, 64, sv.F32, 10, 5, ctypes.byref(c), FAKE, FAKE, 640, None) == sv.ERR_INVALID
+    assert lib.sparvar_dense_attn_q8_fwd(2, 4, 2, 10, 100, 64, sv.BF16, FAKE, 640, ctypes.byref(c), None, FAKE, None, 0.1,
+                                         None, 0, None) == sv.ERR_INVALID
+    g = sv.Geometry(SIDES, SIDES, 4, 1)
+    assert lib.sparvar_block_sparse_attn_q8_fwd(g.ref, 4, 2, 4, 2, 64, sv.BF16, FAKE, 64 * 64, ctypes.byref(c), FAKE, None, 0.1,
+                                                FAKE, FAKE, None, None) == sv.ERR_INVALID
+    assert lib.sparvar_last_error()
+
+
+@pytest.mark.parametrize("bad,status", [
+    (dict(d=96), sv.ERR_UNSUPPORTED), (dict(dt=7), sv.ERR_UNSUPPORTED), (dict(B=0), sv.ERR_INVALID), (dict(H=3), sv.ERR_INVALID),
+    (dict(Hkv=0), sv.ERR_INVALID), (dict(n=0), sv.ERR_INVALID), (dict(t0=-1), sv.ERR_INVALID), (dict(t0=991), sv.ERR_CAPACITY),
+    (dict(t0=(1 << 31) - 5), sv.ERR_INVALID), (dict(q=None), sv.ERR_INVALID), (dict(k=None), sv.ERR_INVALID),
+    (dict(v=None), sv.ERR_INVALID), (dict(out=None), sv.ERR_INVALID), (dict(q=FAKE + 2), sv.ERR_INVALID),
+    (dict(qt=128), sv.ERR_INVALID), (dict(kt=64), sv.ERR_INVALID), (dict(qt=513), sv.ERR_INVALID), (dict(qb=8), sv.ERR_INVALID),
+    (dict(kb=-512), sv.ERR_INVALID), (dict(q8=False), sv.ERR_INVALID), (dict(kc=FAKE, vc=FAKE, cs=960), sv.ERR_INVALID),
+    (dict(q8=False, kc=FAKE), sv.ERR_INVALID), (dict(q8=False, kc=FAKE, vc=FAKE, cs=14 * 64), sv.ERR_INVALID),
+    (dict(q8=False, kc=FAKE, vc=FAKE + 2, cs=960), sv.ERR_INVALID), (dict(n=1 << 25, d=128), sv.ERR_INVALID)])
+def test_append_arguments(bad, status):
+    assert append(**bad) == status
+    assert sv.load_library().sparvar_last_error()
+
+
+@pytest.mark.parametrize("bad,status", [
+    (dict(norm=3), sv.ERR_INVALID), (dict(norm=-1), sv.ERR_INVALID), (dict(layout=2), sv.ERR_INVALID),
+    (dict(eps=-1.0), sv.ERR_INVALID), (dict(eps=float("nan")), sv.ERR_INVALID), (dict(table_rows=14), sv.ERR_CAPACITY),
+    (dict(q_weight=FAKE + 4), sv.ERR_INVALID), (dict(cos_sin=FAKE + 8), sv.ERR_INVALID)])
+def test_norm_rope_struct(bad, status):
+    assert append(h=heads(**bad)) == status
+
+
+def dense(**kw):
+    a = dict(B=2, H=4, Hkv=2, nq=10, nkv=100, d=64, dt=sv.BF16, q=FAKE, qs=640, o=FAKE, sc=0.1, ws=None, size=0)
+    a.update(kw)
+    return sv.load_library().sparvar_dense_attn_q8_fwd(a["B"], a["H"], a["Hkv"], a["nq"], a["nkv"], a["d"], a["dt"], a["q"],
+                                                       a["qs"], ctypes.byref(cache()), None, a["o"], None, a["sc"], a["ws"],
+                                                       a["size"], None)
+
+
+@pytest.mark.parametrize("bad,status", [
+    (dict(dt=sv.F32), sv.ERR_UNSUPPORTED), (dict(d=80), sv.ERR_UNSUPPORTED), (dict(H=5), sv.ERR_INVALID),
+    (dict(nq=0), sv.ERR_INVALID), (dict(nkv=0), sv.ERR_INVALID), (dict(nkv=1001), sv.ERR_CAPACITY), (dict(q=None), sv.ERR_INVALID),
+    (dict(qs=639), sv.ERR_INVALID), (dict(o=FAKE + 2), sv.ERR_INVALID), (dict(sc=0.0), sv.ERR_INVALID),
+    (dict(sc=float("inf")), sv.ERR_INVALID), (dict(ws=FAKE, size=16, nkv=1000), sv.ERR_CAPACITY),
+    (dict(ws=FAKE + 4, size=1 << 30, nkv=1000), sv.ERR_INVALID)])
+def test_dense_arguments(bad, status):
+    assert dense(**bad) == status
+
+
+def test_dense_workspace():
+    lib = sv.load_library()
+    assert sv.sparvar_dense_attn_q8_workspace(1, 4, 2, 1, 1000, 64) > 0
+    assert sv.sparvar_dense_attn_q8_workspace(2, 16, 16, 4096, 10521, 128) == 0
+    assert sv.sparvar_dense_attn_q8_workspace(2, 16, 16, 1, 40, 128) == 0
+    assert lib.sparvar_dense_attn_q8_workspace(1, 3, 2, 1, 1000, 64) == sv.ERR_INVALID
+    assert lib.sparvar_dense_attn_q8_workspace(1, 4, 2, 1, 1000, 65) == sv.ERR_UNSUPPORTED
+    with pytest.raises(sv.SparvarError):
+        sv.sparvar_dense_attn_q8_workspace(1, 3, 2, 1, 1000, 64)
+
+
+@pytest.mark.parametrize("bad,status", [
+    (dict(k=5), sv.ERR_INVALID), (dict(dt=sv.F32), sv.ERR_UNSUPPORTED), (dict(H=3), sv.ERR_INVALID), (dict(rp=None), sv.ERR_INVALID),
+    (dict(ci=None), sv.ERR_INVALID), (dict(cap=84), sv.ERR_CAPACITY), (dict(sc=-1.0), sv.ERR_INVALID)])
+def test_sparse_arguments(bad, status):
+    a = dict(k=4, H=4, dt=sv.BF16, rp=FAKE, ci=FAKE, cap=85, sc=0.1)
+    a.update(bad)
+    g = sv.Geometry(SIDES, SIDES, 4, 1)
+    c = cache(capacity=a["cap"])
+    assert sv.load_library().sparvar_block_sparse_attn_q8_fwd(
+        g.ref, a["k"], 2, a["H"], 2, 64, a["dt"], FAKE, 64 * 64, ctypes.byref(c), FAKE, None, a["sc"], a["rp"], a["ci"], None,
+        None) == status
+
+
+# ---- the binding's own checks (tensors on the CPU: each fails before the library is called)
+def planes(B=1, H=2, n=64, d=64, dtype=torch.bfloat16):
+    return torch.zeros(B, H, n, d, dtype=dtype)
+
+
+def q8(B=1, H=2, n=64, d=64, block=32):
+    return sv.Q8Cache.empty(B, H, n, d, block, device="cpu")
+
+
+def refused(fn, *args, **kw):
+    with pytest.raises(sv.SparvarError):
+        fn(*args, **kw)
+
+
+def test_q8_cache_class():
+    code, scale = torch.zeros(1, 2, 64, 64, dtype=torch.float8_e4m3fn), torch.zeros(1, 2, 2, dtype=torch.uint8)
+    sv.Q8Cache(code, code.clone(), scale, scale.clone(), 32)
+    sv.Q8Cache(code.view(torch.uint8), code, scale.view(torch.float8_e8m0fnu), scale, 32)
+    refused(sv.Q8Cache, code.bfloat16(), code, scale, scale, 32)
+    refused(sv.Q8Cache, code, code, scale.int(), scale, 32)
+    refused(sv.Q8Cache, code, code[:, :, :32], scale, scale, 32)
+    refused(sv.Q8Cache, code, code, scale, scale, 16)  # four blocks of 16 tokens
+    refused(sv.Q8Cache, code, code, scale, scale, 40)
+    refused(sv.Q8Cache, code.transpose(2, 3), code, scale, scale, 32)
+    refused(sv.Q8Cache, code, code, scale, scale[:, :1], 32)
+
+
+def test_norm_rope_class():
+    w, t = torch.ones(2, 64), torch.zeros(10, 32, 2)
+    sv.NormRope("rms", 1e-6, w, w, t, "halves")
+    refused(sv.NormRope, "layer")
+    refused(sv.NormRope, "rms", layout="thirds")
+    refused(sv.NormRope, "rms", q_weight=w.double())
+    refused(sv.NormRope, "rms", q_weight=w[0])
+    refused(sv.NormRope, cos_sin=torch.zeros(10, 32, 3))
+    refused(sv.NormRope, cos_sin=torch.zeros(10, 2, 32).transpose(1, 2))
+
+
+def test_tensors_off_the_gpu():
+    k, c = planes(), q8()
+    refused(sv.sparvar_kv_quantize, k, k, 0, c)
+    refused(sv.sparvar_kv_dequantize, c, 0, k, k)
+    refused(sv.sparvar_dense_attn_q8_fwd, k, c, 64, torch.empty_like(k))
+    x = torch.zeros(1, 64, 2, 64, dtype=torch.bfloat16)
+    refused(sv.sparvar_qkv_append, x, x, x, 0, None, torch.empty_like(k), q8=c)
+    g = sv.Geometry([8], [8], 4, 0)
+    i = torch.zeros(9, dtype=torch.int32)
+    refused(sv.sparvar_block_sparse_attn_q8_fwd, g, 1, k, c, torch.empty_like(k), i, i)
+
+
+def test_mismatched_tensors():
+    x, k = torch.zeros(1, 64, 2, 64, dtype=torch.bfloat16), planes()
+    refused(sv.sparvar_qkv_append, x, x, x[:, :, :1], 0, None, k)
+    refused(sv.sparvar_qkv_append, x, x.float(), x.float(), 0, None, k)
+    refused(sv.sparvar_qkv_append, x, x, x, 0, None, k.float())
+    refused(sv.sparvar_qkv_append, x, x, x, 0, None, planes(n=63))
+    refused(sv.sparvar_qkv_append, x, x[:, :32], x[:, :32], 0, None, k)
+    refused(sv.sparvar_kv_quantize, k, planes(n=32), 0, q8())
+    refused(sv.sparvar_kv_quantize, k, k.float(), 0, q8())
+    refused(sv.sparvar_dense_attn_q8_fwd, k, q8(), 64, planes(n=32))
+    refused(sv.sparvar_dense_attn_q8_fwd, k, q8(), 64, k, lse=torch.zeros(1, 2, 64, dtype=torch.float64))
+    refused(sv.sparvar_block_sparse_attn_q8_fwd, sv.Geometry([9], [8], 4, 0), 1, k, q8(), k, k, k)
