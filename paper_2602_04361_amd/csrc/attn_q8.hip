@@ -83,138 +83,348 @@ struct SparseQ8Src : SparseSrc<KC> {
   }
 };
 
-template <int D, int NW, int KC, class Src>
-__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) void attn_q8_kernel(Q8IO io, Src src) {
-  constexpr int NT = NW * 64;
-  constexpr int U = D / 8;                    // 16-byte units of a bf16 row in LDS
-  constexpr int kRow = D * 2;
-  constexpr int kTile = KC * kRow;            // K (or V) of a chunk in LDS
-  constexpr int kPieces = KC * D / 16;        // 16-code pieces of K (or V) of a chunk
-  constexpr int kLoads = 2 * kPieces / NT;    // pieces a lane converts
-  static_assert(2 * kPieces % NT == 0 && kPieces % 64 == 0, "pieces must split evenly, K and V by whole waves");
-  __shared__ __attribute__((aligned(16))) char stage0[2 * kTile];
-  __shared__ __attribute__((aligned(16))) char stage1[2 * kTile];
+// Which codes of a wave's 16 rows a lane loads and converts: four lanes take a row, 16 codes
+// each (col) and at D = 128 the 16 that lie 64 channels further, so that a token's address and
+// scale are found once for both. Eight neighbouring lanes take a row and the one four further,
+// whose units lie an odd number of units apart (unit_swizzle): every 16-byte write of theirs
+// meets eight different groups of banks.
+__device__ __forceinline__ void lane_piece(int lane, int& row, int& col) {
+  row = ((lane >> 3) & 3) + ((lane >> 2) & 1) * 4 + (lane >> 5) * 8;
+  col = lane & 3;
+}
+
+// The two bf16 units of 16 codes times f.
+__device__ __forceinline__ void put_piece(char* at0, char* at1, const u32x4& raw, float f) {
+  uint32_t w[8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) decode4_bf16(raw[i], f, w[2 * i], w[2 * i + 1]);
+  *reinterpret_cast<u32x4*>(at0) = u32x4{w[0], w[1], w[2], w[3]};
+  *reinterpret_cast<u32x4*>(at1) = u32x4{w[4], w[5], w[6], w[7]};
+}
+
+// What a wave found for its rows: the part's unnormalised sums, maximum and sum, or the output.
+template <int D>
+__device__ __forceinline__ void store_rows(const Q8IO& io, const f32x16 (&acc)[D / 32], float m, float l, bool qvalid, int half,
+                                           int32_t plane, int32_t qrow, int32_t part) {
+  if (!qvalid) return;
+  const int64_t orow = (int64_t)plane * io.o_rows + qrow;
+  if (io.part_o) {
+    const int64_t prow = (int64_t)part * io.rows + orow;
+    float* op = io.part_o + prow * D;
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        *reinterpret_cast<float4*>(op + 32 * dt + 8 * j + 4 * half) =
+            make_float4(acc[dt][4 * j], acc[dt][4 * j + 1], acc[dt][4 * j + 2], acc[dt][4 * j + 3]);
+    if (half == 0) io.part_ml[prow] = make_float2(m, l);
+    return;
+  }
+  const float inv = l > 0.f ? 1.f / l : 0.f;
+  bf16_bits* op = io.o + orow * D;
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      uint2 w;
+      w.x = pack_bf16x2(acc[dt][4 * j] * inv, acc[dt][4 * j + 1] * inv);
+      w.y = pack_bf16x2(acc[dt][4 * j + 2] * inv, acc[dt][4 * j + 3] * inv);
+      *reinterpret_cast<uint2*>(op + 32 * dt + 8 * j + 4 * half) = w;
+    }
+  if (io.lse && half == 0) io.lse[orow] = l > 0.f ? (m + __builtin_log2f(l)) * kLn2 : -INFINITY;
+}
+
+// Query fragments for the products with K's codes: the row divided by a power of two (its
+// largest magnitude at most 448) as the sum of two e4m3 values. bf16 has 8 significant bits and
+// e4m3 4, so the sum is the query itself for every element down to 2^-10 of the row's largest,
+// and within 2^-18 of the largest below: the scores are those of exact products, at the matrix
+// rate of bf16 (two e4m3 products at twice its rate), and K needs no conversion. Step t of a
+// half covers channels 64 t + 32 half .. + 32, as the K fragments do.
+typedef __attribute__((ext_vector_type(8))) int i32x8;
+
+template <int D>
+struct QFragF8 {
+  i32x8 hi[D / 64], lo[D / 64];
+  int32_t scale;  // E8M0 byte
+  __device__ __forceinline__ void load(const bf16_bits* row, int half) {
+    u32x4 raw[D / 16];
+    float top = 0.f;
+#pragma unroll
+    for (int t = 0; t < D / 64; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        raw[4 * t + i] = ldg16(row + 64 * t + 32 * half + 8 * i);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          top = fmaxf(top, fabsf(__uint_as_float(raw[4 * t + i][e] << 16)));
+          top = fmaxf(top, fabsf(__uint_as_float(raw[4 * t + i][e] & 0xffff0000u)));
+        }
+      }
+    const int32_t e2 = block_exponent(max_halves(top));
+    const float inv = pow2f(-e2);
+    scale = e2 + 127;
+#pragma unroll
+    for (int t = 0; t < D / 64; ++t)
+#pragma unroll
+      for (int w = 0; w < 8; ++w) {
+        const uint32_t a = raw[4 * t + w / 2][2 * (w & 1)], b = raw[4 * t + w / 2][2 * (w & 1) + 1];
+        const float x[4] = {__uint_as_float(a << 16) * inv, __uint_as_float(a & 0xffff0000u) * inv, __uint_as_float(b << 16) * inv,
+                            __uint_as_float(b & 0xffff0000u) * inv};
+        const uint32_t h = codes4(x[0], x[1], x[2], x[3]);
+        float y[4];
+        decode4(h, 1.f, y);
+        hi[t][w] = (int)h;
+        lo[t][w] = (int)codes4(x[0] - y[0], x[1] - y[1], x[2] - y[2], x[3] - y[3]);
+      }
+  }
+};
+
+// c += K Q^T over 64 channels: a the codes of 32 keys (scale byte ks of the lane's key).
+template <int D>
+__device__ __forceinline__ f32x16 mfma_k(i32x8 a, int32_t ks, const QFragF8<D>& q, int t, f32x16 c) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  c = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, q.hi[t], c, 0, 0, 0, ks, 0, q.scale);
+  c = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, q.lo[t], c, 0, 0, 0, ks, 0, q.scale);
+#endif
+  return c;
+}
+
+__device__ __forceinline__ i32x8 two_units(u32x4 a, u32x4 b) {
+  return i32x8{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b[0], (int)b[1], (int)b[2], (int)b[3]};
+}
+
+// K codes in LDS: rows of D bytes, 16-byte unit u of row r at u ^ code_swizzle(r): the same unit
+// of eight neighbouring rows lies in eight different groups of banks.
+template <int D>
+__device__ __forceinline__ int code_swizzle(int r) {
+  return D == 128 ? r & 7 : (r >> 1) & 3;
+}
+
+// V^T fragment of step ks2, channels 32 dt .. of a V tile (rows of D bf16 values).
+template <int D, int KC>
+struct VOffsets {
+  int off[2][D / 32];
+  __device__ __forceinline__ void init(int l32, int half, int lane) {
+    FragOffsets<D, KC> fo;
+    fo.init(l32, half, lane);
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) {  // (V alone, no K tile before it)
+      off[0][i] = fo.v_off[0][i] - KC * D * 2;
+      off[1][i] = fo.v_off[1][i] - KC * D * 2;
+    }
+  }
+  __device__ __forceinline__ bf16x8 read(const char* tile, int ks2, int dt) const {
+    const i16x4 lo = lds_read_tr(tile + off[0][dt] + ks2 * 16 * D * 2);
+    const i16x4 hi = lds_read_tr(tile + off[1][dt] + ks2 * 16 * D * 2);
+    u32x4 av;
+    av[0] = __builtin_bit_cast(uint32_t, __builtin_shufflevector(lo, lo, 0, 1));
+    av[1] = __builtin_bit_cast(uint32_t, __builtin_shufflevector(lo, lo, 2, 3));
+    av[2] = __builtin_bit_cast(uint32_t, __builtin_shufflevector(hi, hi, 0, 1));
+    av[3] = __builtin_bit_cast(uint32_t, __builtin_shufflevector(hi, hi, 2, 3));
+    return as_bf16x8(av);
+  }
+};
+
+// Softmax of a chunk of scores: masks past count, moves the running maximum when a row's grew
+// by more than 2^8 (the sums are rescaled then), and packs the probabilities.
+template <int D, int KC>
+__device__ __forceinline__ void softmax_chunk(f32x16 (&st)[KC / 32], int32_t count, int half, float scale_log2, float& m_run,
+                                              float& l_run, f32x16 (&acc)[D / 32], bf16x8 (&pf)[KC / 16]) {
+  if (count < KC) mask_tail<KC>(st, count, half);
+  const float mx = row_max<KC>(st, scale_log2);
+  if (__builtin_amdgcn_ballot_w64(mx > m_run + 8.f)) {
+    const float m_new = fmaxf(m_run, mx);
+    const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+    l_run *= alpha;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) acc[i] *= alpha;
+    m_run = m_new;
+  }
+  l_run += exp_pack<KC>(st, scale_log2, m_run, pf);
+}
+
+// QW waves of 32 queries walk the keys, or (KS > 1) KS such sets, each a part of them with LDS
+// of its own, joined at the end.
+template <int D, int QW, int KS, class Src>
+__global__ __launch_bounds__(QW * KS * 64) __attribute__((amdgpu_waves_per_eu(2))) void attn_q8_kernel(Q8IO io, Src src) {
+  constexpr int KC = 64, NT = QW * KS * 64;
+  constexpr int kRow = D * 2;                 // bytes of a V row in LDS
+  constexpr int kKTile = KC * D, kVTile = KC * kRow;
+  constexpr int U8 = D / 16;                  // 16-byte units of a row of codes
+  constexpr int kPieces = D / 64;             // 16-code pieces of V a lane takes of a row
+  // V rows go to waves 16 at a time, K units 64 at a time; where there are more waves than V
+  // rows, the second half of them copies K.
+  constexpr bool kHalf = QW * 16 > KC;
+  constexpr int kVSteps = kHalf ? 1 : KC / (QW * 16);
+  constexpr int kKSteps = KC * U8 / ((kHalf ? QW / 2 : QW) * 64);
+  static_assert(kHalf ? QW * 16 == 2 * KC : KC % (QW * 16) == 0, "V rows must split evenly");
+  static_assert(KC * U8 % ((kHalf ? QW / 2 : QW) * 64) == 0, "K units must split evenly");
+  static_assert(KS == 1 || Src::kSparse, "parts of a table's walk");
+  // (the parts' outputs go through the V tiles when they join: KS (KS - 1) QW pieces of D / 2 / KS x 64 floats)
+  constexpr int kJoin = KS > 1 ? (KS - 1) * QW * D * 128 / KS : 0;
+  constexpr int kStage = kVTile > kJoin ? kVTile : kJoin;
+  __shared__ __attribute__((aligned(16))) char ktile0[KS][kKTile];
+  __shared__ __attribute__((aligned(16))) char ktile1[KS][kKTile];
+  __shared__ __attribute__((aligned(16))) char vtiles[KS][kStage];
   __shared__ __attribute__((aligned(16))) char tsmem[Src::template table_bytes<NT>()];
 
   const int32_t item = swizzled_item(blockIdx.x, gridDim.x, io.swizzle);
   if (item >= io.n_items) return;
   const int tid = threadIdx.x;
-  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lane = tid & 63, wave_all = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, half = lane >> 5;
+  const int split = wave_all / QW, wave = wave_all % QW;
 
   const QuerySet qs = src.queries(item, wave);
-  const int32_t qslot = qs.q0 + l32;
-  const bool qvalid = qslot < qs.q1;
-  int32_t plane, qrow;
-  src.place(qs, qvalid ? qslot : 0, plane, qrow);
-  QFragBF16<D> qf;
-  qf.load(io.q + (int64_t)plane * io.q_bh_stride + (int64_t)qrow * D, half);
-
+  QFragF8<D> qf;
+  {
+    int32_t plane, qrow;
+    src.place(qs, qs.q0 + l32 < qs.q1 ? qs.q0 + l32 : 0, plane, qrow);
+    qf.load(io.q + (int64_t)plane * io.q_bh_stride + (int64_t)qrow * D, half);
+  }
   const int32_t kvp = src.kv_plane(qs);
-  const uint8_t* planes[2] = {io.c.k + (int64_t)kvp * io.c.bh_stride, io.c.v + (int64_t)kvp * io.c.bh_stride};
-  const uint8_t* scales[2] = {io.c.ks + (int64_t)kvp * io.c.sc_stride, io.c.vs + (int64_t)kvp * io.c.sc_stride};
+  const uint8_t* kp = io.c.k + (int64_t)kvp * io.c.bh_stride;
+  const uint8_t* vp = io.c.v + (int64_t)kvp * io.c.bh_stride;
+  const uint8_t* ksp = io.c.ks + (int64_t)kvp * io.c.sc_stride;
+  const uint8_t* vsp = io.c.vs + (int64_t)kvp * io.c.sc_stride;
 
   f32x16 acc[D / 32];
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) acc[i] = zero16();
   float m_run = kNoMax, l_run = 0.f;
 
-  FragOffsets<D, KC> fo;
-  fo.init(l32, half, lane);
+  // K fragments: unit 4 t + 2 half + x of row l32 (rows 32 apart share their swizzle)
+  int k_off[D / 64][2];
+#pragma unroll
+  for (int t = 0; t < D / 64; ++t)
+#pragma unroll
+    for (int x = 0; x < 2; ++x) k_off[t][x] = l32 * D + 16 * ((4 * t + 2 * half + x) ^ code_swizzle<D>(l32));
+  VOffsets<D, KC> vo;
+  vo.init(l32, half, lane);
 
-  // Piece j of a lane: 16 codes of one key of K (piece below kPieces) or V. Its two units
-  // of bf16 go to LDS in an order that differs between the halves of eight lanes, so that
-  // eight lanes of a write meet eight different groups of banks.
-  int key_of_piece[kLoads], lds_of_piece[kLoads][2];
-  uint32_t off_of_piece[kLoads];
+  // V: a lane's pieces of row vrow, and of rows QW * 16 further (a multiple of 16, so LDS
+  // offsets differ by a constant)
+  char* const vtile = vtiles[split];
+  int vrow, vcol;
+  lane_piece(lane, vrow, vcol);
+  vrow += wave * 16;
+  const bool does_v = !kHalf || wave < QW / 2, does_k = !kHalf || wave >= QW / 2;  // wave-uniform
+  int v_lds[kPieces][2];
 #pragma unroll
-  for (int j = 0; j < kLoads; ++j) {
-    const int x = (j * NT + tid) % kPieces;
-    const int r = x / (D / 16), c = x % (D / 16), swap = (lane >> 2) & 1;
-    key_of_piece[j] = r;
-    off_of_piece[j] = 16 * c;
-    const int base = ((j * NT + wave * 64) >= kPieces ? kTile : 0) + r * kRow, sw = unit_swizzle(r) & (U - 1);
-    lds_of_piece[j][0] = base + 16 * ((2 * c + swap) ^ sw);
-    lds_of_piece[j][1] = base + 16 * ((2 * c + 1 - swap) ^ sw);
-  }
-  const bool swapped = (lane >> 2) & 1;
+  for (int p = 0; p < kPieces; ++p)
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+      v_lds[p][x] = vrow * kRow + 16 * ((2 * (vcol + 4 * p) + x) ^ (unit_swizzle(vrow) & (D / 8 - 1)));
+  // K: a direct copy of the wave covers 64 units in a row; a lane fetches the unit that the
+  // swizzle puts at its place
+  const int k_first = (kHalf ? wave - QW / 2 : wave) * kKSteps * 64;
+  const int k_row = (k_first + lane) / U8, k_unit = (k_first + lane) % U8;
 
-  u32x4 raw[kLoads];
-  uint32_t raw_s[kLoads];
-  auto load = [&](const Chunk& c) {
+  u32x4 raw[kVSteps][kPieces];
+  uint32_t raw_s[kVSteps], k_scale[KC / 32], k_scale_next[KC / 32];
+  auto load = [&](const Chunk& c, char* kdst) {
+    if (does_k) {
 #pragma unroll
-    for (int j = 0; j < kLoads; ++j) {
-      const int is_v = (j * NT + wave * 64) >= kPieces;
-      const uint32_t tok = (uint32_t)chunk_token(c, chunk_slot(key_of_piece[j], c.count));
-      raw[j] = *reinterpret_cast<const u32x4*>(planes[is_v] + (tok * D + off_of_piece[j]));
-      raw_s[j] = scales[is_v][tok >> io.c.lg];
-    }
-  };
-  auto convert = [&](char* st) {
-#pragma unroll
-    for (int j = 0; j < kLoads; ++j) {
-      const float f = scale_of_byte(raw_s[j]);
-      u32x4 a, b;
-      uint32_t w[8];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) decode4_bf16(raw[j][i], f, w[2 * i], w[2 * i + 1]);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        a[i] = swapped ? w[4 + i] : w[i];
-        b[i] = swapped ? w[i] : w[4 + i];
+      for (int j = 0; j < kKSteps; ++j) {
+        const int r = k_row + j * (64 / U8);
+        const uint32_t tok = (uint32_t)chunk_token(c, chunk_slot(r, c.count));
+        dma16(kp + (tok * D + 16 * (k_unit ^ code_swizzle<D>(r))), kdst + (k_first + j * 64) * 16);
       }
-      *reinterpret_cast<u32x4*>(st + lds_of_piece[j][0]) = a;
-      *reinterpret_cast<u32x4*>(st + lds_of_piece[j][1]) = b;
     }
+    if (does_v) {
+#pragma unroll
+      for (int j = 0; j < kVSteps; ++j) {
+        const uint32_t tok = (uint32_t)chunk_token(c, chunk_slot(vrow + j * QW * 16, c.count));
+#pragma unroll
+        for (int p = 0; p < kPieces; ++p)
+          raw[j][p] = *reinterpret_cast<const u32x4*>(vp + (tok * D + 16 * vcol + 64 * p));
+        raw_s[j] = vsp[tok >> io.c.lg];
+      }
+    }
+#pragma unroll
+    for (int kt = 0; kt < KC / 32; ++kt)
+      k_scale_next[kt] = ksp[(uint32_t)chunk_token(c, chunk_slot(32 * kt + l32, c.count)) >> io.c.lg];
+  };
+  // The chunk loaded last becomes the one to be computed: V to LDS, K's copies arrived.
+  auto take = [&]() {
+    if (does_v) {
+#pragma unroll
+      for (int j = 0; j < kVSteps; ++j)
+#pragma unroll
+        for (int p = 0; p < kPieces; ++p)
+          put_piece(vtile + v_lds[p][0] + j * (QW * 16 * kRow), vtile + v_lds[p][1] + j * (QW * 16 * kRow), raw[j][p],
+                    scale_of_byte(raw_s[j]));
+    }
+#pragma unroll
+    for (int kt = 0; kt < KC / 32; ++kt) k_scale[kt] = k_scale_next[kt];
+    __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
   };
 
-  auto compute = [&](const char* kst, int32_t count) {
+  // One chunk, K in kt_, V in vtile; `next` issues the loads of the next one. The order of the
+  // LDS reads is pinned: K first, V under the products of S.
+  auto compute = [&](const char* kt_, int32_t count, auto next) {
     f32x16 st[KC / 32];
-    qk_chunk<D, KC>(kst, fo, qf, st);
-    if (count < KC) mask_tail<KC>(st, count, half);
-    const float mx = row_max<KC>(st, io.scale_log2);
-    if (__builtin_amdgcn_ballot_w64(mx > m_run + 8.f)) {
-      const float m_new = fmaxf(m_run, mx);
-      const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
-      l_run *= alpha;
+    i32x8 kf[KC / 32][D / 64];
+    bf16x8 vf[KC / 16][D / 32], pf[KC / 16];
 #pragma unroll
-      for (int i = 0; i < D / 32; ++i) acc[i] *= alpha;
-      m_run = m_new;
+    for (int kt = 0; kt < KC / 32; ++kt)
+#pragma unroll
+      for (int t = 0; t < D / 64; ++t)
+        kf[kt][t] = two_units(*reinterpret_cast<const u32x4*>(kt_ + k_off[t][0] + kt * 32 * D),
+                              *reinterpret_cast<const u32x4*>(kt_ + k_off[t][1] + kt * 32 * D));
+    __builtin_amdgcn_sched_barrier(0);
+    next();
+    __builtin_amdgcn_sched_barrier(0);
+    constexpr int kProducts = KC / 32 * (D / 64), kV = KC / 16 * (D / 32);  // V fragments to read under them
+#pragma unroll
+    for (int kt = 0; kt < KC / 32; ++kt) st[kt] = zero16();
+#pragma unroll
+    for (int i = 0; i < kProducts; ++i) {
+      const int kt = i / (D / 64), t = i % (D / 64);
+      st[kt] = mfma_k<D>(kf[kt][t], (int32_t)k_scale[kt], qf, t, st[kt]);
+#pragma unroll
+      for (int f = kV * i / kProducts; f < kV * (i + 1) / kProducts; ++f)
+        vf[f / (D / 32)][f % (D / 32)] = vo.read(vtile, f / (D / 32), f % (D / 32));
+      __builtin_amdgcn_sched_barrier(0);
     }
-    bf16x8 pf[KC / 16];
-    l_run += exp_pack<KC>(st, io.scale_log2, m_run, pf);
-    pv_chunk<D, KC>(kst, fo, pf, acc);
+    softmax_chunk<D, KC>(st, count, half, io.scale_log2, m_run, l_run, acc, pf);
+#pragma unroll
+    for (int ks = 0; ks < KC / 16; ++ks)
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt) acc[dt] = mfma_bf16(vf[ks][dt], pf[ks], acc[dt]);
   };
 
   auto cur = [&]() {
     if constexpr (Src::kSparse) return src.template table_cursor<NT>(item, tsmem);
     else return src.cursor(item, qs);
   }();
-  // One pass over what the cursor holds (a block table is filled again between passes,
-  // with a barrier, so both stages are free when a pass starts).
+  // One pass over what the cursor holds, or over the set's part of it (a block table is filled
+  // again between passes, with a barrier, so the tiles are free when a pass starts). Every
+  // wave takes the steps of the longest part, and the barriers in them.
   auto walk = [&]() {
-    Chunk c0, c1;
-    if (!cur.next(c0)) return;
-    load(c0);
-    convert(stage0);
-    bool more = cur.next(c1);
-    if (more) load(c1);
-    auto step = [&](char* now, char* then) -> bool {
+    int32_t steps = 0;
+    if constexpr (KS > 1) steps = cur.take_split(split, KS);
+    Chunk c0;
+    bool have = cur.next(c0);
+    if (KS == 1 && !have) return;
+    if (have) load(c0, ktile0[split]);
+    auto step = [&](const char* now, char* then, bool first) -> bool {
+      if (!first) __syncthreads();  // V and the other K tile have been read
+      if (have) take();
       __syncthreads();
-      const int32_t count = c0.count;
-      const bool go_on = more;
-      if (more) {
-        convert(then);
-        c0 = c1;
-        more = cur.next(c1);
-        if (more) load(c1);
+      if (have) {
+        const int32_t count = c0.count;
+        compute(now, count, [&]() {
+          have = cur.next(c0);
+          if (have) load(c0, then);
+        });
       }
-      compute(now, count);
-      return go_on;
+      return KS > 1 ? --steps > 0 : have;
     };
-    for (;;) {
-      if (!step(stage0, stage1)) break;
-      if (!step(stage1, stage0)) break;
+    if (KS > 1 && steps <= 0) return;
+    for (bool first = true;; first = false) {
+      if (!step(ktile0[split], ktile1[split], first)) break;
+      if (!step(ktile1[split], ktile0[split], false)) break;
     }
   };
   if constexpr (Src::kSparse) {
@@ -226,89 +436,301 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
     walk();
   }
 
-  const float l_tot = sum_halves(l_run);
-  if (!qvalid) return;
-  const int64_t orow = (int64_t)plane * io.o_rows + qrow;
-  if (io.part_o) {
-    const int64_t prow = (int64_t)src.part_of(item) * io.rows + orow;
-    float* op = io.part_o + prow * D;
+  // (the rows' places are found again, not held through the walk)
+  const int32_t qslot = qs.q0 + (fresh_tid() & 31);
+  const bool qvalid = qslot < qs.q1;
+  int32_t plane, qrow;
+  src.place(qs, qvalid ? qslot : 0, plane, qrow);
+  if constexpr (KS > 1) {
+    __shared__ float ml[KS][QW * kQPerWave][2];
+    float m_g, l_g, out[D / 2 / KS];
+    merge_key_splits<D, QW, KS, KS * kStage / 2>(acc, m_run, l_run, split, wave, lane, vtiles[0], vtiles[0] + KS * kStage / 2,
+                                                 ml, m_g, l_g, out);
+    if (!qvalid) return;
+    const float inv = l_g > 0.f ? 1.f / l_g : 0.f;
+    const int64_t orow = (int64_t)plane * io.o_rows + qrow;
 #pragma unroll
-    for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        *reinterpret_cast<float4*>(op + 32 * dt + 8 * j + 4 * half) =
-            make_float4(acc[dt][4 * j], acc[dt][4 * j + 1], acc[dt][4 * j + 2], acc[dt][4 * j + 3]);
-    if (half == 0) io.part_ml[prow] = make_float2(m_run, l_tot);
+    for (int i = 0; i < D / 8 / KS; ++i) {
+      uint2 w;
+      w.x = pack_bf16x2(out[4 * i] * inv, out[4 * i + 1] * inv);
+      w.y = pack_bf16x2(out[4 * i + 2] * inv, out[4 * i + 3] * inv);
+      *reinterpret_cast<uint2*>(io.o + orow * D + channel_of(split * (D / 8 / KS) + i, half)) = w;
+    }
+    if (io.lse && split == 0 && half == 0) io.lse[orow] = l_g > 0.f ? (m_g + __builtin_log2f(l_g)) * kLn2 : -INFINITY;
     return;
   }
-  const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
-  bf16_bits* op = io.o + orow * D;
-#pragma unroll
-  for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      uint2 w;
-      w.x = pack_bf16x2(acc[dt][4 * j] * inv, acc[dt][4 * j + 1] * inv);
-      w.y = pack_bf16x2(acc[dt][4 * j + 2] * inv, acc[dt][4 * j + 3] * inv);
-      *reinterpret_cast<uint2*>(op + 32 * dt + 8 * j + 4 * half) = w;
-    }
-  if (io.lse && half == 0) io.lse[orow] = l_tot > 0.f ? (m_run + __builtin_log2f(l_tot)) * kLn2 : -INFINITY;
+  const float l_tot = sum_halves(l_run);
+  store_rows<D>(io, acc, m_run, l_tot, qvalid, half, plane, qrow, src.part_of(item));
 }
 
-// Joins the parts of every row, in order: a thread takes four channels of a row. A part
-// without keys has no sum and its values are not read.
+// Few rows against a long cache (single tokens, a token a query head): memory bound, so
+// every wave walks chunks of 32 keys by itself, without barriers, its next chunk's codes in
+// flight. Its K codes go from registers to the products (a lane holds half of a key's
+// channels: the sum over channels may run in any order, so step s takes channels 8 s .. of
+// each half); V goes through a piece of LDS of the wave's own, for the transposing read.
+// The four waves of a workgroup take every fourth chunk of a part and join at the end.
+constexpr int kRowWaves = 4;
+
+// LDS of one wave, written by some lanes and read by others: its instructions run in
+// order, so only the compiler has to keep them so.
+__device__ __forceinline__ void wave_fence() {
+#if defined(__HIP_DEVICE_COMPILE__)
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#endif
+}
+
+template <int D>
+__global__ __launch_bounds__(kRowWaves * 64) __attribute__((amdgpu_waves_per_eu(2)))
+void attn_q8_rows_kernel(Q8IO io, DenseQ8Src<32> src) {
+  constexpr int KC = 32, kRow = D * 2;
+  constexpr int kK = D / 32;             // 16-byte pieces of a lane's half of a key
+  constexpr int kPieces = D / 64;        // 16-code pieces of V a lane takes of a row
+  constexpr int kTile = KC * kRow;
+  __shared__ __attribute__((aligned(16))) char tiles[kRowWaves][kTile];
+  __shared__ float2 ml[kRowWaves][32];
+
+  const int32_t item = swizzled_item(blockIdx.x, gridDim.x, io.swizzle);
+  if (item >= io.n_items) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int l32 = lane & 31, half = lane >> 5;
+
+  const QuerySet qs = src.queries(item, 0);
+  const bool qvalid = qs.q0 + l32 < qs.q1;
+  int32_t plane, qrow;
+  src.place(qs, qvalid ? qs.q0 + l32 : qs.q0, plane, qrow);
+  const bf16_bits* q = io.q + (int64_t)plane * io.q_bh_stride + (int64_t)qrow * D + half * (D / 2);
+  bf16x8 qf[D / 16];
+#pragma unroll
+  for (int s = 0; s < D / 16; ++s) qf[s] = as_bf16x8(ldg16(q + 8 * s));
+
+  const uint8_t* kp = io.c.k + (int64_t)qs.bh * io.c.bh_stride;
+  const uint8_t* vp = io.c.v + (int64_t)qs.bh * io.c.bh_stride;
+  const uint8_t* ks = io.c.ks + (int64_t)qs.bh * io.c.sc_stride;
+  const uint8_t* vs = io.c.vs + (int64_t)qs.bh * io.c.sc_stride;
+
+  f32x16 acc[D / 32];
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) acc[i] = zero16();
+  float m_run = kNoMax, l_run = 0.f;
+
+  // V: a lane's pieces of rows vrow and vrow + 16
+  char* tile = tiles[wave];
+  VOffsets<D, KC> vo;
+  vo.init(l32, half, lane);
+  int vrow, vcol;
+  lane_piece(lane, vrow, vcol);
+  const int sw = unit_swizzle(vrow) & (D / 8 - 1);
+
+  u32x4 kr[kK], vr[2][kPieces];
+  uint32_t ksc, vsc[2];
+  const DenseCursor<KC> cur = src.cursor(item, qs);
+  auto load = [&](int32_t pos) {
+    const int32_t last = cur.n - 1;
+    const int32_t kt = pos + l32 < last ? pos + l32 : last;
+#pragma unroll
+    for (int i = 0; i < kK; ++i)
+      kr[i] = *reinterpret_cast<const u32x4*>(kp + ((uint32_t)kt * D + half * (D / 2) + 16 * i));
+    ksc = ks[(uint32_t)kt >> io.c.lg];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int32_t r = pos + vrow + 16 * j, vt = r < last ? r : last;
+#pragma unroll
+      for (int p = 0; p < kPieces; ++p)
+        vr[j][p] = *reinterpret_cast<const u32x4*>(vp + ((uint32_t)vt * D + 16 * vcol + 64 * p));
+      vsc[j] = vs[(uint32_t)vt >> io.c.lg];
+    }
+  };
+  int32_t pos = cur.pos + wave * KC;
+  if (pos < cur.n) load(pos);
+  while (pos < cur.n) {
+    // V to LDS, K to the products
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int p = 0; p < kPieces; ++p) {
+        char* at = tile + (vrow + 16 * j) * kRow;
+        put_piece(at + 16 * ((2 * (vcol + 4 * p)) ^ sw), at + 16 * ((2 * (vcol + 4 * p) + 1) ^ sw), vr[j][p],
+                  scale_of_byte(vsc[j]));
+      }
+    wave_fence();
+    f32x16 st[1] = {zero16()};
+    const float fk = scale_of_byte(ksc);
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) {
+      uint32_t w0, w1, w2, w3;
+      decode4_bf16(kr[s / 2][2 * (s & 1)], fk, w0, w1);
+      decode4_bf16(kr[s / 2][2 * (s & 1) + 1], fk, w2, w3);
+      st[0] = mfma_bf16(as_bf16x8(u32x4{w0, w1, w2, w3}), qf[s], st[0]);
+    }
+    const int32_t count = cur.n - pos;
+    pos += kRowWaves * KC;
+    if (pos < cur.n) load(pos);
+    bf16x8 pf[KC / 16];
+    softmax_chunk<D, KC>(st, count, half, io.scale_log2, m_run, l_run, acc, pf);
+#pragma unroll
+    for (int s2 = 0; s2 < KC / 16; ++s2)
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt) acc[dt] = mfma_bf16(vo.read(tile, s2, dt), pf[s2], acc[dt]);
+    wave_fence();
+  }
+
+  // Join the waves: the row's maximum and sum, then each wave's registers 32 at a time
+  // through the tiles; wave w finishes eight of each 32, in wave order.
+  const float l_own = sum_halves(l_run);
+  if (half == 0) ml[wave][l32] = make_float2(m_run, l_own);
+  __syncthreads();
+  float m_g = kNoMax, l_g = 0.f;
+#pragma unroll
+  for (int w = 0; w < kRowWaves; ++w) m_g = fmaxf(m_g, ml[w][l32].x);
+#pragma unroll
+  for (int w = 0; w < kRowWaves; ++w) l_g += ml[w][l32].y * __builtin_amdgcn_exp2f(ml[w][l32].x - m_g);
+  const float own = __builtin_amdgcn_exp2f(m_run - m_g);
+  const float inv = io.part_o ? 1.f : (l_g > 0.f ? 1.f / l_g : 0.f);
+  const int64_t orow = (int64_t)plane * io.o_rows + qrow;
+  const int64_t prow = (int64_t)src.part_of(item) * io.rows + orow;
+  constexpr int kPass = kTile / 256;  // registers of a lane that a tile holds: 32 (D = 128) or 16
+#pragma unroll
+  for (int p = 0; p < D / 2 / kPass; ++p) {
+    if (p > 0) __syncthreads();
+    float* to = reinterpret_cast<float*>(tile) + lane;
+#pragma unroll
+    for (int i = 0; i < kPass; ++i) to[i * 64] = acc[(p * kPass + i) / 16][(p * kPass + i) % 16] * own;
+    __syncthreads();
+    if (!qvalid) continue;
+#pragma unroll
+    for (int g = 0; g < kPass / 16; ++g) {  // four registers are four neighbouring channels
+      const int i = (wave * (kPass / 16) + g) * 4;
+      float r[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < kRowWaves; ++w)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) r[e] += reinterpret_cast<const float*>(tiles[w])[(i + e) * 64 + lane];
+      const int reg = p * kPass + i, ch = 32 * (reg >> 4) + 8 * ((reg >> 2) & 3) + 4 * half;
+      if (io.part_o) {
+        *reinterpret_cast<float4*>(io.part_o + prow * D + ch) = make_float4(r[0], r[1], r[2], r[3]);
+      } else {
+        uint2 w;
+        w.x = pack_bf16x2(r[0] * inv, r[1] * inv);
+        w.y = pack_bf16x2(r[2] * inv, r[3] * inv);
+        *reinterpret_cast<uint2*>(io.o + orow * D + ch) = w;
+      }
+    }
+  }
+  if (qvalid && wave == 0 && half == 0) {
+    if (io.part_o) io.part_ml[prow] = make_float2(m_g, l_g);
+    else if (io.lse) io.lse[orow] = l_g > 0.f ? (m_g + __builtin_log2f(l_g)) * kLn2 : -INFINITY;
+  }
+}
+
+// Joins the parts of a row: a workgroup's threads are D / 4 channel groups times
+// 1024 / D groups of parts; the groups are added in order through LDS. A part without
+// keys has no sum and its values are not read.
 template <int D>
 __global__ __launch_bounds__(256) void join_parts_kernel(Q8IO io, int32_t parts) {
-  const int32_t row = blockIdx.x * (1024 / D) + threadIdx.x / (D / 4);
-  const int c = threadIdx.x % (D / 4) * 4;
-  if (row >= io.rows) return;
+  constexpr int C = D / 4, P = 256 / C;
+  __shared__ float4 sums[P][C];
+  __shared__ float ls[P];
+  const int32_t row = blockIdx.x;
+  const int c = threadIdx.x % C, g = threadIdx.x / C;
   float m = kNoMax;
-  for (int p = 0; p < parts; ++p) m = fmaxf(m, io.part_ml[(int64_t)p * io.rows + row].x);
-  float l = 0.f, r[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int p = 0; p < parts; ++p) {
+  for (int p = threadIdx.x & 63; p < parts; p += 64) m = fmaxf(m, io.part_ml[(int64_t)p * io.rows + row].x);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+  float l = 0.f;
+  float4 r = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int p = g; p < parts; p += P) {
     const int64_t prow = (int64_t)p * io.rows + row;
     const float2 ml = io.part_ml[prow];
     if (!(ml.y > 0.f)) continue;
     const float f = __builtin_amdgcn_exp2f(ml.x - m);
-    const float4 a = *reinterpret_cast<const float4*>(io.part_o + prow * D + c);
+    const float4 a = *reinterpret_cast<const float4*>(io.part_o + prow * D + 4 * c);
     l += ml.y * f;
-    r[0] += a.x * f;
-    r[1] += a.y * f;
-    r[2] += a.z * f;
-    r[3] += a.w * f;
+    r.x += a.x * f;
+    r.y += a.y * f;
+    r.z += a.z * f;
+    r.w += a.w * f;
+  }
+  sums[g][c] = r;
+  if (c == 0) ls[g] = l;
+  __syncthreads();
+  if (g > 0) return;
+  l = 0.f;
+  r = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+    l += ls[i];
+    r.x += sums[i][c].x;
+    r.y += sums[i][c].y;
+    r.z += sums[i][c].z;
+    r.w += sums[i][c].w;
   }
   const float inv = l > 0.f ? 1.f / l : 0.f;
   uint2 w;
-  w.x = pack_bf16x2(r[0] * inv, r[1] * inv);
-  w.y = pack_bf16x2(r[2] * inv, r[3] * inv);
-  *reinterpret_cast<uint2*>(io.o + (int64_t)row * D + c) = w;
+  w.x = pack_bf16x2(r.x * inv, r.y * inv);
+  w.y = pack_bf16x2(r.z * inv, r.w * inv);
+  *reinterpret_cast<uint2*>(io.o + (int64_t)row * D + 4 * c) = w;
   if (io.lse && c == 0) io.lse[row] = l > 0.f ? (m + __builtin_log2f(l)) * kLn2 : -INFINITY;
 }
 
-// Waves, slabs and parts of a dense call.
+// The form of a dense call: waves of a workgroup (0: the kernel for few rows, 32 rows a
+// workgroup), slabs of rows, parts of the keys.
 struct DenseQ8Plan {
   int waves;
   int32_t slabs, parts;
 };
 
-DenseQ8Plan dense_plan(int32_t planes, int32_t group, int32_t n_q, int32_t n_kv, int num_cu) {
-  DenseQ8Plan p;
-  const int64_t rows = (int64_t)group * n_q;
-  p.waves = rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
-  p.slabs = (int32_t)((rows + 32 * p.waves - 1) / (32 * p.waves));
-  // Parts: as many as fill two workgroups a CU, of at least four chunks each.
-  const int64_t items = planes * (int64_t)p.slabs, want = (2 * (int64_t)num_cu + items - 1) / items;
-  const int64_t most = (n_kv + 255) / 256;
-  p.parts = (int32_t)(want < most ? want : most);
-  if (p.parts > 64) p.parts = 64;
-  return p;
+// Expected time of a form, in us. With m workgroups on the busiest CU, which share it: f0 + f m
+// for starting and storing, and for every 64 keys of a part a + c m; at least what the codes
+// take at 5 TB/s, more where CUs idle in the last round and where few workgroups leave a tail. Parts cost a second
+// launch, some time each and their way through memory. f, a and c are fits to 256 m
+// workgroups, m = 1 .. 6, of 512 and 4608 keys and to the scales of an image; measured at d =
+// 128, us by the forms with few, 4 and 8 waves: 2 x 16 heads, 256 x 521 keys 9.1 / 15.6 / 22.5,
+// 400 x 921 16.8 / 21.7 / 31.4, 1024 x 2521 64 / 49.6 / 70, 1600 x 4121 158 / 119.7 / 115.2,
+// 2304 x 6425 314 / 277 / 342, 4096 x 10521 - / 612 / 592; 8 heads, 1024 x 2521 21.3 / 46.8 /
+// 70. One token of 8 heads, 10521 keys of one head: 281 us in one part, 11.5 in 21, 13.7 in 83;
+// one token of 4 x 32 heads, up to 42521 keys of 8 heads: 76.8 in 8 parts, 58.4 in 16, 62.2 in 32.
+struct DenseForm {
+  int waves;
+  float f0, f, a, c;
+};
+constexpr DenseForm kDenseForms[2][3] = {
+    {{0, 3.f, .6f, .05f, .20f}, {4, 3.f, 1.3f, .2f, .53f}, {8, 4.f, 4.4f, 0.f, 1.12f}},   // d = 64
+    {{0, 2.f, 2.2f, .15f, .35f}, {4, 3.5f, 3.f, .3f, .92f}, {8, 5.f, 6.f, 0.f, 1.77f}}};  // d = 128
+constexpr int kMostParts = 128;
+
+DenseQ8Plan dense_plan(int32_t planes, int32_t group, int32_t n_q, int32_t n_kv, int32_t d, int num_cu, bool may_split) {
+  const int64_t rows = (int64_t)group * n_q, chunks = ((int64_t)n_kv + 63) / 64;
+  const float memory = (float)planes * n_kv * d * (2.f / 5e6f);
+  DenseQ8Plan best{0, 1, 1};
+  float best_us = INFINITY;
+  for (const DenseForm& f : kDenseForms[d == 128]) {
+    const int64_t per = f.waves ? 32 * f.waves : 32, slabs = (rows + per - 1) / per, items = planes * slabs;
+    auto consider = [&](int64_t parts) {
+      if (parts > 1 && (!may_split || parts > chunks || parts > kMostParts)) return;
+      const float m = (float)((items * parts + num_cu - 1) / num_cu), even = (float)(items * parts) / (float)num_cu;
+      const float walk = (float)((chunks + parts - 1) / parts) * (f.a + f.c * m);
+      const float read = memory * (m / even) * (1.f + .25f / m);
+      float us = f.f0 + f.f * m + (walk > read ? walk : read);
+      if (parts > 1) us += 3.f + .08f * parts + (float)parts * planes * rows * d * (8.f / 3e6f);
+      if (us < best_us) {
+        best_us = us;
+        best = DenseQ8Plan{f.waves, (int32_t)slabs, (int32_t)parts};
+      }
+    };
+    // one part; growing numbers of parts while there is less than one workgroup a CU; whole
+    // workgroups a CU
+    for (int64_t parts = 1; parts == 1 || items * parts < num_cu; parts += parts < 4 ? 1 : parts / 4) consider(parts);
+    for (int64_t m = 1; m <= 8; ++m)
+      if (m * num_cu / items > 1) consider(m * num_cu / items);
+  }
+  return best;
 }
 
-template <int D, int NW, int KC, class Src>
-hipError_t launch_one(Q8IO io, const Src& src, hipStream_t stream) {
-  int32_t grid = io.n_items;
-  if (io.swizzle) grid = (grid + 7) / 8 * 8;
-  hipLaunchKernelGGL((attn_q8_kernel<D, NW, KC, Src>), dim3(grid), dim3(NW * 64), 0, stream, io, src);
+int32_t padded_grid(const Q8IO& io) { return io.swizzle ? (io.n_items + 7) / 8 * 8 : io.n_items; }
+
+template <int D, int QW, int KS, class Src>
+hipError_t launch_one(const Q8IO& io, const Src& src, hipStream_t stream) {
+  hipLaunchKernelGGL((attn_q8_kernel<D, QW, KS, Src>), dim3(padded_grid(io)), dim3(QW * KS * 64), 0, stream, io, src);
   return hipGetLastError();
 }
 
@@ -317,14 +739,13 @@ int64_t part_floats(int32_t parts, int64_t rows, int32_t d) { return (int64_t)pa
 }  // namespace
 
 int64_t dense_q8_workspace(int32_t B, int32_t H, int32_t H_kv, int32_t n_q, int32_t n_kv, int32_t d, int num_cu) {
-  const DenseQ8Plan p = dense_plan(B * H_kv, H / H_kv, n_q, n_kv, num_cu);
+  const DenseQ8Plan p = dense_plan(B * H_kv, H / H_kv, n_q, n_kv, d, num_cu, true);
   return p.parts > 1 ? 4 * part_floats(p.parts, (int64_t)B * H * n_q, d) : 0;
 }
 
 hipError_t launch_dense_attn_q8(const DenseQ8Args& a, hipStream_t stream) {
   const int32_t group = a.H / a.H_kv;
-  DenseQ8Plan p = dense_plan(a.B * a.H_kv, group, a.n_q, a.n_kv, a.num_cu);
-  if (!a.workspace) p.parts = 1;
+  const DenseQ8Plan p = dense_plan(a.B * a.H_kv, group, a.n_q, a.n_kv, a.d, a.num_cu, a.workspace != nullptr);
   Q8IO io;
   io.q = static_cast<const bf16_bits*>(a.q);
   io.o = static_cast<bf16_bits*>(a.o);
@@ -339,25 +760,32 @@ hipError_t launch_dense_attn_q8(const DenseQ8Args& a, hipStream_t stream) {
   io.rows = a.B * a.H * a.n_q;
   io.part_o = p.parts > 1 ? a.workspace : nullptr;
   io.part_ml = p.parts > 1 ? reinterpret_cast<float2*>(a.workspace + (int64_t)p.parts * io.rows * a.d) : nullptr;
-  DenseQ8Src<64> src;
-  src.n_q = a.n_q;
-  src.n_kv = a.n_kv;
-  src.H_kv = a.H_kv;
-  src.group = group;
-  src.slabs = p.slabs;
-  src.q_per_wg = 32 * p.waves;
-  src.parts = p.parts;
-  src.kv_len = a.kv_len;
+  auto fill = [&](auto src) {
+    src.n_q = a.n_q;
+    src.n_kv = a.n_kv;
+    src.H_kv = a.H_kv;
+    src.group = group;
+    src.slabs = p.slabs;
+    src.q_per_wg = p.waves ? 32 * p.waves : 32;
+    src.parts = p.parts;
+    src.kv_len = a.kv_len;
+    return src;
+  };
   hipError_t e = hipErrorInvalidValue;
-#define SV_DENSE(DD, NN) \
-  if (a.d == DD && p.waves == NN) e = launch_one<DD, NN, 64>(io, src, stream);
-  SV_DENSE(64, 1) SV_DENSE(64, 2) SV_DENSE(64, 4) SV_DENSE(128, 1) SV_DENSE(128, 2) SV_DENSE(128, 4)
-#undef SV_DENSE
+  if (p.waves == 0) {
+    const int32_t grid = padded_grid(io);
+    const DenseQ8Src<32> src = fill(DenseQ8Src<32>{});
+    if (a.d == 128) hipLaunchKernelGGL((attn_q8_rows_kernel<128>), dim3(grid), dim3(kRowWaves * 64), 0, stream, io, src);
+    else hipLaunchKernelGGL((attn_q8_rows_kernel<64>), dim3(grid), dim3(kRowWaves * 64), 0, stream, io, src);
+    e = hipGetLastError();
+  } else {
+    const DenseQ8Src<64> src = fill(DenseQ8Src<64>{});
+    if (a.d == 128) e = p.waves == 4 ? launch_one<128, 4, 1>(io, src, stream) : launch_one<128, 8, 1>(io, src, stream);
+    else e = p.waves == 4 ? launch_one<64, 4, 1>(io, src, stream) : launch_one<64, 8, 1>(io, src, stream);
+  }
   if (e != hipSuccess || p.parts == 1) return e;
-  const int per = 1024 / a.d;
-  const int32_t grid = (io.rows + per - 1) / per;
-  if (a.d == 128) hipLaunchKernelGGL((join_parts_kernel<128>), dim3(grid), dim3(256), 0, stream, io, p.parts);
-  else hipLaunchKernelGGL((join_parts_kernel<64>), dim3(grid), dim3(256), 0, stream, io, p.parts);
+  if (a.d == 128) hipLaunchKernelGGL((join_parts_kernel<128>), dim3(io.rows), dim3(256), 0, stream, io, p.parts);
+  else hipLaunchKernelGGL((join_parts_kernel<64>), dim3(io.rows), dim3(256), 0, stream, io, p.parts);
   return hipGetLastError();
 }
 
@@ -392,10 +820,16 @@ hipError_t launch_sparse_attn_q8(const SparseQ8Args& a, hipStream_t stream) {
   src.q_per_wg = qpw;
   src.slabs = slabs;
   src.n_rows = a.BH * G_k;
-#define SV_SPARSE(DD, NN) \
-  if (a.d == DD && nw == NN) return launch_one<DD, NN, 64>(io, src, stream);
-  SV_SPARSE(64, 1) SV_SPARSE(64, 2) SV_SPARSE(64, 4) SV_SPARSE(64, 8)
-  SV_SPARSE(128, 1) SV_SPARSE(128, 2) SV_SPARSE(128, 4) SV_SPARSE(128, 8)
+  // Tiles of 33 to 64 queries (8 x 8): launches of few waves a SIMD walk their rows in two parts
+  // (8 heads of a 64 x 64 scale, 512 workgroups: d = 128 37.2 against 45.8 us, d = 64 25.0 /
+  // 32.4; 12 heads, 768: 53.9 / 48.8 and 31.6 / 34; 800: d = 64 36.9 / 35.6), d = 64 in four up
+  // to one workgroup a CU (128 workgroups: 17.0 against 18.5).
+  int ks = 1;
+  if (nw == 2 && io.n_items <= (a.d == 64 ? 3 : 2) * a.num_cu) ks = a.d == 64 && io.n_items <= a.num_cu ? 4 : 2;
+#define SV_SPARSE(DD, NN, KK) \
+  if (a.d == DD && nw == NN && ks == KK) return launch_one<DD, NN, KK>(io, src, stream);
+  SV_SPARSE(64, 1, 1) SV_SPARSE(64, 2, 1) SV_SPARSE(64, 2, 2) SV_SPARSE(64, 2, 4) SV_SPARSE(64, 4, 1) SV_SPARSE(64, 8, 1)
+  SV_SPARSE(128, 1, 1) SV_SPARSE(128, 2, 1) SV_SPARSE(128, 2, 2) SV_SPARSE(128, 4, 1) SV_SPARSE(128, 8, 1)
 #undef SV_SPARSE
   return hipErrorInvalidValue;
 }

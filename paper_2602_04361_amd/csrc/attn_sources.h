@@ -871,6 +871,64 @@ constexpr bool kRemapOf<Src, std::void_t<decltype(Src::kRemap)>> = Src::kRemap;
 // walk starts anywhere in the row, so its first keys may well be such keys.
 constexpr float kNoMax = -3.402823466e38f;
 
+// Merge of KS key splits of one workgroup (QW query waves each): the softmax maximum
+// m_g and sum l_g over the splits, and in out the unnormalised sums of the accumulator
+// registers [split R, (split + 1) R) (16 per 32-channel group, R = D / 2 / KS) that
+// this wave finishes, added in split order. The other splits hand theirs over through the stage arrays s0 and s1 of SB
+// bytes each, which every wave has finished with by the first barrier.
+template <int D, int QW, int KS, int SB>
+__device__ __forceinline__ void merge_key_splits(const f32x16 (&acc)[D / 32], float m_run, float l_run, int split,
+                                                 int qwave, int lane, char* s0, char* s1,
+                                                 float (&ml)[KS][QW * kQPerWave][2], float& m_g, float& l_g,
+                                                 float (&out)[D / 2 / KS]) {
+  constexpr int R = D / 2 / KS;
+  constexpr int kPart = R * 64;  // floats one wave hands to one other split
+  constexpr int kHalf = SB / (kPart * 4);
+  static_assert(R % 4 == 0, "output channels must split into groups of four");
+  static_assert(KS * (KS - 1) * QW <= 2 * kHalf, "split outputs must fit the stages they merge through");
+  const int slot = qwave * kQPerWave + (lane & 31);
+  const float l_tot = sum_halves(l_run);
+  if (lane < 32) {
+    ml[split][slot][0] = m_run;
+    ml[split][slot][1] = l_tot;
+  }
+  __syncthreads();
+  m_g = kNoMax;
+#pragma unroll
+  for (int s = 0; s < KS; ++s) m_g = fmaxf(m_g, ml[s][slot][0]);
+  l_g = 0.f;
+#pragma unroll
+  for (int s = 0; s < KS; ++s) l_g += ml[s][slot][1] * __builtin_amdgcn_exp2f(ml[s][slot][0] - m_g);
+  const float own = __builtin_amdgcn_exp2f(m_run - m_g);
+  auto part = [&](int t, int from) {
+    const int i = (t * (KS - 1) + (from < t ? from : from - 1)) * QW + qwave;
+    char* base = i < kHalf ? s0 + i * (kPart * 4) : s1 + (i - kHalf) * (kPart * 4);
+    return reinterpret_cast<float*>(base) + lane;
+  };
+#pragma unroll
+  for (int t = 0; t < KS; ++t) {
+    if (t == split) continue;
+    float* to = part(t, split);
+#pragma unroll
+    for (int i = 0; i < R; ++i) to[i * 64] = acc[(t * R + i) / 16][(t * R + i) % 16] * own;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int t = 0; t < KS; ++t) {
+    if (t != split) continue;  // (a compare per split, so that register indices stay constant)
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      float r = 0.f;
+#pragma unroll
+      for (int u = 0; u < KS; ++u) r += u == t ? acc[(t * R + i) / 16][(t * R + i) % 16] * own : part(t, u)[i * 64];
+      out[i] = r;
+    }
+  }
+}
+
+// Channel of the first of the four accumulator registers 4 i .. 4 i + 3.
+__device__ __forceinline__ int channel_of(int i, int half) { return 32 * (i >> 2) + 8 * (i & 3) + 4 * half; }
+
 // Waves (32 queries each) for a tile of that many queries.
 inline int waves_for(int32_t queries) {
   if (queries <= 32) return 1;

@@ -25,6 +25,17 @@ __device__ __forceinline__ int32_t block_exponent(float top) {
 __device__ __forceinline__ float scale_of_byte(uint32_t byte) { return __uint_as_float(byte << 23); }
 __device__ __forceinline__ float pow2f(int32_t e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
 
+// Four codes of values within the format's range.
+__device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  w = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+  return (uint32_t)w;
+#else
+  return 0;
+#endif
+}
+
 // Four codes of x * inv (inv = 2^-e, so the product is exact but for underflow far below
 // a code's step): rounded to nearest even, saturated at 448, NaN kept.
 __device__ __forceinline__ uint32_t encode4(const float* x, float inv) {
@@ -35,13 +46,7 @@ __device__ __forceinline__ uint32_t encode4(const float* x, float inv) {
     const float s = fminf(fmaxf(t, -kE4m3Max), kE4m3Max);
     y[i] = t == t ? s : t;
   }
-#if defined(__HIP_DEVICE_COMPILE__)
-  int w = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
-  w = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], w, true);
-  return (uint32_t)w;
-#else
-  return 0;
-#endif
+  return codes4(y[0], y[1], y[2], y[3]);
 }
 
 // Values of four codes times s.

@@ -244,10 +244,16 @@ def launch_options(**opts):
 
 
 # ---------------------------------------------------------------- tensor helpers
-def _torch():
-    import torch  # imported lazily so that the geometry helpers work without torch
+_torch_module = None
 
-    return torch
+
+def _torch():
+    global _torch_module  # (an import statement takes 0.3 us a call, and a call asks several times)
+    if _torch_module is None:
+        import torch  # imported lazily so that the geometry helpers work without torch
+
+        _torch_module = torch
+    return _torch_module
 
 
 def _dtype_code(t):
@@ -509,19 +515,32 @@ def sparvar_block_sparse_attn_fwd(geom, k, q_k, k_lek, v_lek, o, row_ptr, col_id
 
 
 # ---------------------------------------------------------------- 8-bit cache
-def _here(*tensors):
-    """Every tensor is on the current device (None: not given)."""
-    torch = _torch()
-    dev = None
-    for t in tensors:
-        if t is None:
-            continue
-        if dev is None:
-            if not t.is_cuda:
-                raise SparvarError(ERR_INVALID, f"a tensor is on {t.device}, not on a GPU")
-            dev = torch.cuda.current_device()
-        if t.get_device() != dev:
-            raise SparvarError(ERR_INVALID, f"a tensor is on {t.device}, the current device is cuda:{dev}")
+def _here(first, *others):
+    """Every tensor is on the current device (None among the others: not given)."""
+    dev = first.get_device()
+    if dev < 0:
+        raise SparvarError(ERR_INVALID, f"a tensor is on {first.device}, not on a GPU")
+    if dev != _torch()._C._cuda_getDevice():
+        raise SparvarError(ERR_INVALID, f"a tensor is on {first.device}, which is not the current device")
+    for t in others:
+        if t is not None and t.get_device() != dev:
+            raise SparvarError(ERR_INVALID, f"tensors are on {t.device} and {first.device}")
+    return dev
+
+
+def _on(dev, *objects):
+    """Caches and maps (or None) whose tensors are on device dev."""
+    for x in objects:
+        if x is not None and x.device != dev:
+            raise SparvarError(ERR_INVALID, f"the tensors of a {type(x).__name__} are on device {x.device}, not on {dev}")
+
+
+def _shared_device(name, *tensors):
+    """The one device that tensors (None: not given) are on; None without any."""
+    devices = {t.get_device() for t in tensors if t is not None}
+    if len(devices) > 1:
+        raise SparvarError(ERR_INVALID, f"the tensors of a {name} are on several devices")
+    return devices.pop() if devices else None
 
 
 def _same(name, t, shape, dtype):
@@ -555,6 +574,8 @@ class Q8Cache:
                     t.stride(1) != k_scale.stride(1) or (self.B > 1 and t.stride(0) != self.H_kv * t.stride(1)):
                 raise SparvarError(ERR_INVALID, f"{name} must be [B,H_kv,>= {blocks}] with evenly spaced planes, as the other's")
         self.block, self.k, self.v, self.k_scale, self.v_scale = int(block), k, v, k_scale, v_scale
+        self.device = _shared_device("Q8Cache", k, v, k_scale, v_scale)
+        self.planes = (self.B, self.H_kv, self.d)
         self.c = _CQ8Cache(self.block, self.capacity, k.data_ptr(), v.data_ptr(), self.bh_stride, k_scale.data_ptr(),
                            v_scale.data_ptr(), k_scale.stride(1))
         self.ref = ctypes.byref(self.c)
@@ -586,6 +607,9 @@ class NormRope:
         if cos_sin is not None and cos_sin.shape[2] != 2:
             raise SparvarError(ERR_INVALID, "cos_sin must be [rows, d/2, 2]")
         self.q_weight, self.k_weight, self.cos_sin = q_weight, k_weight, cos_sin
+        self.device = _shared_device("NormRope", q_weight, k_weight, cos_sin)
+        self.q_shape, self.k_shape = (None if t is None else tuple(t.shape) for t in (q_weight, k_weight))
+        self.d = None if cos_sin is None else 2 * cos_sin.shape[1]
         self.c = _CNormRope(NORMS[norm], ROPE_LAYOUTS[layout], float(eps), 0 if cos_sin is None else cos_sin.shape[0],
                             _ptr(q_weight), _ptr(k_weight), _ptr(cos_sin))
         self.ref = ctypes.byref(self.c)
@@ -607,62 +631,61 @@ def sparvar_qkv_append(q, k, v, t0, heads, q_out, k_cache=None, v_cache=None, q8
     and values to k_cache, v_cache or to an 8-bit cache q8; see sparvar.h."""
     lib = load_library()
     B, n, H, d = q.shape
-    H_kv = k.shape[2]
+    kv_shape = k.shape
+    H_kv = kv_shape[2]
     qb, qt = _token_strides(q, "q")
-    kb, kt = _token_strides(k, "k")
-    if v.shape != k.shape or _token_strides(v, "v") != (kb, kt):
+    kb, kt = kv = _token_strides(k, "k")
+    if v.shape != kv_shape or _token_strides(v, "v") != kv:
         raise SparvarError(ERR_INVALID, "k and v must share their shape and strides")
-    if k.shape != (B, n, H_kv, d):
+    if kv_shape != (B, n, H_kv, d):
         raise SparvarError(ERR_INVALID, "q and k must share batch, tokens and d")
+    dtype = q.dtype
     dt = _dtype_code(q)
-    if k.dtype != q.dtype or v.dtype != q.dtype:
+    if k.dtype != dtype or v.dtype != dtype:
         raise SparvarError(ERR_INVALID, "q, k and v must share a dtype")
-    _same("q_out", q_out, (B, H, n, d), q.dtype)
-    _here(q, k, v, q_out, k_cache, v_cache)
+    _same("q_out", q_out, (B, H, n, d), dtype)
+    dev = _here(q, k, v, q_out, k_cache, v_cache)
     if heads is not None:
-        for name, t, shape in (("q_weight", heads.q_weight, (H, d)), ("k_weight", heads.k_weight, (H_kv, d))):
-            if t is not None and t.shape != shape:
-                raise SparvarError(ERR_INVALID, f"{name} must be {list(shape)}")
-        if heads.cos_sin is not None and heads.cos_sin.shape[1] * 2 != d:
-            raise SparvarError(ERR_INVALID, "cos_sin must be [rows, d/2, 2]")
-        _here(heads.q_weight, heads.k_weight, heads.cos_sin)
+        if heads.q_shape not in (None, (H, d)) or heads.k_shape not in (None, (H_kv, d)) or heads.d not in (None, d):
+            raise SparvarError(ERR_INVALID, f"weights must be [{H},{d}] and [{H_kv},{d}], cos_sin [rows,{d // 2},2]")
+        if heads.device is not None:
+            _on(dev, heads)
     cs = 0
     if k_cache is not None and v_cache is not None:
         cs = _plane_stride(k_cache, "k_cache")
         if v_cache.shape != k_cache.shape or _plane_stride(v_cache, "v_cache") != cs:
             raise SparvarError(ERR_INVALID, "k_cache and v_cache must share their shape and plane stride")
-        if k_cache.dtype != q.dtype or v_cache.dtype != q.dtype or k_cache.shape[:2] != (B, H_kv) or k_cache.shape[3] != d:
-            raise SparvarError(ERR_INVALID, f"the caches must be [{B},{H_kv},tokens,{d}] of {q.dtype}")
+        if k_cache.dtype != dtype or v_cache.dtype != dtype or k_cache.shape[:2] != (B, H_kv) or k_cache.shape[3] != d:
+            raise SparvarError(ERR_INVALID, f"the caches must be [{B},{H_kv},tokens,{d}] of {dtype}")
         if t0 + n > k_cache.shape[2]:
             raise SparvarError(ERR_CAPACITY, f"tokens up to {t0 + n} exceed the cache's {k_cache.shape[2]}")
     if q8 is not None:
-        _check_q8(q8, B, H_kv, d)
+        _check_q8(q8, B, H_kv, d, dev)
     _check(lib.sparvar_qkv_append(B, H, H_kv, d, dt, n, t0, _ptr(q), qb, qt, _ptr(k), _ptr(v), kb, kt,
                                   None if heads is None else heads.ref, _ptr(q_out), _ptr(k_cache), _ptr(v_cache), cs,
                                   None if q8 is None else q8.ref, _stream(stream)))
     return q_out
 
 
-def _check_q8(q8, B, H_kv, d):
-    if (q8.B, q8.H_kv, q8.d) != (B, H_kv, d):
+def _check_q8(q8, B, H_kv, d, dev):
+    if q8.planes != (B, H_kv, d):
         raise SparvarError(ERR_INVALID, f"the cache is [{q8.B},{q8.H_kv},{q8.capacity},{q8.d}], not of [{B},{H_kv},.,{d}]")
-    _here(q8.k, q8.v, q8.k_scale, q8.v_scale)
+    _on(dev, q8)
 
 
 def _kv_planes(k, v):
     stride = _plane_stride(k, "k")
     if v.shape != k.shape or v.dtype != k.dtype or _plane_stride(v, "v") != stride:
         raise SparvarError(ERR_INVALID, "k and v must share their shape, dtype and plane stride")
-    _here(k, v)
-    return stride
+    return stride, _here(k, v)
 
 
 def sparvar_kv_quantize(k_src, v_src, t0, q8, stream=None):
     """Write rows of k_src, v_src [B,H_kv,n,d] to tokens [t0, t0 + n) of an 8-bit cache; see sparvar.h."""
     lib = load_library()
     B, H_kv, n, d = k_src.shape
-    stride = _kv_planes(k_src, v_src)
-    _check_q8(q8, B, H_kv, d)
+    stride, dev = _kv_planes(k_src, v_src)
+    _check_q8(q8, B, H_kv, d, dev)
     _check(lib.sparvar_kv_quantize(B, H_kv, d, _dtype_code(k_src), n, t0, _ptr(k_src), _ptr(v_src), stride, q8.ref,
                                    _stream(stream)))
     return q8
@@ -672,8 +695,8 @@ def sparvar_kv_dequantize(q8, t0, k_dst, v_dst, stream=None):
     """Read tokens [t0, t0 + n) of an 8-bit cache back to k_dst, v_dst [B,H_kv,n,d]; see sparvar.h."""
     lib = load_library()
     B, H_kv, n, d = k_dst.shape
-    stride = _kv_planes(k_dst, v_dst)
-    _check_q8(q8, B, H_kv, d)
+    stride, dev = _kv_planes(k_dst, v_dst)
+    _check_q8(q8, B, H_kv, d, dev)
     _check(lib.sparvar_kv_dequantize(B, H_kv, d, _dtype_code(k_dst), n, t0, q8.ref, _ptr(k_dst), _ptr(v_dst), stride,
                                      _stream(stream)))
     return k_dst, v_dst
@@ -687,15 +710,14 @@ def sparvar_dense_attn_q8_workspace(B, H, H_kv, n_q, n_kv, d):
     return int(n)
 
 
-def _q8_attn(q, q8, o, lse):
+def _q8_attn(q, q8, o, lse, *others):
     """The checks that both attention calls over an 8-bit cache share."""
-    B, H, n_q, d = q.shape
+    shape = q.shape
     dt = _dtype_code(q)
-    _same("o", o, q.shape, q.dtype)
+    _same("o", o, shape, q.dtype)
     if lse is not None:
-        _same("lse", lse, (B, H, n_q), _torch().float32)
-    _here(q, o, lse)
-    _check_q8(q8, B, q8.H_kv, d)
+        _same("lse", lse, shape[:3], _torch().float32)
+    _check_q8(q8, shape[0], q8.H_kv, shape[3], _here(q, o, lse, *others))
     return dt
 
 
@@ -704,15 +726,14 @@ def sparvar_dense_attn_q8_fwd(q, q8, n_kv, o, lse=None, kv_len=None, softmax_sca
     contiguous tensor of at least sparvar_dense_attn_q8_workspace() bytes, or None; see sparvar.h."""
     lib = load_library()
     B, H, n_q, d = q.shape
-    dt = _q8_attn(q, q8, o, lse)
+    dt = _q8_attn(q, q8, o, lse, kv_len, workspace)
     if kv_len is not None:
         _same("kv_len", kv_len, (B,), _torch().int32)
     size = 0
     if workspace is not None:
         if not workspace.is_contiguous():
             raise SparvarError(ERR_INVALID, "workspace must be contiguous")
-        size = workspace.numel() * workspace.element_size()
-    _here(kv_len, workspace)
+        size = workspace.nbytes
     _check(lib.sparvar_dense_attn_q8_fwd(B, H, q8.H_kv, n_q, n_kv, d, dt, _ptr(q), _plane_stride(q, "q"), q8.ref,
                                          _ptr(kv_len), _ptr(o), _ptr(lse), _scale(softmax_scale, d), _ptr(workspace), size,
                                          _stream(stream)))
@@ -726,11 +747,10 @@ def sparvar_block_sparse_attn_q8_fwd(geom, k, q_k, q8, o, row_ptr, col_idx, lse=
     B, H, n, d = q_k.shape
     if 1 <= k <= len(geom.h) and n != geom.h[k - 1] * geom.w[k - 1]:
         raise SparvarError(ERR_INVALID, f"q_k has {n} rows, scale {k} has {geom.h[k - 1] * geom.w[k - 1]} tokens")
-    dt = _q8_attn(q_k, q8, o, lse)
+    dt = _q8_attn(q_k, q8, o, lse, row_ptr, col_idx, schedule)
     i32 = _torch().int32
     if row_ptr.dtype != i32 or col_idx.dtype != i32 or (schedule is not None and schedule.dtype != i32):
         raise SparvarError(ERR_INVALID, "row_ptr, col_idx and schedule must be int32")
-    _here(row_ptr, col_idx, schedule)
     _check(lib.sparvar_block_sparse_attn_q8_fwd(geom.ref, k, B, H, q8.H_kv, d, dt, _ptr(q_k), _plane_stride(q_k, "q_k"),
                                                 q8.ref, _ptr(o), _ptr(lse), _scale(softmax_scale, d), _ptr(row_ptr),
                                                 _ptr(col_idx), _ptr(schedule), _stream(stream)))

@@ -1,9 +1,10 @@
 """GPU parity of attention over an 8-bit cache, dense and block-sparse, through the C ABI, against the fp64 oracle on the
 values that the codes stand for.
 
-Tolerance: K and V are exact in bf16 and Q is given, so what is rounded to 16 bits are the probabilities and the output,
-each by at most u = 2^-8 of its value: |o - ref| <= u (sum_j p_j |v_j| + |ref|), times 1.02 for what 32-bit sums and the
-exponential add (both below 2^-14 here). The log of the softmax denominator is held to 2e-4, as everywhere."""
+Tolerance: K and V are exact and Q is given, so what is rounded to 16 bits are the probabilities and the output, each by
+at most u = 2^-8 of its value: |o - ref| <= u (sum_j p_j |v_j| + |ref|), times 1.02 for what 32-bit sums, the exponential
+and queries' elements below 2^-10 of their row's largest (held to 2^-18 of it) add: a score is off by less than 2^-14 for
+the rows of unit normals here. The log of the softmax denominator is held to 2e-4, as everywhere."""
 import numpy as np
 import pytest
 import torch
@@ -88,7 +89,11 @@ def run_dense(B, H, Hkv, nq, nkv, d, G, lens=None, ws=False, seed=0, cap=None, p
 @pytest.mark.parametrize("B,H,Hkv,nq,nkv,d,G", [
     (1, 1, 1, 1, 1, 128, 64), (2, 3, 3, 4, 5, 64, 32), (1, 2, 2, 16, 21, 128, 16), (2, 2, 2, 64, 121, 128, 64),
     (1, 2, 2, 33, 63, 64, 16), (1, 2, 2, 65, 64, 128, 128), (1, 1, 1, 129, 65, 64, 64), (1, 2, 1, 257, 300, 128, 32),
-    (1, 4, 2, 36, 57, 64, 64), (2, 8, 2, 1, 777, 128, 64), (1, 8, 1, 7, 1500, 64, 128), (1, 16, 1, 5, 333, 128, 16)])
+    (1, 4, 2, 36, 57, 64, 64), (2, 8, 2, 1, 777, 128, 64), (1, 8, 1, 7, 1500, 64, 128), (1, 16, 1, 5, 333, 128, 16),
+    # long enough for parts: few rows, odd lengths and more parts than chunks divide into
+    (1, 8, 2, 1, 9001, 128, 64), (1, 2, 2, 1, 20011, 64, 16), (1, 8, 1, 6, 7777, 64, 32), (1, 2, 2, 70, 8000, 128, 64),
+    # slabs of 128 and 256 rows
+    (2, 8, 8, 900, 1000, 128, 32), (2, 8, 8, 900, 1000, 64, 64), (2, 16, 16, 1600, 1000, 128, 64), (2, 16, 16, 1600, 200, 64, 16)])
 @pytest.mark.parametrize("ws", [False, True])
 def test_dense(B, H, Hkv, nq, nkv, d, G, ws):
     note(f"[q8 dense] B={B} H={H}/{Hkv} nq={nq} nkv={nkv} d={d} G={G} ws={ws}")
@@ -96,7 +101,7 @@ def test_dense(B, H, Hkv, nq, nkv, d, G, ws):
 
 
 @pytest.mark.parametrize("ws", [False, True])
-@pytest.mark.parametrize("nq,nkv,d", [(1, 4000, 128), (20, 900, 64), (100, 500, 128)])
+@pytest.mark.parametrize("nq,nkv,d", [(1, 4000, 128), (20, 900, 64), (100, 500, 128), (1000, 300, 128)])
 def test_dense_lengths(nq, nkv, d, ws):
     """Lengths of their own: none, negative, one, a chunk's edge, past the end; codes past a length are NaN."""
     lens = [0, -3, 1, 63, 64, 65, 200, nkv - 1, nkv, nkv + 99]
@@ -137,6 +142,33 @@ def test_dense_full_size():
         rows = np.sort(r.choice(nq, 200, replace=False))
         check_rows(o[0, h].double().cpu().numpy()[rows], lse[0, h].double().cpu().numpy()[rows],
                    q[0, h].double().cpu().numpy()[rows], k[0, h], v[0, h], scale_of(d), what=f"head {h}")
+
+
+def test_queries_of_any_size():
+    """Queries times 2^60 under a scale divided by it give the same; rows whose elements spread over 2^24 keep the bound with
+    a score's own error added: scale 2^-18 max|q| sum|k|, twice it on a probability."""
+    note("[q8 dense] sizes of queries")
+    B, H, nq, nkv, d = 1, 1, 300, 400, 128
+    for rows in (20, nq):  # few rows, slabs
+        q8, k, v = make_cache(B, H, nkv, d, 64, 77)
+        g = torch.Generator(device="cuda").manual_seed(rows)
+        q = torch.randn(B, H, rows, d, generator=g, device="cuda").bfloat16()
+        o = [torch.empty_like(q) for _ in range(2)]
+        sv.sparvar_dense_attn_q8_fwd(q, q8, nkv, o[0], softmax_scale=0.0625)
+        sv.sparvar_dense_attn_q8_fwd(q * 2.0 ** 60, q8, nkv, o[1], softmax_scale=0.0625 * 2.0 ** -60)
+        torch.cuda.synchronize()
+        assert torch.equal(o[0], o[1])
+        spread = torch.randint(-24, 1, q.shape, generator=g, device="cuda").float().exp2()
+        q = (q * spread * 4).bfloat16()
+        sv.sparvar_dense_attn_q8_fwd(q, q8, nkv, o[0], softmax_scale=0.0625)
+        torch.cuda.synchronize()
+        qn, kn, vn, on = q[0, 0].double().cpu().numpy(), k[0, 0], v[0, 0], o[0][0, 0].double().cpu().numpy()
+        s = qn @ kn.T * 0.0625
+        p = np.exp(s - s.max(1, keepdims=True))
+        p /= p.sum(1, keepdims=True)
+        ref, size = p @ vn, p @ np.abs(vn)
+        off = 2 * 0.0625 * 2.0 ** -18 * np.abs(qn).max(1) * np.abs(kn).sum(1).max()
+        assert (np.abs(on - ref) <= 1.02 * U16 * (size + np.abs(ref)) + 2 * off[:, None] * size + 1e-30).all()
 
 
 def test_scores_that_spread():
@@ -209,6 +241,8 @@ def run_sparse(h, w, b, k, B, H, Hkv, d, G, seed, empty=(), order=False, dup=Non
     ([1, 3, 5, 7, 11], [1, 4, 6, 9, 13], 4, 5, 1, 4, 2, 128, 16),   # small tiles, shared heads
     ([1, 2, 4, 8, 20], [1, 2, 4, 8, 20], 16, 5, 1, 2, 1, 128, 128), # tiles of four chunks
     ([2, 9, 13], [2, 9, 13], 3, 3, 1, 2, 2, 64, 16), ([40], [70], 33, 1, 1, 1, 1, 64, 64),
+    ([1, 4, 30], [1, 4, 30], 8, 3, 2, 20, 20, 64, 64), ([1, 4, 30], [1, 4, 30], 8, 3, 2, 20, 20, 128, 64),  # one part a row
+    ([1, 4, 30], [1, 4, 30], 8, 3, 1, 20, 20, 64, 64), ([1, 4, 30], [1, 4, 30], 5, 3, 1, 2, 2, 128, 16),
     ([1, 70], [1, 70], 64, 2, 1, 1, 1, 128, 64)])                   # tile rows of a whole chunk
 @pytest.mark.parametrize("order", [False, True])
 def test_sparse(h, w, b, k, B, H, Hkv, d, G, order):

@@ -72,27 +72,30 @@ def test_norm_rope_struct(bad, status):
     assert append(h=heads(**bad)) == status
 
 
+LONG = cache(capacity=20000, bh_stride=20000 * 64, scale_bh_stride=313)
+
+
 def dense(**kw):
     a = dict(B=2, H=4, Hkv=2, nq=10, nkv=100, d=64, dt=sv.BF16, q=FAKE, qs=640, o=FAKE, sc=0.1, ws=None, size=0)
     a.update(kw)
     return sv.load_library().sparvar_dense_attn_q8_fwd(a["B"], a["H"], a["Hkv"], a["nq"], a["nkv"], a["d"], a["dt"], a["q"],
-                                                       a["qs"], ctypes.byref(cache()), None, a["o"], None, a["sc"], a["ws"],
+                                                       a["qs"], ctypes.byref(LONG), None, a["o"], None, a["sc"], a["ws"],
                                                        a["size"], None)
 
 
 @pytest.mark.parametrize("bad,status", [
     (dict(dt=sv.F32), sv.ERR_UNSUPPORTED), (dict(d=80), sv.ERR_UNSUPPORTED), (dict(H=5), sv.ERR_INVALID),
-    (dict(nq=0), sv.ERR_INVALID), (dict(nkv=0), sv.ERR_INVALID), (dict(nkv=1001), sv.ERR_CAPACITY), (dict(q=None), sv.ERR_INVALID),
+    (dict(nq=0), sv.ERR_INVALID), (dict(nkv=0), sv.ERR_INVALID), (dict(nkv=20001), sv.ERR_CAPACITY), (dict(q=None), sv.ERR_INVALID),
     (dict(qs=639), sv.ERR_INVALID), (dict(o=FAKE + 2), sv.ERR_INVALID), (dict(sc=0.0), sv.ERR_INVALID),
-    (dict(sc=float("inf")), sv.ERR_INVALID), (dict(ws=FAKE, size=16, nkv=1000), sv.ERR_CAPACITY),
-    (dict(ws=FAKE + 4, size=1 << 30, nkv=1000), sv.ERR_INVALID)])
+    (dict(sc=float("inf")), sv.ERR_INVALID), (dict(ws=FAKE, size=16, nkv=20000), sv.ERR_CAPACITY),
+    (dict(ws=FAKE + 4, size=1 << 30, nkv=20000), sv.ERR_INVALID)])
 def test_dense_arguments(bad, status):
     assert dense(**bad) == status
 
 
 def test_dense_workspace():
     lib = sv.load_library()
-    assert sv.sparvar_dense_attn_q8_workspace(1, 4, 2, 1, 1000, 64) > 0
+    assert sv.sparvar_dense_attn_q8_workspace(1, 4, 2, 1, 20000, 64) >= 2 * 4 * (64 + 2) * 4  # two parts of four rows
     assert sv.sparvar_dense_attn_q8_workspace(2, 16, 16, 4096, 10521, 128) == 0
     assert sv.sparvar_dense_attn_q8_workspace(2, 16, 16, 1, 40, 128) == 0
     assert lib.sparvar_dense_attn_q8_workspace(1, 3, 2, 1, 1000, 64) == sv.ERR_INVALID
