@@ -15,7 +15,7 @@ namespace sparvar {
 
 namespace {
 
-constexpr int kNT = 256;
+constexpr int kNT = 256;  // threads of a workgroup that encodes no block
 
 // ------------------------------------------------------------------ eight channels
 template <int D, int LAY>
@@ -76,8 +76,15 @@ __device__ __forceinline__ void load_codes(const uint8_t* row, int u, uint32_t& 
 }
 
 template <int D, int LAY>
-__device__ __forceinline__ void store_codes(uint8_t* row, int u, const float (&x)[8], float inv) {
-  const uint32_t a = encode4(x, inv), b = encode4(x + 4, inv);
+__device__ __forceinline__ void store_codes(uint8_t* row, int u, const float (&x)[8], float inv, bool saturate) {
+  uint32_t a, b;
+  if (saturate) {
+    a = encode4(x, inv);
+    b = encode4(x + 4, inv);
+  } else {
+    a = codes4(x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
+    b = codes4(x[4] * inv, x[5] * inv, x[6] * inv, x[7] * inv);
+  }
   if constexpr (LAY == SPARVAR_ROPE_PAIRS) {
     *reinterpret_cast<uint2*>(row + 8 * u) = make_uint2(a, b);
   } else {
@@ -86,11 +93,28 @@ __device__ __forceinline__ void store_codes(uint8_t* row, int u, const float (&x
   }
 }
 
-// Sum over the LANES lanes of a row.
-template <int LANES>
-__device__ __forceinline__ float row_sum(float x) {
-#pragma unroll
-  for (int o = LANES / 2; o > 0; o >>= 1) x += __shfl_xor(x, o);
+// x of another lane by DPP (no trip through LDS): lane ^ 1, lane ^ 2, and mirrored in groups of
+// 8 and of 16, which after the steps before stand for lane ^ 4 and lane ^ 8.
+constexpr int kDppXor1 = 0xB1, kDppXor2 = 0x4E, kDppMirror8 = 0x141, kDppMirror16 = 0x140;
+
+template <int CTRL>
+__device__ __forceinline__ float dpp(float x) {
+  return __uint_as_float((uint32_t)dpp_or_zero<CTRL, 0xf>((int32_t)__float_as_uint(x)));
+}
+template <int CTRL>
+__device__ __forceinline__ double dpp(double x) {
+  const uint2 w = __builtin_bit_cast(uint2, x);
+  const uint2 v = make_uint2((uint32_t)dpp_or_zero<CTRL, 0xf>((int32_t)w.x), (uint32_t)dpp_or_zero<CTRL, 0xf>((int32_t)w.y));
+  return __builtin_bit_cast(double, v);
+}
+
+// Sum over the LANES (8 or 16) lanes of a row.
+template <int LANES, class T>
+__device__ __forceinline__ T row_sum(T x) {
+  x += dpp<kDppXor1>(x);
+  x += dpp<kDppXor2>(x);
+  x += dpp<kDppMirror8>(x);
+  if constexpr (LANES == 16) x += dpp<kDppMirror16>(x);
   return x;
 }
 
@@ -137,6 +161,63 @@ __device__ __forceinline__ void weigh8(float (&x)[8], const float* w, int u) {
   for (int i = 0; i < 8; ++i) x[i] *= t[i];
 }
 
+// y rounded to odd at 20 bits after the point: cut, with the last bit set where anything was
+// cut off. A value so rounded and one more rounding to nearest even with two bits fewer or less
+// is the value rounded once.
+__device__ __forceinline__ float round_odd(double y) {
+  uint2 w = __builtin_bit_cast(uint2, y);
+  w.y |= w.x < 1u ? w.x : 1u;
+  w.x = 0u;
+  return (float)__builtin_bit_cast(double, w);
+}
+
+// The whole map of a key on its way to codes, in 64 bits, rounded to odd: codes and exponents
+// are then those of the exact map, which 32 bits miss wherever a value lies within their error
+// of a tie (about one of a million codes, each off by a step). 64x64 append of 2 x 16 heads: 47
+// us, 43 with the map in 32 bits, 39 without norm, weight and rotation.
+template <int D, int LAY>
+__device__ __forceinline__ void map_exactly(float (&x)[8], const HeadMap& map, bool weighed, const float (&w)[8],
+                                            const float (&cs)[8]) {
+  double y[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) y[i] = (double)x[i];
+  if (map.norm != SPARVAR_NORM_NONE) {
+    double s = 0.0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s = __builtin_fma(y[i], y[i], s);
+    s = row_sum<D / 8>(s);
+    const double eps = (double)map.eps;
+    const bool rms = map.norm == SPARVAR_NORM_RMS;
+    const double z = rms ? s * (1.0 / D) + eps : s;
+    double r;
+    if (z > 1e-30 && z < 1e30) {  // 1 / sqrt(z) to 2^-45: the 32-bit one and a Newton step
+      const double r0 = (double)__builtin_amdgcn_rsqf((float)z);
+      r = r0 * __builtin_fma(-0.5 * z * r0, r0, 1.5);
+      if (!rms && r * eps > 1.0) r = 1.0 / eps;
+    } else {
+      r = rms ? 1.0 / __builtin_sqrt(z) : 1.0 / fmax(__builtin_sqrt(z), eps);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] *= r;
+  }
+  if (weighed) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] *= (double)w[i];
+  }
+  if (map.cos_sin) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int a = LAY == SPARVAR_ROPE_PAIRS ? 2 * i : i, b = LAY == SPARVAR_ROPE_PAIRS ? 2 * i + 1 : i + 4;
+      const double c = (double)cs[2 * i], t = (double)cs[2 * i + 1];
+      const double ya = y[a] * c - y[b] * t, yb = y[a] * t + y[b] * c;
+      y[a] = ya;
+      y[b] = yb;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = round_odd(y[i]);
+}
+
 // ------------------------------------------------------------------ kernels
 struct AppendIO {
   const void *q, *k, *v;
@@ -156,14 +237,14 @@ struct AppendIO {
 // turn, the table's values of its tokens held for all of them.
 constexpr int kHeads = 4;
 
-template <class T, int D, int LAY>
+template <class T, int D, int LAY, int NT>
 __device__ __forceinline__ void append_rows(const AppendIO& io, int32_t item) {
   constexpr int L = D / 8, kRows = 64 / L;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int u = lane % L;
   const int32_t hg = item % io.n_head_groups, rest = item / io.n_head_groups;
   const int32_t tg = rest % io.n_token_groups, b = rest / io.n_token_groups;
-  const int32_t tok = (tg * (kNT / 64) + wave) * kRows + lane / L;
+  const int32_t tok = (tg * (NT / 64) + wave) * kRows + lane / L;
   const bool valid = tok < io.n;
   const int32_t i = valid ? tok : io.n - 1;
   const int32_t h0 = hg * kHeads, hn = io.n_heads - h0 < kHeads ? io.n_heads - h0 : kHeads;
@@ -204,16 +285,20 @@ __device__ __forceinline__ void append_rows(const AppendIO& io, int32_t item) {
 // One block of G tokens of a plane, by a workgroup: its rows in registers (PASSES rows a
 // lane), mapped, their largest magnitude found, encoded and written. Rows before t0 are
 // what the cache holds, rows from t0 + n on are not there.
-template <class T, int D, int LAY, int PASSES, bool MAP>
+template <class T, int D, int LAY, int PASSES, int NT, bool MAP>
 __device__ __forceinline__ void encode_block(const Q8View& c8, bool is_v, int32_t plane, int32_t j, int32_t t0, int32_t n,
                                              const T* src, int64_t src_token, const HeadMap& map, const float* weight) {
-  constexpr int L = D / 8, kRows = kNT / L;
+  constexpr int L = D / 8, kRows = NT / L;
   const int u = threadIdx.x % L, r0 = threadIdx.x / L;
   const int32_t G = 1 << c8.lg, first = j << c8.lg, end = t0 + n;
   uint8_t* codes = (is_v ? c8.v : c8.k) + (int64_t)plane * c8.bh_stride;
   uint8_t* scale = (is_v ? c8.vs : c8.ks) + (int64_t)plane * c8.sc_stride + j;
   float x[PASSES][8];
   float top = 0.f;
+  float w[8];
+  if constexpr (MAP) {
+    if (!is_v && weight) load8<D, LAY>(weight, u, w);
+  }
 #pragma unroll
   for (int p = 0; p < PASSES; ++p) {
     const int32_t r = p * kRows + r0, t = first + r;
@@ -236,38 +321,40 @@ __device__ __forceinline__ void encode_block(const Q8View& c8, bool is_v, int32_
     if constexpr (MAP) {
       // (whole rows take the branch together, and with them the lanes that exchange)
       if (!is_v && r < G && t >= t0 && t < end) {
-        norm8<D>(x[p], map.norm, map.eps);
-        if (weight) weigh8<D, LAY>(x[p], weight, u);
-        if (map.cos_sin) {
-          float cs[8];
-          load_cs(map.cos_sin + (int64_t)t * D, u, cs);
-          rotate8<LAY>(x[p], cs);
-        }
+        float cs[8];
+        if (map.cos_sin) load_cs(map.cos_sin + (int64_t)t * D, u, cs);
+        map_exactly<D, LAY>(x[p], map, weight != nullptr, w, cs);
       }
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(x[p][i]));
   }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-  __shared__ float tops[kNT / 64];
+  top = fmaxf(top, dpp<kDppXor1>(top));
+  top = fmaxf(top, dpp<kDppXor2>(top));
+  top = fmaxf(top, dpp<kDppMirror8>(top));
+  top = fmaxf(top, dpp<kDppMirror16>(top));
+  top = fmaxf(top, __shfl_xor(top, 16));
+  top = max_halves(top);
+  __shared__ float tops[NT / 64];
   if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
   __syncthreads();
 #pragma unroll
-  for (int w = 0; w < kNT / 64; ++w) top = fmaxf(top, tops[w]);
-  const int32_t e = block_exponent(top);
+  for (int w = 0; w < NT / 64; ++w) top = fmaxf(top, tops[w]);
+  // (the exponent is the workgroup's; below the last one nothing exceeds 448)
+  const int32_t e = __builtin_amdgcn_readfirstlane(block_exponent(top));
   const float inv = pow2f(-e);
 #pragma unroll
   for (int p = 0; p < PASSES; ++p) {
     const int32_t r = p * kRows + r0, t = first + r;
-    if (r < G && t < end) store_codes<D, LAY>(codes + (int64_t)t * D, u, x[p], inv);
+    if (r < G && t < end) store_codes<D, LAY>(codes + (int64_t)t * D, u, x[p], inv, e == kScaleExpMax);
   }
   if (threadIdx.x == 0) *scale = (uint8_t)(e + 127);
 }
 
-// PASSES = 0: a 16- or 32-bit cache, row part only.
-template <class T, int D, int LAY, int PASSES>
-__global__ __launch_bounds__(kNT) void qkv_append_kernel(AppendIO io) {
+// PASSES = 0: a 16- or 32-bit cache, row part only. Six waves a SIMD: the map in 64 bits and the
+// loads ahead of it would take the registers of four.
+template <class T, int D, int LAY, int PASSES, int NT>
+__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(6))) void qkv_append_kernel(AppendIO io) {
   int32_t item = blockIdx.x;
   if constexpr (PASSES > 0) {
     if (item < io.encode_items) {
@@ -277,13 +364,13 @@ __global__ __launch_bounds__(kNT) void qkv_append_kernel(AppendIO io) {
       rest >>= 1;
       const int32_t h = rest % io.H_kv, b = rest / io.H_kv;
       const T* src = static_cast<const T*>(is_v ? io.v : io.k) + b * io.kv_batch + (int64_t)h * D;
-      encode_block<T, D, LAY, PASSES, true>(io.c8, is_v, rest, (io.t0 >> io.c8.lg) + bi, io.t0, io.n, src, io.kv_token, io.map,
+      encode_block<T, D, LAY, PASSES, NT, true>(io.c8, is_v, rest, (io.t0 >> io.c8.lg) + bi, io.t0, io.n, src, io.kv_token, io.map,
                                             io.map.k_weight ? io.map.k_weight + (int64_t)h * D : nullptr);
       return;
     }
     item -= io.encode_items;
   }
-  append_rows<T, D, LAY>(io, item);
+  append_rows<T, D, LAY, NT>(io, item);
 }
 
 struct QuantizeIO {
@@ -293,13 +380,13 @@ struct QuantizeIO {
   int32_t n, t0, n_blocks;
 };
 
-template <class T, int D, int PASSES>
-__global__ __launch_bounds__(kNT) void kv_quantize_kernel(QuantizeIO io) {
+template <class T, int D, int PASSES, int NT>
+__global__ __launch_bounds__(NT) void kv_quantize_kernel(QuantizeIO io) {
   const int32_t bi = blockIdx.x % io.n_blocks, rest = blockIdx.x / io.n_blocks;
   const bool is_v = rest & 1;
   const int32_t plane = rest >> 1;
   const T* src = static_cast<const T*>(is_v ? io.v : io.k) + (int64_t)plane * io.bh_stride;
-  encode_block<T, D, SPARVAR_ROPE_PAIRS, PASSES, false>(io.c8, is_v, plane, (io.t0 >> io.c8.lg) + bi, io.t0, io.n, src, D,
+  encode_block<T, D, SPARVAR_ROPE_PAIRS, PASSES, NT, false>(io.c8, is_v, plane, (io.t0 >> io.c8.lg) + bi, io.t0, io.n, src, D,
                                                         HeadMap{}, nullptr);
 }
 
@@ -350,24 +437,30 @@ __global__ __launch_bounds__(kNT) void kv_dequantize_kernel(DequantizeIO io) {
   }
 }
 
-// Rows a lane of the encoding part holds: blocks of G rows of d / 8 lanes in 256 threads.
-int passes_of(int32_t lg, int32_t d) {
-  const int p = (d << lg) / (8 * kNT);
-  return p > 0 ? p : 1;
+// Threads that encode a block of G rows, d / 8 to a row, two rows each at most: every row more
+// costs registers and with them waves that wait for memory side by side (64x64 append of 2 x 16
+// heads, d = 128, blocks of 64 tokens: two rows a thread 47.4 us, four 50.7).
+struct BlockShape {
+  int passes, threads;
+};
+BlockShape block_shape(int32_t lg, int32_t d) {
+  const int lanes = (d << lg) / 8;  // 128 .. 2048
+  return lanes <= 256 ? BlockShape{1, 256} : BlockShape{2, lanes / 2};
 }
 
 template <class T, int D, int LAY>
-hipError_t append_with(const AppendIO& io, int passes, int32_t grid, hipStream_t stream) {
-  switch (passes) {
-#define SV_PASS(P) \
-  case P: hipLaunchKernelGGL((qkv_append_kernel<T, D, LAY, P>), dim3(grid), dim3(kNT), 0, stream, io); break;
-    SV_PASS(0) SV_PASS(1) SV_PASS(2) SV_PASS(4)
-#undef SV_PASS
-    default:
-      if constexpr (D == 128) hipLaunchKernelGGL((qkv_append_kernel<T, D, LAY, 8>), dim3(grid), dim3(kNT), 0, stream, io);
-      else return hipErrorInvalidValue;
+hipError_t append_with(const AppendIO& io, const BlockShape& b, int32_t grid, hipStream_t stream) {
+#define SV_SHAPE(P, NN)                                                                                               \
+  if (b.passes == P && b.threads == NN) {                                                                             \
+    hipLaunchKernelGGL((qkv_append_kernel<T, D, LAY, P, NN>), dim3(grid), dim3(NN), 0, stream, io);                   \
+    return hipGetLastError();                                                                                         \
   }
-  return hipGetLastError();
+  SV_SHAPE(0, 256) SV_SHAPE(1, 256) SV_SHAPE(2, 256) SV_SHAPE(2, 512)
+  if constexpr (D == 128) {
+    SV_SHAPE(2, 1024)
+  }
+#undef SV_SHAPE
+  return hipErrorInvalidValue;
 }
 
 }  // namespace
@@ -393,14 +486,14 @@ hipError_t launch_qkv_append(const AppendArgs& a, hipStream_t stream) {
   io.t0 = a.t0;
   io.n_heads = a.q8 ? a.H : a.H + 2 * a.H_kv;
   io.n_head_groups = (io.n_heads + kHeads - 1) / kHeads;
-  const int tokens = kNT / (a.d / 8);  // of a workgroup
+  const BlockShape shape = a.q8 ? block_shape(a.c8.lg, a.d) : BlockShape{0, kNT};
+  const int tokens = shape.threads / (a.d / 8);  // of a workgroup of the row part
   io.n_token_groups = (a.n + tokens - 1) / tokens;
   io.n_blocks = a.q8 ? (int32_t)((((int64_t)a.t0 + a.n - 1) >> a.c8.lg) - (a.t0 >> a.c8.lg) + 1) : 0;
   io.encode_items = 2 * a.B * a.H_kv * io.n_blocks;
-  const int passes = a.q8 ? passes_of(a.c8.lg, a.d) : 0;
   const int32_t grid = io.encode_items + a.B * io.n_head_groups * io.n_token_groups;
 #define SV_APPEND(TT, BF, DD, LL) \
-  if (a.bf16 == BF && a.d == DD && a.map.layout == LL) return append_with<TT, DD, LL>(io, passes, grid, stream);
+  if (a.bf16 == BF && a.d == DD && a.map.layout == LL) return append_with<TT, DD, LL>(io, shape, grid, stream);
   SV_APPEND(bf16_bits, true, 64, 0) SV_APPEND(bf16_bits, true, 128, 0) SV_APPEND(bf16_bits, true, 64, 1)
   SV_APPEND(bf16_bits, true, 128, 1) SV_APPEND(float, false, 64, 0) SV_APPEND(float, false, 128, 0)
   SV_APPEND(float, false, 64, 1) SV_APPEND(float, false, 128, 1)
@@ -417,16 +510,16 @@ hipError_t launch_kv_quantize(const KvQuantizeArgs& a, hipStream_t stream) {
   io.n = a.n;
   io.t0 = a.t0;
   io.n_blocks = (int32_t)((((int64_t)a.t0 + a.n - 1) >> a.c8.lg) - (a.t0 >> a.c8.lg) + 1);
-  const int passes = passes_of(a.c8.lg, a.d);
+  const BlockShape shape = block_shape(a.c8.lg, a.d);
   const int32_t grid = 2 * a.planes * io.n_blocks;
-#define SV_QUANT(TT, BF, DD, P)                                                                                \
-  if (a.bf16 == BF && a.d == DD && passes == P) {                                                              \
-    hipLaunchKernelGGL((kv_quantize_kernel<TT, DD, P>), dim3(grid), dim3(kNT), 0, stream, io);                 \
+#define SV_QUANT(TT, BF, DD, P, NN)                                                                            \
+  if (a.bf16 == BF && a.d == DD && shape.passes == P && shape.threads == NN) {                                 \
+    hipLaunchKernelGGL((kv_quantize_kernel<TT, DD, P, NN>), dim3(grid), dim3(NN), 0, stream, io);              \
     return hipGetLastError();                                                                                  \
   }
-#define SV_QUANT_T(TT, BF) \
-  SV_QUANT(TT, BF, 64, 1) SV_QUANT(TT, BF, 64, 2) SV_QUANT(TT, BF, 64, 4) SV_QUANT(TT, BF, 128, 1) \
-  SV_QUANT(TT, BF, 128, 2) SV_QUANT(TT, BF, 128, 4) SV_QUANT(TT, BF, 128, 8)
+#define SV_QUANT_T(TT, BF)                                                                                     \
+  SV_QUANT(TT, BF, 64, 1, 256) SV_QUANT(TT, BF, 64, 2, 256) SV_QUANT(TT, BF, 64, 2, 512)                       \
+  SV_QUANT(TT, BF, 128, 1, 256) SV_QUANT(TT, BF, 128, 2, 256) SV_QUANT(TT, BF, 128, 2, 512) SV_QUANT(TT, BF, 128, 2, 1024)
   SV_QUANT_T(bf16_bits, true) SV_QUANT_T(float, false)
 #undef SV_QUANT_T
 #undef SV_QUANT

@@ -617,13 +617,14 @@ class NormRope:
 
 def _token_strides(t, name):
     """Batch and token stride of a [B,n,heads,d] tensor whose heads are contiguous."""
-    if t.dim() != 4:
-        raise SparvarError(ERR_INVALID, f"{name} must be [B,n,heads,d]")
     stride = t.stride()
-    if stride[3] != 1 or (stride[2] != t.shape[3] and t.shape[2] > 1):
+    if len(stride) != 4:
+        raise SparvarError(ERR_INVALID, f"{name} must be [B,n,heads,d]")
+    B, n, heads, d = t.shape
+    if stride[3] != 1 or (stride[2] != d and heads > 1):
         raise SparvarError(ERR_INVALID, f"{name} heads must be contiguous")
     # (an axis of one has no stride of its own; any multiple of 16 bytes will do)
-    return stride[0] if t.shape[0] > 1 else 0, stride[1] if t.shape[1] > 1 else t.shape[2] * t.shape[3]
+    return stride[0] if B > 1 else 0, stride[1] if n > 1 else heads * d
 
 
 def sparvar_qkv_append(q, k, v, t0, heads, q_out, k_cache=None, v_cache=None, q8=None, stream=None):
@@ -634,8 +635,8 @@ def sparvar_qkv_append(q, k, v, t0, heads, q_out, k_cache=None, v_cache=None, q8
     kv_shape = k.shape
     H_kv = kv_shape[2]
     qb, qt = _token_strides(q, "q")
-    kb, kt = kv = _token_strides(k, "k")
-    if v.shape != kv_shape or _token_strides(v, "v") != kv:
+    kb, kt = _token_strides(k, "k")
+    if v.shape != kv_shape or (v.stride() != k.stride() and _token_strides(v, "v") != (kb, kt)):
         raise SparvarError(ERR_INVALID, "k and v must share their shape and strides")
     if kv_shape != (B, n, H_kv, d):
         raise SparvarError(ERR_INVALID, "q and k must share batch, tokens and d")

@@ -1,6 +1,6 @@
 """GPU parity of the append (norms, rotation), of the 8-bit cache as it is written and of its way back, through the C ABI,
-against the fp64 oracle. Codes and scales are bit-exact where their inputs are given, and within the rounding of the 32-bit
-norm and rotation before them otherwise."""
+against the fp64 oracle. Codes and scales are bit-exact; queries and 16- or 32-bit caches are within the rounding of the
+32-bit norm and rotation."""
 import numpy as np
 import pytest
 import torch
@@ -229,18 +229,10 @@ def test_append(case, to8):
             v8, e8 = before[0][1][b, h].copy(), before[1][1][b, h].copy()
             O.append_codes(v8, e8, xv[b, :, h], t0, G)  # values are only encoded: exact
             assert np.array_equal(exps[1][b, h, :nb], e8[:nb]) and np.array_equal(codes[1][b, h, :t0 + n], v8[:t0 + n])
-            # keys: the nearest code of something within the map's bound of y, at the exponent of such a maximum
-            y = mapped(xk, b, h, ww[1])
-            off = map_bound(y, layout, turn)
+            # keys are mapped in 64 bits and rounded once
             k8, e8 = before[0][0][b, h].copy(), before[1][0][b, h].copy()
-            lo, hi = e8.copy(), e8.copy()
-            O.append_codes(k8.copy(), lo, np.sign(y) * np.maximum(np.abs(y) - off, 0), t0, G)
-            O.append_codes(k8.copy(), hi, np.sign(y) * (np.abs(y) + off), t0, G)
-            e = exps[0][b, h]
-            assert (lo[:nb] <= e[:nb]).all() and (e[:nb] <= hi[:nb]).all()
-            step = 2.0 ** e[np.arange(t0, t0 + n) // G][:, None]
-            z = O.cache_values(codes[0][b, h], e, G)[t0:t0 + n]
-            assert (np.abs(z - y) <= np.maximum(2.0 ** -4 * np.abs(y), 2.0 ** -10 * step) * 1.001 + 2 * off).all(), (b, h)
+            O.append_codes(k8, e8, mapped(xk, b, h, ww[1]), t0, G)
+            assert np.array_equal(exps[0][b, h, :nb], e8[:nb]) and np.array_equal(codes[0][b, h, :t0 + n], k8[:t0 + n])
 
 
 def test_norm_of_zero_rows():
