@@ -509,7 +509,8 @@ int sparvar_kv_compact(const sparvar_geometry_t* g, int32_t n_keep, const int32_
  * with the values its tokens before t0 hold and the new ones: its exponent may
  * grow, which only moves codes towards the subnormals of the format. Tokens from
  * t0 + n on in the last block are not counted and their codes stay as they were
- * (their values change with the block's scale): append in ascending order.
+ * (their values change with the block's scale): append in ascending order. Calls
+ * that write one cache, or read what another writes, are ordered by the caller.
  *
  * The struct is host memory read during the call; k, v and the scales are device
  * memory. H_kv planes a batch entry; a call's H (query heads) is a multiple of
@@ -549,8 +550,8 @@ typedef struct sparvar_norm_rope {
  *   (y_a, y_b) -> (y_a cos - y_b sin, y_a sin + y_b cos) for every pair of the
  *   layout, with cos and sin of row t0 + i of the table;
  * for queries (to q_out) and keys (to cache token t0 + i); values are copied. In
- * 32 bits from the inputs on, rounded once, to the output's type or to the codes
- * of an 8-bit cache.
+ * 32 bits from the inputs on (keys on their way to codes in 64), rounded once, to
+ * the output's type or to the codes of an 8-bit cache.
  *   q: [B,n,H,d], k, v: [B,n,H_kv,d] of `dtype`, the layout of a fused
  *   projection: heads contiguous, tokens and batch entries at strides of their
  *   own (elements, multiples of 16 bytes; k and v share theirs).
@@ -587,8 +588,8 @@ int sparvar_kv_dequantize(int32_t B, int32_t H_kv, int32_t d, sparvar_dtype_t dt
 /*
  * Dense attention over the first n_kv tokens of an 8-bit cache: the definition
  * of sparvar_dense_attn_fwd on the values that the codes stand for (bf16 only).
- *   q: [B,H,n_q,d] (plane stride q_bh_stride); o: [B,H,n_q,d] contiguous;
- *   lse (nullable): [B,H,n_q] fp32.
+ *   q: [B,H,n_q,d] (plane stride q_bh_stride), magnitudes below 2^120; o:
+ *   [B,H,n_q,d] contiguous; lse (nullable): [B,H,n_q] fp32.
  *   kv_len (nullable): device int32 [B]; entry b attends to its first
  *   min(max(kv_len[b], 0), n_kv) tokens. With none, o = 0 and lse = -inf.
  *   workspace (nullable, 16-byte aligned): workspace_bytes of device memory, at
@@ -610,7 +611,8 @@ int sparvar_dense_attn_q8_fwd(int32_t B, int32_t H, int32_t H_kv, int32_t n_q, i
 /*
  * sparvar_block_sparse_attn_fwd over an 8-bit cache (bf16 queries and outputs):
  * the same rows, launch orders of rows and outputs, on the values that the codes
- * stand for. CSR rows stay per query head; an order of groups is not used.
+ * stand for, queries' magnitudes below 2^120. CSR rows stay per query head; an
+ * order of groups is not used.
  */
 int sparvar_block_sparse_attn_q8_fwd(const sparvar_geometry_t* g, int32_t k, int32_t B, int32_t H,
                                      int32_t H_kv, int32_t d, sparvar_dtype_t dtype, const void* q_k,

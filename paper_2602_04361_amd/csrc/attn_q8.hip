@@ -1,15 +1,20 @@
 // Attention over an 8-bit cache: dense, and block-sparse over CSR rows.
 //
 // The walk is that of the bf16 kernels (attention.hip): S^T = K Q^T, softmax in the exp2
-// domain with a running maximum, O^T += V^T P^T, on 32x32x16 bf16 MFMA with K and V chunks
-// staged in LDS. Codes become bf16 on their way to LDS, once a workgroup: e4m3 has 4
-// significant bits and scales are powers of two, so code * 2^e is exact in bf16 and the
-// conversion (one instruction for two values, the scale its operand) rounds nothing. The
-// products are then those of a 16-bit cache holding the same values.
+// domain with a running maximum, O^T += V^T P^T. With K = c 2^e (codes c of e4m3, a
+// power-of-two scale a block of tokens) S = sum c 2^e q runs on the codes themselves: the
+// 32x32x64 8-bit MFMA takes a scale byte a row, and Q goes in as the sum of two e4m3 values
+// (QFragF8), at the same rate as one bf16 product. V becomes bf16 on its way to LDS, once a
+// workgroup: c 2^e has 4 significant bits, so the conversion (one instruction for two values,
+// the scale its operand) rounds nothing, and O is the bf16 product that a 16-bit cache of the
+// same values would have. A lane loads 16 or 32 codes of V of one token, so of one scale.
 //
-// A step of the pipeline: chunk i sits in one LDS stage while chunk i + 1, loaded to
-// registers a step ago, is converted into the other and the loads of chunk i + 2 are
-// issued; one barrier a chunk. A lane loads 16 codes (of one token, so one scale) at a time.
+// Large calls are bound by the matrix cores and the softmax's VALU work, which share the clock
+// that power allows: 4096 x 10521, 2 x 16 heads, d = 128: 585-620 us, 1.14-1.21 PFLOP/s, where a
+// large bf16 matrix product reaches 1.23-1.34; MFMA busy 53% of the cycles at 2.0 GHz, no bank
+// conflicts. (With K converted to bf16 in LDS as well 633-677 us; that kernel with its waves in
+// two groups a phase apart, products beside softmax, 597-612, this one so 575: not kept.) Few
+// rows against a long cache are bound by memory: 4.8 TB/s.
 #include "attn_chunk.h"
 #include "attn_sources.h"
 #include "q8.h"
@@ -27,7 +32,6 @@ struct Q8IO {
   int32_t o_rows;   // rows of an output plane
   int32_t n_items;  // workgroups doing work
   int32_t swizzle;
-  int32_t group;    // query heads a key head
   float scale_log2;
   float* part_o;    // dense calls in parts: [part, row, D] unnormalised sums, and
   float2* part_ml;  // [part, row] maximum (exp2 domain) and sum
@@ -72,8 +76,7 @@ struct DenseQ8Src {
   }
 };
 
-template <int KC>
-struct SparseQ8Src : SparseSrc<KC> {
+struct SparseQ8Src : SparseSrc<64> {
   int32_t group;
   __device__ __forceinline__ int32_t part_of(int32_t) const { return 0; }
   __device__ __forceinline__ int32_t kv_plane(const QuerySet& s) const { return s.bh / group; }
@@ -135,11 +138,12 @@ __device__ __forceinline__ void store_rows(const Q8IO& io, const f32x16 (&acc)[D
 }
 
 // Query fragments for the products with K's codes: the row divided by a power of two (its
-// largest magnitude at most 448) as the sum of two e4m3 values. bf16 has 8 significant bits and
-// e4m3 4, so the sum is the query itself for every element down to 2^-10 of the row's largest,
-// and within 2^-18 of the largest below: the scores are those of exact products, at the matrix
-// rate of bf16 (two e4m3 products at twice its rate), and K needs no conversion. Step t of a
-// half covers channels 64 t + 32 half .. + 32, as the K fragments do.
+// largest magnitude then in (224, 448]) as the sum of two e4m3 values. bf16 has 8 significant
+// bits and e4m3 4, so the sum is the query itself for elements from 2^-9 of the row's largest
+// on; below, the smaller part ends at the format's last place, 2^-9, and is off by at most half
+// of it: 2^-10 / 224 < 2^-17 of the largest. The rate is that of one bf16 product (two e4m3
+// ones at twice its rate), and K needs no conversion. Step t of a half covers channels
+// 64 t + 32 half .. + 32, as the K fragments do.
 typedef __attribute__((ext_vector_type(8))) int i32x8;
 
 template <int D>
@@ -168,8 +172,8 @@ struct QFragF8 {
 #pragma unroll
       for (int w = 0; w < 8; ++w) {
         const uint32_t a = raw[4 * t + w / 2][2 * (w & 1)], b = raw[4 * t + w / 2][2 * (w & 1) + 1];
-        const float x[4] = {__uint_as_float(a << 16) * inv, __uint_as_float(a & 0xffff0000u) * inv, __uint_as_float(b << 16) * inv,
-                            __uint_as_float(b & 0xffff0000u) * inv};
+        const float x[4] = {__uint_as_float(a << 16) * inv, __uint_as_float(a & 0xffff0000u) * inv,
+                            __uint_as_float(b << 16) * inv, __uint_as_float(b & 0xffff0000u) * inv};
         const uint32_t h = codes4(x[0], x[1], x[2], x[3]);
         float y[4];
         decode4(h, 1.f, y);
@@ -243,8 +247,11 @@ __device__ __forceinline__ void softmax_chunk(f32x16 (&st)[KC / 32], int32_t cou
   l_run += exp_pack<KC>(st, scale_log2, m_run, pf);
 }
 
-// QW waves of 32 queries walk the keys, or (KS > 1) KS such sets, each a part of them with LDS
-// of its own, joined at the end.
+// QW waves of 32 queries walk the keys in chunks of 64, or (KS > 1) KS such sets, each a part of
+// them with LDS of its own, joined at the end. While a chunk is computed, the next one's K is
+// copied to the other K tile and its V loaded to registers, to be converted into the one V tile
+// between two barriers: with one V tile four workgroups of two waves fit a CU's LDS, where two
+// tiles leave two (block-sparse 64x64, d = 128: 141 against 171 us, both with K converted).
 template <int D, int QW, int KS, class Src>
 __global__ __launch_bounds__(QW * KS * 64) __attribute__((amdgpu_waves_per_eu(2))) void attn_q8_kernel(Q8IO io, Src src) {
   constexpr int KC = 64, NT = QW * KS * 64;
@@ -463,12 +470,15 @@ __global__ __launch_bounds__(QW * KS * 64) __attribute__((amdgpu_waves_per_eu(2)
   store_rows<D>(io, acc, m_run, l_tot, qvalid, half, plane, qrow, src.part_of(item));
 }
 
-// Few rows against a long cache (single tokens, a token a query head): memory bound, so
-// every wave walks chunks of 32 keys by itself, without barriers, its next chunk's codes in
-// flight. Its K codes go from registers to the products (a lane holds half of a key's
-// channels: the sum over channels may run in any order, so step s takes channels 8 s .. of
-// each half); V goes through a piece of LDS of the wave's own, for the transposing read.
-// The four waves of a workgroup take every fourth chunk of a part and join at the end.
+// Few rows (single tokens against a long cache, a token a query head; early scales): bound by
+// memory or latency, so every wave walks chunks of 32 keys by itself, without barriers, its next
+// chunk's codes in flight. K goes from registers to the products (converted: splitting the
+// queries in two would take longer than a short walk saves, 64 x 121 keys 5.8 against 7.4 us):
+// a lane holds half of a key's channels, and as a sum over channels may run in any order, step
+// s takes channels 8 s .. of each half. V goes through a piece of LDS of the wave's own, for the
+// transposing read. The four waves of a workgroup take every fourth chunk of a part and join
+// at the end. One token of 4 x 32 heads, up to 42521 keys of 8 heads: 58.5 us, 4.8 TB/s (a large
+// copy reaches 4.8); by the 64-key kernel with parts 91 us.
 constexpr int kRowWaves = 4;
 
 // LDS of one wave, written by some lanes and read by others: its instructions run in
@@ -624,7 +634,8 @@ void attn_q8_rows_kernel(Q8IO io, DenseQ8Src<32> src) {
 
 // Joins the parts of a row: a workgroup's threads are D / 4 channel groups times
 // 1024 / D groups of parts; the groups are added in order through LDS. A part without
-// keys has no sum and its values are not read.
+// keys has no sum and its values are not read (a NaN sum is one: its row is NaN in every form).
+// Latency: the token case's 16 parts of 128 rows are 1 MB, 5 us with the launch.
 template <int D>
 __global__ __launch_bounds__(256) void join_parts_kernel(Q8IO io, int32_t parts) {
   constexpr int C = D / 4, P = 256 / C;
@@ -641,7 +652,7 @@ __global__ __launch_bounds__(256) void join_parts_kernel(Q8IO io, int32_t parts)
   for (int p = g; p < parts; p += P) {
     const int64_t prow = (int64_t)p * io.rows + row;
     const float2 ml = io.part_ml[prow];
-    if (!(ml.y > 0.f)) continue;
+    if (ml.y == 0.f) continue;
     const float f = __builtin_amdgcn_exp2f(ml.x - m);
     const float4 a = *reinterpret_cast<const float4*>(io.part_o + prow * D + 4 * c);
     l += ml.y * f;
@@ -681,8 +692,8 @@ struct DenseQ8Plan {
 
 // Expected time of a form, in us. With m workgroups on the busiest CU, which share it: f0 + f m
 // for starting and storing, and for every 64 keys of a part a + c m; at least what the codes
-// take at 5 TB/s, more where CUs idle in the last round and where few workgroups leave a tail. Parts cost a second
-// launch, some time each and their way through memory. f, a and c are fits to 256 m
+// take at 5 TB/s, more where CUs idle in the last round and where few workgroups leave a tail.
+// Parts cost a second launch, some time each and their way through memory. f, a and c are fits to 256 m
 // workgroups, m = 1 .. 6, of 512 and 4608 keys and to the scales of an image; measured at d =
 // 128, us by the forms with few, 4 and 8 waves: 2 x 16 heads, 256 x 521 keys 9.1 / 15.6 / 22.5,
 // 400 x 921 16.8 / 21.7 / 31.4, 1024 x 2521 64 / 49.6 / 70, 1600 x 4121 158 / 119.7 / 115.2,
@@ -755,7 +766,6 @@ hipError_t launch_dense_attn_q8(const DenseQ8Args& a, hipStream_t stream) {
   io.o_rows = a.n_q;
   io.n_items = a.B * a.H_kv * p.slabs * p.parts;
   io.swizzle = a.swizzle;
-  io.group = group;
   io.scale_log2 = a.softmax_scale * kLog2e;
   io.rows = a.B * a.H * a.n_q;
   io.part_o = p.parts > 1 ? a.workspace : nullptr;
@@ -803,13 +813,12 @@ hipError_t launch_sparse_attn_q8(const SparseQ8Args& a, hipStream_t stream) {
   io.o_rows = G.h[a.k - 1] * G.w[a.k - 1];
   io.n_items = a.BH * G_k * slabs;
   io.swizzle = a.swizzle;
-  io.group = a.H / a.H_kv;
   io.scale_log2 = a.softmax_scale * kLog2e;
   io.part_o = nullptr;
   io.part_ml = nullptr;
   io.rows = a.BH * io.o_rows;
-  SparseQ8Src<64> src;
-  src.group = io.group;
+  SparseQ8Src src;
+  src.group = a.H / a.H_kv;
   src.max_chunks_per_block = max_chunks_per_block(G, a.k, 64);
   src.G = G;
   src.row_ptr = a.row_ptr;

@@ -155,7 +155,6 @@ struct AppendArgs {
   int64_t cache_bh_stride;
   bool q8;
   Q8View c8;
-  int num_cu;
 };
 hipError_t launch_qkv_append(const AppendArgs& a, hipStream_t stream);
 

@@ -247,6 +247,32 @@ def test_norm_of_zero_rows():
         assert (qo == 0).all() and (q8.k == 0).all() and (q8.k_scale == 27).all()
 
 
+@pytest.mark.parametrize("norm,eps", [("l2", 1e-12), ("rms", 1e-6), (None, 0.0)])
+def test_a_nan_stays_in_its_row(norm, eps):
+    """A NaN makes its row NaN under a norm, itself alone without one, and does not count for its block's exponent."""
+    note(f"[append] NaN under {norm}")
+    r = np.random.default_rng(5)
+    x = r.standard_normal((1, 20, 3, 64)).astype(np.float32)
+    x[0, 3, :, 17] = np.nan
+    t = torch.from_numpy(x).cuda()
+    q8, qo = fresh(1, 1, 20, 64, 16), torch.full((1, 1, 20, 64), 9.0, device="cuda")
+    q, k, v = t.split([1, 1, 1], 2)
+    sv.sparvar_qkv_append(q, k, v, 0, sv.NormRope(norm, eps), qo, q8=q8)
+    torch.cuda.synchronize()
+    codes, exps = codes_and_exps(q8)
+    y = [O.norm_rope(x[0, :, 0], norm, float(np.float32(eps)), None, None, "pairs"),
+         O.norm_rope(x[0, :, 1], norm, float(np.float32(eps)), None, None, "pairs"), x[0, :, 2].astype(np.float64)]
+    got = qo[0, 0].double().cpu().numpy()
+    assert np.array_equal(np.isnan(got), np.isnan(y[0]))
+    assert np.isnan(got[3]).sum() == (1 if norm is None else 64)
+    ok = ~np.isnan(y[0])
+    assert (np.abs(got - y[0])[ok] <= (U32 * 1.001 * np.abs(y[0]) + map_bound(y[0], "pairs", False))[ok]).all()
+    for w in range(2):
+        c, e = np.zeros((20, 64)), np.zeros(2, dtype=np.int64)
+        O.append_codes(c, e, y[w + 1], 0, 16)
+        assert np.array_equal(exps[w][0, 0], e) and np.array_equal(codes[w][0, 0], c, equal_nan=True)
+
+
 def test_planes_far_apart():
     """Planes of codes more than 2^32 bytes apart."""
     note("[q8] planes 5 GB apart")
