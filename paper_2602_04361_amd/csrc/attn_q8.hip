@@ -197,11 +197,12 @@ __device__ __forceinline__ i32x8 two_units(u32x4 a, u32x4 b) {
   return i32x8{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b[0], (int)b[1], (int)b[2], (int)b[3]};
 }
 
-// K codes in LDS: rows of D bytes, 16-byte unit u of row r at u ^ code_swizzle(r): the same unit
-// of eight neighbouring rows lies in eight different groups of banks.
+// K codes in LDS: rows of D bytes, 16-byte unit u of row r at u ^ code_swizzle(r): two or four
+// rows fill the 256 bytes of the banks, and the same unit of sixteen neighbouring rows lies in
+// sixteen different places of them.
 template <int D>
 __device__ __forceinline__ int code_swizzle(int r) {
-  return D == 128 ? r & 7 : (r >> 1) & 3;
+  return D == 128 ? (r >> 1) & 7 : (r >> 2) & 3;
 }
 
 // V^T fragment of step ks2, channels 32 dt .. of a V tile (rows of D bf16 values).
