@@ -268,12 +268,9 @@ __global__ __launch_bounds__(QW * KS * 64) __attribute__((amdgpu_waves_per_eu(2)
   static_assert(kHalf ? QW * 16 == 2 * KC : KC % (QW * 16) == 0, "V rows must split evenly");
   static_assert(KC * U8 % ((kHalf ? QW / 2 : QW) * 64) == 0, "K units must split evenly");
   static_assert(KS == 1 || Src::kSparse, "parts of a table's walk");
-  // (the parts' outputs go through the V tiles when they join: KS (KS - 1) QW pieces of D / 2 / KS x 64 floats)
-  constexpr int kJoin = KS > 1 ? (KS - 1) * QW * D * 128 / KS : 0;
-  constexpr int kStage = kVTile > kJoin ? kVTile : kJoin;
   __shared__ __attribute__((aligned(16))) char ktile0[KS][kKTile];
   __shared__ __attribute__((aligned(16))) char ktile1[KS][kKTile];
-  __shared__ __attribute__((aligned(16))) char vtiles[KS][kStage];
+  __shared__ __attribute__((aligned(16))) char vtiles[KS][kVTile];
   __shared__ __attribute__((aligned(16))) char tsmem[Src::template table_bytes<NT>()];
 
   const int32_t item = swizzled_item(blockIdx.x, gridDim.x, io.swizzle);
@@ -452,8 +449,9 @@ __global__ __launch_bounds__(QW * KS * 64) __attribute__((amdgpu_waves_per_eu(2)
   if constexpr (KS > 1) {
     __shared__ float ml[KS][QW * kQPerWave][2];
     float m_g, l_g, out[D / 2 / KS];
-    merge_key_splits<D, QW, KS, KS * kStage / 2>(acc, m_run, l_run, split, wave, lane, vtiles[0], vtiles[0] + KS * kStage / 2,
-                                                 ml, m_g, l_g, out);
+    // (through the V tiles and the first K tiles)
+    merge_key_splits<D, QW, KS, KS * kVTile, KS * kKTile>(acc, m_run, l_run, split, wave, lane, vtiles[0], ktile0[0], ml, m_g,
+                                                          l_g, out);
     if (!qvalid) return;
     const float inv = l_g > 0.f ? 1.f / l_g : 0.f;
     const int64_t orow = (int64_t)plane * io.o_rows + qrow;
@@ -832,14 +830,18 @@ hipError_t launch_sparse_attn_q8(const SparseQ8Args& a, hipStream_t stream) {
   src.n_rows = a.BH * G_k;
   // Tiles of 33 to 64 queries (8 x 8): launches of few waves a SIMD walk their rows in two parts
   // (8 heads of a 64 x 64 scale, 512 workgroups: d = 128 37.2 against 45.8 us, d = 64 25.0 /
-  // 32.4; 12 heads, 768: 53.9 / 48.8 and 31.6 / 34; 800: d = 64 36.9 / 35.6), d = 64 in four up
-  // to one workgroup a CU (128 workgroups: 17.0 against 18.5).
+  // 32.4; 12 heads, 768: 53.9 / 48.8 and 31.6 / 34; 800: d = 64 36.9 / 35.6), up to one workgroup
+  // a CU in four, where the cache is long enough for rows that give back what the join costs
+  // (256 workgroups, 10521 tokens: d = 128 26.8 in four against 29.2, d = 64 19.8 / 21.7; 921
+  // tokens 24.7 / 25.8 and 17.9 / 19.3; 521: 18.9 / 18.8 and 13.8 / 14.3; 265: 17.1 / 15.4 and
+  // 12.4 / 11.9; past one workgroup a CU, 512: 48.3 / 38.6 and 35.0 / 28.2).
   int ks = 1;
-  if (nw == 2 && io.n_items <= (a.d == 64 ? 3 : 2) * a.num_cu) ks = a.d == 64 && io.n_items <= a.num_cu ? 4 : 2;
+  if (nw == 2 && io.n_items <= (a.d == 64 ? 3 : 2) * a.num_cu)
+    ks = io.n_items <= a.num_cu && G.C[a.k] >= (a.d == 64 ? 384 : 640) ? 4 : 2;
 #define SV_SPARSE(DD, NN, KK) \
   if (a.d == DD && nw == NN && ks == KK) return launch_one<DD, NN, KK>(io, src, stream);
   SV_SPARSE(64, 1, 1) SV_SPARSE(64, 2, 1) SV_SPARSE(64, 2, 2) SV_SPARSE(64, 2, 4) SV_SPARSE(64, 4, 1) SV_SPARSE(64, 8, 1)
-  SV_SPARSE(128, 1, 1) SV_SPARSE(128, 2, 1) SV_SPARSE(128, 2, 2) SV_SPARSE(128, 4, 1) SV_SPARSE(128, 8, 1)
+  SV_SPARSE(128, 1, 1) SV_SPARSE(128, 2, 1) SV_SPARSE(128, 2, 2) SV_SPARSE(128, 2, 4) SV_SPARSE(128, 4, 1) SV_SPARSE(128, 8, 1)
 #undef SV_SPARSE
   return hipErrorInvalidValue;
 }

@@ -874,9 +874,9 @@ constexpr float kNoMax = -3.402823466e38f;
 // Merge of KS key splits of one workgroup (QW query waves each): the softmax maximum
 // m_g and sum l_g over the splits, and in out the unnormalised sums of the accumulator
 // registers [split R, (split + 1) R) (16 per 32-channel group, R = D / 2 / KS) that
-// this wave finishes, added in split order. The other splits hand theirs over through the stage arrays s0 and s1 of SB
-// bytes each, which every wave has finished with by the first barrier.
-template <int D, int QW, int KS, int SB>
+// this wave finishes, added in split order. The other splits hand theirs over through the stage
+// arrays s0 of SB and s1 of SB1 bytes, which every wave has finished with by the first barrier.
+template <int D, int QW, int KS, int SB, int SB1 = SB>
 __device__ __forceinline__ void merge_key_splits(const f32x16 (&acc)[D / 32], float m_run, float l_run, int split,
                                                  int qwave, int lane, char* s0, char* s1,
                                                  float (&ml)[KS][QW * kQPerWave][2], float& m_g, float& l_g,
@@ -885,7 +885,7 @@ __device__ __forceinline__ void merge_key_splits(const f32x16 (&acc)[D / 32], fl
   constexpr int kPart = R * 64;  // floats one wave hands to one other split
   constexpr int kHalf = SB / (kPart * 4);
   static_assert(R % 4 == 0, "output channels must split into groups of four");
-  static_assert(KS * (KS - 1) * QW <= 2 * kHalf, "split outputs must fit the stages they merge through");
+  static_assert(KS * (KS - 1) * QW <= kHalf + SB1 / (kPart * 4), "split outputs must fit the stages they merge through");
   const int slot = qwave * kQPerWave + (lane & 31);
   const float l_tot = sum_halves(l_run);
   if (lane < 32) {

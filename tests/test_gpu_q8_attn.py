@@ -272,7 +272,9 @@ def run_sparse(h, w, b, k, B, H, Hkv, d, G, seed, empty=(), order=False, dup=Non
     ([2, 9, 13], [2, 9, 13], 3, 3, 1, 2, 2, 64, 16), ([40], [70], 33, 1, 1, 1, 1, 64, 64),
     ([1, 4, 30], [1, 4, 30], 8, 3, 2, 20, 20, 64, 64), ([1, 4, 30], [1, 4, 30], 8, 3, 2, 20, 20, 128, 64),  # one part a row
     ([1, 4, 30], [1, 4, 30], 8, 3, 1, 20, 20, 64, 64), ([1, 4, 30], [1, 4, 30], 5, 3, 1, 2, 2, 128, 16),
-    ([1, 70], [1, 70], 64, 2, 1, 1, 1, 128, 64)])                   # tile rows of a whole chunk
+    ([1, 70], [1, 70], 64, 2, 1, 1, 1, 128, 64),                    # tile rows of a whole chunk
+    ([1, 2, 4, 8, 16, 29], [1, 2, 4, 8, 16, 25], 8, 6, 1, 4, 2, 128, 64),  # rows in four parts, edges of 5 and 1
+    ([1, 2, 4, 8, 16, 25], [1, 2, 4, 8, 16, 29], 8, 6, 1, 3, 3, 64, 16)])
 @pytest.mark.parametrize("order", [False, True])
 def test_sparse(h, w, b, k, B, H, Hkv, d, G, order):
     note(f"[q8 sparse] h={h} w={w} b={b} k={k} B={B} H={H}/{Hkv} d={d} G={G} order={order}")
