@@ -10,11 +10,11 @@
 // same values would have. A lane loads 16 or 32 codes of V of one token, so of one scale.
 //
 // Large calls are bound by the matrix cores and the softmax's VALU work, which share the clock
-// that power allows: 4096 x 10521, 2 x 16 heads, d = 128: 585-620 us, 1.14-1.21 PFLOP/s, where a
-// large bf16 matrix product reaches 1.23-1.34; MFMA busy 53% of the cycles at 2.0 GHz, no bank
-// conflicts. (With K converted to bf16 in LDS as well 633-677 us; that kernel with its waves in
-// two groups a phase apart, products beside softmax, 597-612, this one so 575: not kept.) Few
-// rows against a long cache are bound by memory: 4.8 TB/s.
+// that power allows: 4096 x 10521, 2 x 16 heads, d = 128: 559-592 us, 1.19-1.26 PFLOP/s, where a
+// large bf16 matrix product reaches 1.23-1.34; MFMA busy 57% of the cycles, no bank conflicts.
+// (With K converted to bf16 in LDS as well 633-677 us; with the waves in two groups a phase
+// apart, products beside softmax, 575 where this one takes 592: not kept.) Few rows against a
+// long cache are bound by memory: 4.8 TB/s.
 #include "attn_chunk.h"
 #include "attn_sources.h"
 #include "q8.h"
