@@ -364,7 +364,7 @@ int check_dense_q8(int32_t B, int32_t H, int32_t H_kv, int32_t n_q, int32_t n_kv
   if (st) return st;
   if ((st = check_heads(B, H, H_kv))) return st;
   if (n_q < 1 || n_kv < 1) return fail(SPARVAR_ERR_INVALID, "n_q and n_kv must be >= 1");
-  // (the parts of a call are at most 64 and only taken by calls of few rows)
+  // (parts are taken by calls of few workgroups only, at most eight a CU)
   if ((int64_t)B * H * n_q >= (int64_t(1) << 31)) return fail(SPARVAR_ERR_INVALID, "B*H*n_q too large");
   return SPARVAR_OK;
 }

@@ -235,6 +235,30 @@ def test_append(case, to8):
             assert np.array_equal(exps[0][b, h, :nb], e8[:nb]) and np.array_equal(codes[0][b, h, :t0 + n], k8[:t0 + n])
 
 
+@pytest.mark.parametrize("to8", [False, True])
+def test_tokens_first(to8):
+    """Projections of tokens first, [n, B, heads, d] seen as [B, n, heads, d]: the same bytes as batch first."""
+    note(f"[append] tokens first, to8={to8}")
+    B, n, H, Hkv, d, t0 = 3, 37, 4, 2, 128, 11
+    x = torch.randn(n, B, H + 2 * Hkv, d, device="cuda").bfloat16()
+    heads = sv.NormRope("rms", 1e-6, cos_sin=torch.randn(t0 + n, d // 2, 2, device="cuda"))
+    got = []
+    for y in (x.transpose(0, 1), x.transpose(0, 1).contiguous()):
+        q, k, v = y.split([H, Hkv, Hkv], 2)
+        qo = torch.full((B, H, n, d), 9.0, device="cuda").bfloat16()
+        if to8:
+            q8 = fresh(B, Hkv, t0 + n, d, 32)
+            sv.sparvar_qkv_append(q, k, v, t0, heads, qo, q8=q8)
+            got.append([qo] + [t.clone().view(torch.uint8) for t in (q8.k, q8.v, q8.k_scale, q8.v_scale)])
+        else:
+            kc, vc = (torch.full((B, Hkv, t0 + n, d), 9.0, device="cuda").bfloat16() for _ in range(2))
+            sv.sparvar_qkv_append(q, k, v, t0, heads, qo, kc, vc)
+            got.append([qo, kc, vc])
+    torch.cuda.synchronize()
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
+
+
 def test_norm_of_zero_rows():
     """Rows of zeros: L2 divides by eps, RMS by its root; both give zeros, and a block of them the smallest exponent."""
     note("[append] zero rows")
