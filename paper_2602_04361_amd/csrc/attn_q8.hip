@@ -76,8 +76,149 @@ struct DenseQ8Src {
   }
 };
 
+// Chunks of a CSR row whose blocks are packed: the row's tokens, block after block, cut every 64.
+// A block cut at its scale's edge (24 tokens of an 8 x 8 block, say) then takes no more room in a
+// chunk than it has tokens, where the block table of the bf16 kernels gives it a chunk: block
+// sparse 48 x 36, d = 64, 83% of whose table's slots held a token, 30.5 -> 27.5 us, 32 x 18 with
+// 54% 15.7 -> 12.5, 64 x 64 with 98% the same (121). tok is the token of the lane's slot (the
+// last one's past count).
+struct PackedChunk {
+  uint32_t tok;
+  int32_t count;
+};
+
+// Token of slot base + step, base the lane's and step the same for all: as one instruction, so that
+// no register holds a slot (base is taken again at each load: the compiler would keep every sum).
+__device__ __forceinline__ int32_t slot_base(const Chunk&, int32_t slot) { return slot; }
+__device__ __forceinline__ uint32_t token_at(const Chunk& c, int32_t base, int32_t step) {
+  return (uint32_t)chunk_token(c, chunk_slot(base + step, c.count));
+}
+__device__ __forceinline__ int32_t slot_base(const PackedChunk&, int32_t slot) {
+  int32_t b = slot * 4;
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile("" : "+v"(b));
+#endif
+  return b;
+}
+__device__ __forceinline__ uint32_t token_at(const PackedChunk& c, int32_t base, int32_t step) {
+  return (uint32_t)__builtin_amdgcn_ds_bpermute(base + step * 4, (int32_t)c.tok);
+}
+
+// Where the blocks of a fill stand: for each that has tokens {first token, first position,
+// width of its scale << 8 | its own width, ceil(2^20 / its width)}, and the positions apart.
+template <int NT>
+struct PackedLds {  // byte offsets
+  static constexpr int kInfo = 0;
+  static constexpr int kStart = kInfo + NT * 16;
+  static constexpr int kWt = kStart + (NT + 1) * 4 + 12;
+  static constexpr int kGeo = kWt + 16 * 4;
+  static constexpr int kBytes = kGeo + (int)((sizeof(GeoTable) + 15) / 16 * 16);
+};
+
+template <int NT>
+struct PackedCursor {
+  using L = PackedLds<NT>;
+  static constexpr int kGroup = NT < 512 ? NT : 511;  // entries of a fill: their count in 9 bits, their tokens in 22
+  const int32_t* col;
+  int32_t nb, pos, end;       // ids below nb are blocks; entries of the row not yet decoded
+  int32_t n, total;           // blocks and tokens of this fill
+  int32_t blk, at, stop;      // block of the wave's next position, that position, the end of its part
+  char* lds;
+
+  __device__ __forceinline__ bool more() const { return pos < end; }
+
+  // Decodes the next kGroup entries, a thread each (false: none left). Entries that are no blocks
+  // are left out, so that no two blocks share a position.
+  __device__ __forceinline__ bool fill() {
+    int4* info = reinterpret_cast<int4*>(lds + L::kInfo);
+    int32_t* start = reinterpret_cast<int32_t*>(lds + L::kStart);
+    const GeoTable& G = *reinterpret_cast<const GeoTable*>(lds + L::kGeo);
+    const int tid = fresh_tid();
+    total = 0;
+    while (pos < end && total == 0) {
+      __syncthreads();
+      const int32_t v = tid < kGroup && pos + tid < end ? col[pos + tid] : -1;
+      Tile t{0, 0, 1, 1};
+      if (v >= 0 && v < nb) t = block_tile(G, v);
+      const int32_t size = t.nr * t.nc;  // at most 4096
+      int32_t sum;
+      const int32_t before = block_excl_scan<NT>(size > 0 ? 1 << 22 | size : 0, reinterpret_cast<int32_t*>(lds + L::kWt), sum);
+      n = __builtin_amdgcn_readfirstlane((uint32_t)sum >> 22);
+      total = __builtin_amdgcn_readfirstlane(sum & 0x3fffff);
+      // (last blocks first: the full blocks of late scales then begin on a chunk's first slot, and
+      // most chunks hold one; 64 x 64 127 us with the few tokens of the first scales in front)
+      if (size > 0) {
+        const int32_t i = n - 1 - (before >> 22), first = total - size - (before & 0x3fffff);
+        info[i] = make_int4(t.base, first, t.stride << 8 | t.nc, ((1 << 20) + t.nc - 1) / t.nc);
+        start[i] = first;
+      }
+      if (tid == 0) start[n] = total;
+      __syncthreads();
+      pos += kGroup;
+    }
+    blk = 0;
+    at = 0;
+    stop = total;
+    return total > 0;
+  }
+
+  // Restricts the walk to part s of ks; returns the chunks of the longest part.
+  __device__ __forceinline__ int32_t take_split(int s, int ks) {
+    const int32_t* start = reinterpret_cast<const int32_t*>(lds + L::kStart);
+    const int32_t per = ((total + 63) / 64 + ks - 1) / ks;
+    at = s * per * 64;
+    stop = at + per * 64 < total ? at + per * 64 : total;
+    if (at < total) {
+      int32_t upto = 0;
+      for (int32_t i = 0; i < n; i += 64) {
+        const int32_t j = i + (fresh_tid() & 63);
+        upto += __builtin_popcountll(__builtin_amdgcn_ballot_w64(j < n && start[j < n ? j : n] <= at));
+      }
+      blk = upto - 1;
+    }
+    return per;
+  }
+
+  __device__ __forceinline__ bool next(PackedChunk& c) {
+    if (at >= stop) return false;
+    const int lane = fresh_tid() & 63;
+    const int4* info = reinterpret_cast<const int4*>(lds + L::kInfo);
+    const int32_t* start = reinterpret_cast<const int32_t*>(lds + L::kStart);
+    c.count = stop - at < 64 ? stop - at : 64;
+    // the blocks that begin inside the chunk, at most 63
+    const int32_t s = start[blk + 1 + lane < n ? blk + 1 + lane : n];
+    const int32_t inside = __builtin_popcountll(__builtin_amdgcn_ballot_w64(blk + 1 + lane < n && s < at + c.count));
+    int32_t own = blk;
+    for (int32_t i = 0; i < inside; ++i) own += at + lane >= __builtin_amdgcn_readlane(s, i) ? 1 : 0;
+    const int4 b = info[own];
+    const uint32_t r = (uint32_t)(at + lane - b.y);
+    const uint32_t q = __umul24(r, (uint32_t)b.w) >> 20;  // r / width: r < 4096, width <= 64
+    c.tok = (uint32_t)b.x + r + __umul24(q, (uint32_t)((b.z >> 8) - (b.z & 0xff)));
+    if (c.count < 64) c.tok = lane < c.count ? c.tok : (uint32_t)__builtin_amdgcn_readlane(c.tok, c.count - 1);
+    at += 64;
+    blk += inside + (__builtin_amdgcn_readlane(s, inside) <= at && blk + 1 + inside < n ? 1 : 0);
+    return true;
+  }
+};
+
 struct SparseQ8Src : SparseSrc<64> {
   int32_t group;
+  template <int NT>
+  static constexpr int table_bytes() { return PackedLds<NT>::kBytes; }
+  template <int NT>
+  __device__ __forceinline__ PackedCursor<NT> packed_cursor(int32_t item, char* lds) const {
+    const int32_t r = row_of(item);
+    PackedCursor<NT> c;
+    constexpr int kWords = (int)(sizeof(GeoTable) / 4);
+    const int32_t* from = reinterpret_cast<const int32_t*>(&G);  // (the first fill starts with a barrier)
+    for (int i = threadIdx.x; i < kWords; i += NT) reinterpret_cast<int32_t*>(lds + PackedLds<NT>::kGeo)[i] = from[i];
+    c.col = col_idx;
+    c.nb = G.NB[k];
+    c.pos = row_ptr[r];
+    c.end = row_ptr[r + 1];
+    c.lds = lds;
+    return c;
+  }
   __device__ __forceinline__ int32_t part_of(int32_t) const { return 0; }
   __device__ __forceinline__ int32_t kv_plane(const QuerySet& s) const { return s.bh / group; }
   __device__ __forceinline__ void place(const QuerySet& s, int32_t i, int32_t& plane, int32_t& row) const {
@@ -327,28 +468,35 @@ __global__ __launch_bounds__(QW * KS * 64) __attribute__((amdgpu_waves_per_eu(2)
 
   u32x4 raw[kVSteps][kPieces];
   uint32_t raw_s[kVSteps], k_scale[KC / 32], k_scale_next[KC / 32];
-  auto load = [&](const Chunk& c, char* kdst) {
+  auto load = [&](const auto& c, char* kdst) {
     if (does_k) {
+      const int32_t base = slot_base(c, k_row);
 #pragma unroll
       for (int j = 0; j < kKSteps; ++j) {
         const int r = k_row + j * (64 / U8);
-        const uint32_t tok = (uint32_t)chunk_token(c, chunk_slot(r, c.count));
+        const uint32_t tok = token_at(c, base, j * (64 / U8));
         dma16(kp + (tok * D + 16 * (k_unit ^ code_swizzle<D>(r))), kdst + (k_first + j * 64) * 16);
       }
     }
     if (does_v) {
+      const int32_t base = slot_base(c, vrow);
 #pragma unroll
       for (int j = 0; j < kVSteps; ++j) {
-        const uint32_t tok = (uint32_t)chunk_token(c, chunk_slot(vrow + j * QW * 16, c.count));
+        const uint32_t tok = token_at(c, base, j * QW * 16);
 #pragma unroll
         for (int p = 0; p < kPieces; ++p)
           raw[j][p] = *reinterpret_cast<const u32x4*>(vp + (tok * D + 16 * vcol + 64 * p));
         raw_s[j] = vsp[tok >> io.c.lg];
       }
     }
+    if constexpr (Src::kSparse) {  // (the tokens of slots l32 and 32 + l32)
+      const auto t = __builtin_amdgcn_permlane32_swap(c.tok, c.tok, false, false);
+      k_scale_next[0] = ksp[(uint32_t)t[0] >> io.c.lg];
+      k_scale_next[1] = ksp[(uint32_t)t[1] >> io.c.lg];
+    } else {
 #pragma unroll
-    for (int kt = 0; kt < KC / 32; ++kt)
-      k_scale_next[kt] = ksp[(uint32_t)chunk_token(c, chunk_slot(32 * kt + l32, c.count)) >> io.c.lg];
+      for (int kt = 0; kt < KC / 32; ++kt) k_scale_next[kt] = ksp[token_at(c, l32, 32 * kt) >> io.c.lg];
+    }
   };
   // The chunk loaded last becomes the one to be computed: V to LDS, K's copies arrived.
   auto take = [&]() {
@@ -400,7 +548,7 @@ __global__ __launch_bounds__(QW * KS * 64) __attribute__((amdgpu_waves_per_eu(2)
   };
 
   auto cur = [&]() {
-    if constexpr (Src::kSparse) return src.template table_cursor<NT>(item, tsmem);
+    if constexpr (Src::kSparse) return src.template packed_cursor<NT>(item, tsmem);
     else return src.cursor(item, qs);
   }();
   // One pass over what the cursor holds, or over the set's part of it (a block table is filled
@@ -409,7 +557,7 @@ __global__ __launch_bounds__(QW * KS * 64) __attribute__((amdgpu_waves_per_eu(2)
   auto walk = [&]() {
     int32_t steps = 0;
     if constexpr (KS > 1) steps = cur.take_split(split, KS);
-    Chunk c0;
+    std::conditional_t<Src::kSparse, PackedChunk, Chunk> c0;
     bool have = cur.next(c0);
     if (KS == 1 && !have) return;
     if (have) load(c0, ktile0[split]);
@@ -818,7 +966,7 @@ hipError_t launch_sparse_attn_q8(const SparseQ8Args& a, hipStream_t stream) {
   io.rows = a.BH * io.o_rows;
   SparseQ8Src src;
   src.group = a.H / a.H_kv;
-  src.max_chunks_per_block = max_chunks_per_block(G, a.k, 64);
+  src.max_chunks_per_block = 0;  // (of the block tables, which these kernels do not use)
   src.G = G;
   src.row_ptr = a.row_ptr;
   src.col_idx = a.col_idx;
@@ -829,15 +977,15 @@ hipError_t launch_sparse_attn_q8(const SparseQ8Args& a, hipStream_t stream) {
   src.slabs = slabs;
   src.n_rows = a.BH * G_k;
   // Tiles of 33 to 64 queries (8 x 8): launches of few waves a SIMD walk their rows in two parts
-  // (8 heads of a 64 x 64 scale, 512 workgroups: d = 128 37.2 against 45.8 us, d = 64 25.0 /
-  // 32.4; 12 heads, 768: 53.9 / 48.8 and 31.6 / 34; 800: d = 64 36.9 / 35.6), up to one workgroup
-  // a CU in four, where the cache is long enough for rows that give back what the join costs
-  // (256 workgroups, 10521 tokens: d = 128 26.8 in four against 29.2, d = 64 19.8 / 21.7; 921
-  // tokens 24.7 / 25.8 and 17.9 / 19.3; 521: 18.9 / 18.8 and 13.8 / 14.3; 265: 17.1 / 15.4 and
-  // 12.4 / 11.9; past one workgroup a CU, 512: 48.3 / 38.6 and 35.0 / 28.2).
+  // (64 x 64 scale, d = 128: 512 workgroups 39.0 us against 50.7, 640 57.0 / 53.6; d = 64: 512
+  // 27.5 / 38.4, 768 33.9 / 39.7, 896 44.1 / 42.3; past that within 8% of each other, with the
+  // rounds that either makes), up to one workgroup a CU in four, where the cache is long enough
+  // for rows that give back what the join costs (256 workgroups, 10521 tokens: d = 128 26.9 in
+  // four against 29.4, d = 64 18.8 / 21.1; 921 tokens 20.9 / 21.1 and 14.2 / 15.1; 521 17.4 /
+  // 16.3 and 12.2 / 12.0; past one workgroup a CU, 320: 47.6 / 38.1 and 32.9 / 26.6).
   int ks = 1;
   if (nw == 2 && io.n_items <= (a.d == 64 ? 3 : 2) * a.num_cu)
-    ks = io.n_items <= a.num_cu && G.C[a.k] >= (a.d == 64 ? 384 : 640) ? 4 : 2;
+    ks = io.n_items <= a.num_cu && G.C[a.k] >= 640 ? 4 : 2;
 #define SV_SPARSE(DD, NN, KK) \
   if (a.d == DD && nw == NN && ks == KK) return launch_one<DD, NN, KK>(io, src, stream);
   SV_SPARSE(64, 1, 1) SV_SPARSE(64, 2, 1) SV_SPARSE(64, 2, 2) SV_SPARSE(64, 2, 4) SV_SPARSE(64, 4, 1) SV_SPARSE(64, 8, 1)

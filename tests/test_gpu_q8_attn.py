@@ -231,7 +231,7 @@ def test_scores_that_spread():
 
 
 # ------------------------------------------------------------------------------------------------ block-sparse
-def run_sparse(h, w, b, k, B, H, Hkv, d, G, seed, empty=(), order=False, dup=None):
+def run_sparse(h, w, b, k, B, H, Hkv, d, G, seed, empty=(), order=False):
     og, g = O.Geometry(h, w, b, 1), sv.Geometry(h, w, b, 1)
     n = og.C(k)
     q8, kk, vv = make_cache(B, Hkv, n, d, G, seed, cap=n + 9)
@@ -274,7 +274,8 @@ def run_sparse(h, w, b, k, B, H, Hkv, d, G, seed, empty=(), order=False, dup=Non
     ([1, 4, 30], [1, 4, 30], 8, 3, 1, 20, 20, 64, 64), ([1, 4, 30], [1, 4, 30], 5, 3, 1, 2, 2, 128, 16),
     ([1, 70], [1, 70], 64, 2, 1, 1, 1, 128, 64),                    # tile rows of a whole chunk
     ([1, 2, 4, 8, 16, 29], [1, 2, 4, 8, 16, 25], 8, 6, 1, 4, 2, 128, 64),  # rows in four parts, edges of 5 and 1
-    ([1, 2, 4, 8, 16, 25], [1, 2, 4, 8, 16, 29], 8, 6, 1, 3, 3, 64, 16)])
+    ([1, 2, 4, 8, 16, 25], [1, 2, 4, 8, 16, 29], 8, 6, 1, 3, 3, 64, 16),
+    ([3, 12], [3, 12], 1, 2, 1, 1, 1, 64, 16), ([5, 9, 7], [1, 3, 2], 2, 3, 2, 2, 1, 128, 32)])  # blocks of one to four tokens
 @pytest.mark.parametrize("order", [False, True])
 def test_sparse(h, w, b, k, B, H, Hkv, d, G, order):
     note(f"[q8 sparse] h={h} w={w} b={b} k={k} B={B} H={H}/{Hkv} d={d} G={G} order={order}")
@@ -306,6 +307,26 @@ def test_sparse_long_rows():
     """More chunks than a table holds: 300 blocks a row, walked in several fills."""
     note("[q8 sparse] long rows")
     run_sparse([1, 36], [1, 36], 2, 2, 1, 1, 1, 64, 16, seed=9)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_sparse_long_rows_in_parts(d):
+    """A small scale after a large one: few tiles, so rows in four parts, and more blocks than a fill decodes."""
+    note(f"[q8 sparse] 534 blocks a row in parts, d={d}")
+    h, k = [1, 184, 16], 3
+    og, g = O.Geometry(h, h, 8, 1), sv.Geometry(h, h, 8, 1)
+    q8, kk, vv = make_cache(1, 1, og.C(k), d, 64, 17)
+    q = torch.randn(1, 1, og.N(k), d, device="cuda").bfloat16()
+    nb, G_k = og.nb_le(k), og.tiles(k)
+    assert nb == 534 and G_k == 4
+    ids = [list(range(nb)), list(range(20, nb)), [0, 533], list(range(0, nb, 2))]
+    ptr = np.cumsum([0] + [len(x) for x in ids])
+    rp, ci = torch.from_numpy(ptr.astype(np.int32)).cuda(), torch.tensor(sum(ids, []), dtype=torch.int32, device="cuda")
+    o, lse = torch.full_like(q, 5.0), torch.full((1, 1, og.N(k)), 5.0, device="cuda")
+    sv.sparvar_block_sparse_attn_q8_fwd(g, k, q, q8, o, rp, ci, lse=lse)
+    torch.cuda.synchronize()
+    check_rows(o[0, 0].double().cpu().numpy(), lse[0, 0].double().cpu().numpy(), q[0, 0].double().cpu().numpy(), kk[0, 0],
+               vv[0, 0], scale_of(d), mask=O.block_mask(og, k, ids))
 
 
 def test_every_block_is_dense():
