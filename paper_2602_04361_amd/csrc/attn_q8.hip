@@ -162,8 +162,7 @@ struct PackedCursor {
     return total > 0;
   }
 
-  // Restricts the walk to part s of ks; returns the chunks of the longest part.
-  __device__ __forceinline__ int32_t take_split(int s, int ks) {
+  __device__ __forceinline__ int32_t take_part(int s, int ks) {
     const int32_t* start = reinterpret_cast<const int32_t*>(lds + L::kStart);
     const int32_t per = ((total + 63) / 64 + ks - 1) / ks;
     at = s * per * 64;
@@ -200,6 +199,17 @@ struct PackedCursor {
     return true;
   }
 };
+
+// Restricts a walk to part s of ks; returns the chunks of the longest part.
+template <int NT>
+__device__ __forceinline__ int32_t take_part(PackedCursor<NT>& c, int s, int ks) { return c.take_part(s, ks); }
+template <int KC>
+__device__ __forceinline__ int32_t take_part(DenseCursor<KC>& c, int s, int ks) {
+  const int32_t chunks = c.n > c.pos ? (c.n - c.pos + KC - 1) / KC : 0, per = (chunks + ks - 1) / ks;
+  c.pos += s * per * KC;
+  c.n = c.pos + per * KC < c.n ? c.pos + per * KC : c.n;
+  return per;
+}
 
 struct SparseQ8Src : SparseSrc<64> {
   int32_t group;
@@ -390,7 +400,7 @@ __device__ __forceinline__ void softmax_chunk(f32x16 (&st)[KC / 32], int32_t cou
 }
 
 // QW waves of 32 queries walk the keys in chunks of 64, or (KS > 1) KS such sets, each a part of
-// them with LDS of its own, joined at the end. While a chunk is computed, the next one's K is
+// them with LDS of its own, joined through it at the end. While a chunk is computed, the next one's K is
 // copied to the other K tile and its V loaded to registers, to be converted into the one V tile
 // between two barriers: with one V tile four workgroups of two waves fit a CU's LDS, where two
 // tiles leave two (block-sparse 64x64, d = 128: 141 against 171 us, both with K converted).
@@ -408,10 +418,12 @@ __global__ __launch_bounds__(QW * KS * 64) __attribute__((amdgpu_waves_per_eu(2)
   constexpr int kKSteps = KC * U8 / ((kHalf ? QW / 2 : QW) * 64);
   static_assert(kHalf ? QW * 16 == 2 * KC : KC % (QW * 16) == 0, "V rows must split evenly");
   static_assert(KC * U8 % ((kHalf ? QW / 2 : QW) * 64) == 0, "K units must split evenly");
-  static_assert(KS == 1 || Src::kSparse, "parts of a table's walk");
+  // (sets hand their sums over through the V tiles and the first K tiles: KS (KS - 1) QW pieces)
+  constexpr int kJoin = KS > 1 ? (KS - 1) * QW * (D / 2 / KS) * 256 - kKTile : 0;
+  constexpr int kStage = kVTile > kJoin ? kVTile : kJoin;
   __shared__ __attribute__((aligned(16))) char ktile0[KS][kKTile];
   __shared__ __attribute__((aligned(16))) char ktile1[KS][kKTile];
-  __shared__ __attribute__((aligned(16))) char vtiles[KS][kVTile];
+  __shared__ __attribute__((aligned(16))) char vtiles[KS][kStage];
   __shared__ __attribute__((aligned(16))) char tsmem[Src::template table_bytes<NT>()];
 
   const int32_t item = swizzled_item(blockIdx.x, gridDim.x, io.swizzle);
@@ -556,7 +568,7 @@ __global__ __launch_bounds__(QW * KS * 64) __attribute__((amdgpu_waves_per_eu(2)
   // wave takes the steps of the longest part, and the barriers in them.
   auto walk = [&]() {
     int32_t steps = 0;
-    if constexpr (KS > 1) steps = cur.take_split(split, KS);
+    if constexpr (KS > 1) steps = take_part(cur, split, KS);
     std::conditional_t<Src::kSparse, PackedChunk, Chunk> c0;
     bool have = cur.next(c0);
     if (KS == 1 && !have) return;
@@ -597,8 +609,7 @@ __global__ __launch_bounds__(QW * KS * 64) __attribute__((amdgpu_waves_per_eu(2)
   if constexpr (KS > 1) {
     __shared__ float ml[KS][QW * kQPerWave][2];
     float m_g, l_g, out[D / 2 / KS];
-    // (through the V tiles and the first K tiles)
-    merge_key_splits<D, QW, KS, KS * kVTile, KS * kKTile>(acc, m_run, l_run, split, wave, lane, vtiles[0], ktile0[0], ml, m_g,
+    merge_key_splits<D, QW, KS, KS * kStage, KS * kKTile>(acc, m_run, l_run, split, wave, lane, vtiles[0], ktile0[0], ml, m_g,
                                                           l_g, out);
     if (!qvalid) return;
     const float inv = l_g > 0.f ? 1.f / l_g : 0.f;
@@ -779,48 +790,59 @@ void attn_q8_rows_kernel(Q8IO io, DenseQ8Src<32> src) {
   }
 }
 
-// Joins the parts of a row: a workgroup's threads are D / 4 channel groups times
-// 1024 / D groups of parts; the groups are added in order through LDS. A part without
-// keys has no sum and its values are not read (a NaN sum is one: its row is NaN in every form).
-// Latency: the token case's 16 parts of 128 rows are 1 MB, 5 us with the launch.
-template <int D>
+// Joins the parts of a row: D / 4 channel groups times `side` threads that take every side-th
+// part, added in order through LDS; a workgroup of 256 threads takes as many rows as that leaves.
+// A part without keys has no sum and its values do not count (a NaN sum is one: its row is NaN in
+// every form). Few parts of many rows go a thread a channel group (side = 1, memory bound); else
+// a row's parts go side by side (ALL: latency, the token case's 16 parts of 128 rows are 1 MB, 5
+// us with the launch). A whole call of 32768 rows of 64 channels in two parts takes 40 us that
+// way, 60 with a workgroup a row; 9040 rows in three 28.6 and 34.
+template <int D, bool ALL>
 __global__ __launch_bounds__(256) void join_parts_kernel(Q8IO io, int32_t parts) {
-  constexpr int C = D / 4, P = 256 / C;
-  __shared__ float4 sums[P][C];
+  constexpr int C = D / 4, P = 256 / C, side = ALL ? P : 1;
+  __shared__ float4 sums[ALL ? P : 1][C];
   __shared__ float ls[P];
-  const int32_t row = blockIdx.x;
   const int c = threadIdx.x % C, g = threadIdx.x / C;
+  const int32_t row = ALL ? (int32_t)blockIdx.x : (int32_t)blockIdx.x * P + g;
+  if (!ALL && row >= io.rows) return;
   float m = kNoMax;
-  for (int p = threadIdx.x & 63; p < parts; p += 64) m = fmaxf(m, io.part_ml[(int64_t)p * io.rows + row].x);
+  if constexpr (ALL) {
+    for (int p = threadIdx.x & 63; p < parts; p += 64) m = fmaxf(m, io.part_ml[(int64_t)p * io.rows + row].x);
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+  } else {
+    for (int p = 0; p < parts; ++p) m = fmaxf(m, io.part_ml[(int64_t)p * io.rows + row].x);
+  }
   float l = 0.f;
   float4 r = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int p = g; p < parts; p += P) {
+#pragma unroll 4
+  for (int p = ALL ? g : 0; p < parts; p += side) {
     const int64_t prow = (int64_t)p * io.rows + row;
     const float2 ml = io.part_ml[prow];
-    if (ml.y == 0.f) continue;
-    const float f = __builtin_amdgcn_exp2f(ml.x - m);
     const float4 a = *reinterpret_cast<const float4*>(io.part_o + prow * D + 4 * c);
-    l += ml.y * f;
-    r.x += a.x * f;
-    r.y += a.y * f;
-    r.z += a.z * f;
-    r.w += a.w * f;
+    const bool none = ml.y == 0.f;
+    const float f = __builtin_amdgcn_exp2f(ml.x - m);
+    l += none ? 0.f : ml.y * f;
+    r.x += none ? 0.f : a.x * f;
+    r.y += none ? 0.f : a.y * f;
+    r.z += none ? 0.f : a.z * f;
+    r.w += none ? 0.f : a.w * f;
   }
-  sums[g][c] = r;
-  if (c == 0) ls[g] = l;
-  __syncthreads();
-  if (g > 0) return;
-  l = 0.f;
-  r = make_float4(0.f, 0.f, 0.f, 0.f);
+  if constexpr (ALL) {
+    sums[g][c] = r;
+    if (c == 0) ls[g] = l;
+    __syncthreads();
+    if (g > 0) return;
+    l = 0.f;
+    r = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-  for (int i = 0; i < P; ++i) {
-    l += ls[i];
-    r.x += sums[i][c].x;
-    r.y += sums[i][c].y;
-    r.z += sums[i][c].z;
-    r.w += sums[i][c].w;
+    for (int i = 0; i < P; ++i) {
+      l += ls[i];
+      r.x += sums[i][c].x;
+      r.y += sums[i][c].y;
+      r.z += sums[i][c].z;
+      r.w += sums[i][c].w;
+    }
   }
   const float inv = l > 0.f ? 1.f / l : 0.f;
   uint2 w;
@@ -830,10 +852,18 @@ __global__ __launch_bounds__(256) void join_parts_kernel(Q8IO io, int32_t parts)
   if (io.lse && c == 0) io.lse[row] = l > 0.f ? (m + __builtin_log2f(l)) * kLn2 : -INFINITY;
 }
 
-// The form of a dense call: waves of a workgroup (0: the kernel for few rows, 32 rows a
-// workgroup), slabs of rows, parts of the keys.
+template <int D>
+hipError_t join_parts(const Q8IO& io, int32_t parts, int num_cu, hipStream_t stream) {
+  constexpr int P = 1024 / D;  // rows of a workgroup, or threads of a row's channel group
+  if (io.rows <= 8 * num_cu || parts > 8) hipLaunchKernelGGL((join_parts_kernel<D, true>), dim3(io.rows), dim3(256), 0, stream, io, parts);
+  else hipLaunchKernelGGL((join_parts_kernel<D, false>), dim3((io.rows + P - 1) / P), dim3(256), 0, stream, io, parts);
+  return hipGetLastError();
+}
+
+// The form of a dense call: waves of 32 rows in a workgroup (0: the kernel for few rows, 32 rows a
+// workgroup) and sets of them that share its keys, slabs of rows, parts of the keys.
 struct DenseQ8Plan {
-  int waves;
+  int waves, sets;
   int32_t slabs, parts;
 };
 
@@ -845,34 +875,38 @@ struct DenseQ8Plan {
 // 128, us by the forms with few, 4 and 8 waves: 2 x 16 heads, 256 x 521 keys 9.1 / 15.6 / 22.5,
 // 400 x 921 16.8 / 21.7 / 31.4, 1024 x 2521 64 / 49.6 / 70, 1600 x 4121 158 / 119.7 / 115.2,
 // 2304 x 6425 314 / 277 / 342, 4096 x 10521 - / 612 / 592; 8 heads, 1024 x 2521 21.3 / 46.8 /
-// 70. One token of 8 heads, 10521 keys of one head: 281 us in one part, 11.5 in 21, 13.7 in 83;
-// one token of 4 x 32 heads, up to 42521 keys of 8 heads: 76.8 in 8 parts, 58.4 in 16, 62.2 in 32.
+// 70. Two sets of four waves are for launches of up to a workgroup a CU, which then has two waves
+// a SIMD: against one set 256 workgroups of 10521 keys 160 / 174 (d = 64 104 / 124), 192 of 5575
+// 80.5 / 95, 256 of 2521 46.0 / 49.6; 384 workgroups 297 / 282. One token of 8 heads, 10521 keys
+// of one head: 281 us in one part, 11.5 in 21, 13.7 in 83; one token of 4 x 32 heads, up to 42521
+// keys of 8 heads: 76.8 in 8 parts, 58.4 in 16, 62.2 in 32.
 struct DenseForm {
-  int waves;
+  int waves, sets;
   float f0, f, a, c;
 };
-constexpr DenseForm kDenseForms[2][3] = {
-    {{0, 3.f, .6f, .05f, .20f}, {4, 3.f, 1.3f, .2f, .53f}, {8, 4.f, 4.4f, 0.f, 1.12f}},   // d = 64
-    {{0, 2.f, 2.2f, .15f, .35f}, {4, 3.5f, 3.f, .3f, .92f}, {8, 5.f, 6.f, 0.f, 1.77f}}};  // d = 128
+constexpr DenseForm kDenseForms[2][4] = {
+    // d = 64, d = 128
+    {{0, 1, 3.f, .6f, .05f, .20f}, {4, 1, 3.f, 1.3f, .2f, .53f}, {4, 2, 4.5f, 4.4f, 0.f, 1.15f}, {8, 1, 4.f, 4.4f, 0.f, 1.12f}},
+    {{0, 1, 2.f, 2.2f, .15f, .35f}, {4, 1, 3.5f, 3.f, .3f, .92f}, {4, 2, 5.5f, 6.f, 0.f, 1.8f}, {8, 1, 5.f, 6.f, 0.f, 1.77f}}};
 constexpr int kMostParts = 128;
 
 DenseQ8Plan dense_plan(int32_t planes, int32_t group, int32_t n_q, int32_t n_kv, int32_t d, int num_cu, bool may_split) {
   const int64_t rows = (int64_t)group * n_q, chunks = ((int64_t)n_kv + 63) / 64;
   const float memory = (float)planes * n_kv * d * (2.f / 5e6f);
-  DenseQ8Plan best{0, 1, 1};
+  DenseQ8Plan best{0, 1, 1, 1};
   float best_us = INFINITY;
   for (const DenseForm& f : kDenseForms[d == 128]) {
     const int64_t per = f.waves ? 32 * f.waves : 32, slabs = (rows + per - 1) / per, items = planes * slabs;
     auto consider = [&](int64_t parts) {
-      if (parts > 1 && (!may_split || parts > chunks || parts > kMostParts)) return;
+      if (parts > 1 && (!may_split || f.sets > 1 || parts > chunks || parts > kMostParts)) return;
       const float m = (float)((items * parts + num_cu - 1) / num_cu), even = (float)(items * parts) / (float)num_cu;
-      const float walk = (float)((chunks + parts - 1) / parts) * (f.a + f.c * m);
+      const float walk = (float)((chunks + parts * f.sets - 1) / (parts * f.sets)) * (f.a + f.c * m);
       const float read = memory * (m / even) * (1.f + .25f / m);
       float us = f.f0 + f.f * m + (walk > read ? walk : read);
       if (parts > 1) us += 3.f + .08f * parts + (float)parts * planes * rows * d * (8.f / 3e6f);
       if (us < best_us) {
         best_us = us;
-        best = DenseQ8Plan{f.waves, (int32_t)slabs, (int32_t)parts};
+        best = DenseQ8Plan{f.waves, f.sets, (int32_t)slabs, (int32_t)parts};
       }
     };
     // one part; growing numbers of parts while there is less than one workgroup a CU; whole
@@ -937,13 +971,15 @@ hipError_t launch_dense_attn_q8(const DenseQ8Args& a, hipStream_t stream) {
     e = hipGetLastError();
   } else {
     const DenseQ8Src<64> src = fill(DenseQ8Src<64>{});
-    if (a.d == 128) e = p.waves == 4 ? launch_one<128, 4, 1>(io, src, stream) : launch_one<128, 8, 1>(io, src, stream);
-    else e = p.waves == 4 ? launch_one<64, 4, 1>(io, src, stream) : launch_one<64, 8, 1>(io, src, stream);
+    if (a.d == 128)
+      e = p.waves == 8 ? launch_one<128, 8, 1>(io, src, stream)
+                       : (p.sets == 2 ? launch_one<128, 4, 2>(io, src, stream) : launch_one<128, 4, 1>(io, src, stream));
+    else
+      e = p.waves == 8 ? launch_one<64, 8, 1>(io, src, stream)
+                       : (p.sets == 2 ? launch_one<64, 4, 2>(io, src, stream) : launch_one<64, 4, 1>(io, src, stream));
   }
   if (e != hipSuccess || p.parts == 1) return e;
-  if (a.d == 128) hipLaunchKernelGGL((join_parts_kernel<128>), dim3(io.rows), dim3(256), 0, stream, io, p.parts);
-  else hipLaunchKernelGGL((join_parts_kernel<64>), dim3(io.rows), dim3(256), 0, stream, io, p.parts);
-  return hipGetLastError();
+  return a.d == 128 ? join_parts<128>(io, p.parts, a.num_cu, stream) : join_parts<64>(io, p.parts, a.num_cu, stream);
 }
 
 hipError_t launch_sparse_attn_q8(const SparseQ8Args& a, hipStream_t stream) {
