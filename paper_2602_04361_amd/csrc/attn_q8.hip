@@ -875,19 +875,24 @@ struct DenseQ8Plan {
 // 128, us by the forms with few, 4 and 8 waves: 2 x 16 heads, 256 x 521 keys 9.1 / 15.6 / 22.5,
 // 400 x 921 16.8 / 21.7 / 31.4, 1024 x 2521 64 / 49.6 / 70, 1600 x 4121 158 / 119.7 / 115.2,
 // 2304 x 6425 314 / 277 / 342, 4096 x 10521 - / 612 / 592; 8 heads, 1024 x 2521 21.3 / 46.8 /
-// 70. Two sets of four waves are for launches of up to a workgroup a CU, which then has two waves
-// a SIMD: against one set 256 workgroups of 10521 keys 160 / 174 (d = 64 104 / 124), 192 of 5575
-// 80.5 / 95, 256 of 2521 46.0 / 49.6; 384 workgroups 297 / 282. One token of 8 heads, 10521 keys
-// of one head: 281 us in one part, 11.5 in 21, 13.7 in 83; one token of 4 x 32 heads, up to 42521
+// 70. Sets are for launches of up to a workgroup a CU, which then has two waves a SIMD. Two sets
+// of four waves against one: 256 workgroups of 10521 keys 160 / 174 (d = 64 104 / 124), 192 of
+// 5575 80.5 / 95, 256 of 2521 46.0 / 49.6; 384 workgroups 297 / 282. Four sets of two against the
+// best of the others: d = 64, 16 heads, 646 x 2755 20.3 / 22.9, 1024 x 2521 19.7 / 22.6, d = 128,
+// 12 heads, 1024 x 2521 28.2 / 30.8; 8 heads, 1024 x 2521 28.0 / 21; without a workspace, 4 heads,
+// 4096 x 10521 96.6 / 114 (90 in four parts of the others). One token of 8 heads, 10521 keys of
+// one head: 281 us in one part, 11.5 in 21, 13.7 in 83; one token of 4 x 32 heads, up to 42521
 // keys of 8 heads: 76.8 in 8 parts, 58.4 in 16, 62.2 in 32.
 struct DenseForm {
   int waves, sets;
   float f0, f, a, c;
 };
-constexpr DenseForm kDenseForms[2][4] = {
+constexpr DenseForm kDenseForms[2][5] = {
     // d = 64, d = 128
-    {{0, 1, 3.f, .6f, .05f, .20f}, {4, 1, 3.f, 1.3f, .2f, .53f}, {4, 2, 4.5f, 4.4f, 0.f, 1.15f}, {8, 1, 4.f, 4.4f, 0.f, 1.12f}},
-    {{0, 1, 2.f, 2.2f, .15f, .35f}, {4, 1, 3.5f, 3.f, .3f, .92f}, {4, 2, 5.5f, 6.f, 0.f, 1.8f}, {8, 1, 5.f, 6.f, 0.f, 1.77f}}};
+    {{0, 1, 3.f, .6f, .05f, .20f}, {2, 4, 2.5f, 3.f, 0.f, 1.38f}, {4, 1, 3.f, 1.3f, .2f, .53f}, {4, 2, 4.5f, 4.4f, 0.f, 1.15f},
+     {8, 1, 4.f, 4.4f, 0.f, 1.12f}},
+    {{0, 1, 2.f, 2.2f, .15f, .35f}, {2, 4, 5.f, 4.5f, 0.f, 1.92f}, {4, 1, 3.5f, 3.f, .3f, .92f}, {4, 2, 5.5f, 6.f, 0.f, 1.8f},
+     {8, 1, 5.f, 6.f, 0.f, 1.77f}}};
 constexpr int kMostParts = 128;
 
 DenseQ8Plan dense_plan(int32_t planes, int32_t group, int32_t n_q, int32_t n_kv, int32_t d, int num_cu, bool may_split) {
@@ -903,7 +908,7 @@ DenseQ8Plan dense_plan(int32_t planes, int32_t group, int32_t n_q, int32_t n_kv,
       const float walk = (float)((chunks + parts * f.sets - 1) / (parts * f.sets)) * (f.a + f.c * m);
       const float read = memory * (m / even) * (1.f + .25f / m);
       float us = f.f0 + f.f * m + (walk > read ? walk : read);
-      if (parts > 1) us += 3.f + .08f * parts + (float)parts * planes * rows * d * (8.f / 3e6f);
+      if (parts > 1) us += 3.f + .08f * parts + (float)parts * planes * rows * d * (8.f / 6e6f);
       if (us < best_us) {
         best_us = us;
         best = DenseQ8Plan{f.waves, f.sets, (int32_t)slabs, (int32_t)parts};
@@ -971,12 +976,11 @@ hipError_t launch_dense_attn_q8(const DenseQ8Args& a, hipStream_t stream) {
     e = hipGetLastError();
   } else {
     const DenseQ8Src<64> src = fill(DenseQ8Src<64>{});
-    if (a.d == 128)
-      e = p.waves == 8 ? launch_one<128, 8, 1>(io, src, stream)
-                       : (p.sets == 2 ? launch_one<128, 4, 2>(io, src, stream) : launch_one<128, 4, 1>(io, src, stream));
-    else
-      e = p.waves == 8 ? launch_one<64, 8, 1>(io, src, stream)
-                       : (p.sets == 2 ? launch_one<64, 4, 2>(io, src, stream) : launch_one<64, 4, 1>(io, src, stream));
+#define SV_DENSE(DD, NN, KK) \
+  if (a.d == DD && p.waves == NN && p.sets == KK) e = launch_one<DD, NN, KK>(io, src, stream);
+    SV_DENSE(64, 2, 4) SV_DENSE(64, 4, 1) SV_DENSE(64, 4, 2) SV_DENSE(64, 8, 1)
+    SV_DENSE(128, 2, 4) SV_DENSE(128, 4, 1) SV_DENSE(128, 4, 2) SV_DENSE(128, 8, 1)
+#undef SV_DENSE
   }
   if (e != hipSuccess || p.parts == 1) return e;
   return a.d == 128 ? join_parts<128>(io, p.parts, a.num_cu, stream) : join_parts<64>(io, p.parts, a.num_cu, stream);
