@@ -94,6 +94,8 @@ def run_dense(B, H, Hkv, nq, nkv, d, G, lens=None, ws=False, seed=0, cap=None, p
     (1, 8, 2, 1, 9001, 128, 64), (1, 2, 2, 1, 20011, 64, 16), (1, 8, 1, 6, 7777, 64, 32), (1, 2, 2, 70, 8000, 128, 64),
     # more rows than a join takes a workgroup each; two sets of waves that share the keys
     (1, 4, 4, 700, 3000, 64, 32), (1, 4, 2, 701, 3000, 128, 64), (1, 20, 20, 1000, 1100, 128, 64), (1, 32, 32, 1000, 2600, 64, 16),
+    # four sets of two waves
+    (2, 8, 8, 646, 2755, 64, 64), (1, 12, 12, 1030, 2500, 128, 32),
     # slabs of 128 and 256 rows
     (2, 8, 8, 900, 1000, 128, 32), (2, 8, 8, 900, 1000, 64, 64), (2, 16, 16, 1600, 1000, 128, 64), (2, 16, 16, 1600, 200, 64, 16)])
 @pytest.mark.parametrize("ws", [False, True])
@@ -104,7 +106,7 @@ def test_dense(B, H, Hkv, nq, nkv, d, G, ws):
 
 @pytest.mark.parametrize("ws", [False, True])
 @pytest.mark.parametrize("nq,nkv,d", [(1, 4000, 128), (20, 900, 64), (100, 500, 128), (1000, 300, 128),
-                                      (1000, 1500, 128), (700, 5000, 64)])
+                                      (1000, 1500, 128), (700, 5000, 64), (540, 1500, 64)])
 def test_dense_lengths(nq, nkv, d, ws):
     """Lengths of their own: none, negative, one, a chunk's edge, past the end; codes past a length are NaN."""
     lens = [0, -3, 1, 63, 64, 65, 200, nkv - 1, nkv, nkv + 99]
