@@ -80,7 +80,7 @@ struct DenseQ8Src {
 // A block cut at its scale's edge (24 tokens of an 8 x 8 block, say) then takes no more room in a
 // chunk than it has tokens, where the block table of the bf16 kernels gives it a chunk: block
 // sparse 48 x 36, d = 64, 83% of whose table's slots held a token, 30.5 -> 27.5 us, 32 x 18 with
-// 54% 15.7 -> 12.5, 64 x 64 with 98% the same (121). tok is the token of the lane's slot (the
+// 54% 15.7 -> 12.5, 64 x 64 with 98% 120.3 -> 121.4. tok is the token of the lane's slot (the
 // last one's past count).
 struct PackedChunk {
   uint32_t tok;
