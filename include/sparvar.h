@@ -587,7 +587,12 @@ int sparvar_kv_dequantize(int32_t B, int32_t H_kv, int32_t d, sparvar_dtype_t dt
 
 /*
  * Dense attention over the first n_kv tokens of an 8-bit cache: the definition
- * of sparvar_dense_attn_fwd on the values that the codes stand for (bf16 only).
+ * of sparvar_dense_attn_fwd on the values that the codes stand for (bf16 only),
+ * but for queries whose elements lie far apart: calls of many rows hold a query's
+ * elements below 2^-13 of its largest to 2^-21 of that largest (the others are
+ * exact, and all of them in calls of few rows), so that a score is off by at most
+ * softmax_scale * 2^-21 * max|q| * sum|k|. Which form a call takes goes by its
+ * sizes and by whether it has a workspace.
  *   q: [B,H,n_q,d] (plane stride q_bh_stride), magnitudes below 2^120; o:
  *   [B,H,n_q,d] contiguous; lse (nullable): [B,H,n_q] fp32.
  *   kv_len (nullable): device int32 [B]; entry b attends to its first
@@ -596,8 +601,8 @@ int sparvar_kv_dequantize(int32_t B, int32_t H_kv, int32_t d, sparvar_dtype_t dt
  *   least what sparvar_dense_attn_q8_workspace gives for the same sizes on this
  *   device (0: none is used). With it, calls of few rows cut the keys into parts
  *   that run side by side and are joined in order by a second launch; without
- *   it, every row is walked in one part. The last bits of o and lse may depend
- *   on that. A workspace serves one call at a time: calls that may overlap,
+ *   it, every row is walked in one part. The last bits of o and lse, and scores
+ *   within the bound above, may depend on that. A workspace serves one call at a time: calls that may overlap,
  *   replays of captured graphs among them, need one each.
  */
 int64_t sparvar_dense_attn_q8_workspace(int32_t B, int32_t H, int32_t H_kv, int32_t n_q, int32_t n_kv,
@@ -611,7 +616,8 @@ int sparvar_dense_attn_q8_fwd(int32_t B, int32_t H, int32_t H_kv, int32_t n_q, i
 /*
  * sparvar_block_sparse_attn_fwd over an 8-bit cache (bf16 queries and outputs):
  * the same rows, launch orders of rows and outputs, on the values that the codes
- * stand for, queries' magnitudes below 2^120. CSR rows stay per query head; an
+ * stand for, queries' magnitudes below 2^120 and held as by the dense call's form
+ * of many rows (exact from 2^-13 of a row's largest, 2^-21 of it below). CSR rows stay per query head; an
  * order of groups is not used.
  */
 int sparvar_block_sparse_attn_q8_fwd(const sparvar_geometry_t* g, int32_t k, int32_t B, int32_t H,

@@ -290,17 +290,20 @@ __device__ __forceinline__ void store_rows(const Q8IO& io, const f32x16 (&acc)[D
 
 // Query fragments for the products with K's codes: the row divided by a power of two (its
 // largest magnitude then in (224, 448]) as the sum of two e4m3 values. bf16 has 8 significant
-// bits and e4m3 4, so the sum is the query itself for elements from 2^-9 of the row's largest
-// on; below, the smaller part ends at the format's last place, 2^-9, and is off by at most half
-// of it: 2^-10 / 224 < 2^-17 of the largest. The rate is that of one bf16 product (two e4m3
-// ones at twice its rate), and K needs no conversion. Step t of a half covers channels
-// 64 t + 32 half .. + 32, as the K fragments do.
+// bits and e4m3 4. What the larger part leaves is at most 16, so the smaller one is stored
+// times 2^4, under a scale byte of its own: its last place is 2^-13. The sum is the query itself
+// for elements from 2^-6 on, among them all from 2^-13 of the row's largest; below, it is off by
+// at most half that place, 2^-14 / 224 < 2^-21 of the largest. Rows of one channel of 100 beside
+// normals times 0.1, keys of normals times 4: the split alone, in exact sums, moves the LSE by
+// 3e-5 (without the 2^4 by 2e-3). The rate is that of one bf16 product (two e4m3 ones at twice
+// its rate), and K needs no conversion. Step t of a half covers channels 64 t + 32 half .. + 32,
+// as the K fragments do.
 typedef __attribute__((ext_vector_type(8))) int i32x8;
 
 template <int D>
 struct QFragF8 {
   i32x8 hi[D / 64], lo[D / 64];
-  int32_t scale;  // E8M0 byte
+  int32_t scale;  // E8M0 bytes: of hi, and above it of lo
   __device__ __forceinline__ void load(const bf16_bits* row, int half) {
     u32x4 raw[D / 16];
     float top = 0.f;
@@ -317,7 +320,7 @@ struct QFragF8 {
       }
     const int32_t e2 = block_exponent(max_halves(top));
     const float inv = pow2f(-e2);
-    scale = e2 + 127;
+    scale = (e2 + 127) | (e2 + 123) << 8;
 #pragma unroll
     for (int t = 0; t < D / 64; ++t)
 #pragma unroll
@@ -329,17 +332,18 @@ struct QFragF8 {
         float y[4];
         decode4(h, 1.f, y);
         hi[t][w] = (int)h;
-        lo[t][w] = (int)codes4(x[0] - y[0], x[1] - y[1], x[2] - y[2], x[3] - y[3]);
+        lo[t][w] = (int)codes4((x[0] - y[0]) * 16.f, (x[1] - y[1]) * 16.f, (x[2] - y[2]) * 16.f, (x[3] - y[3]) * 16.f);
       }
   }
 };
 
-// c += K Q^T over 64 channels: a the codes of 32 keys (scale byte ks of the lane's key).
+// c += K Q^T over 64 channels: a the codes of 32 keys (scale byte ks of the lane's key). Of the
+// queries' scale, byte 0 goes with hi and byte 1 with lo.
 template <int D>
 __device__ __forceinline__ f32x16 mfma_k(i32x8 a, int32_t ks, const QFragF8<D>& q, int t, f32x16 c) {
 #if defined(__HIP_DEVICE_COMPILE__)
   c = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, q.hi[t], c, 0, 0, 0, ks, 0, q.scale);
-  c = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, q.lo[t], c, 0, 0, 0, ks, 0, q.scale);
+  c = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, q.lo[t], c, 0, 0, 0, ks, 1, q.scale);
 #endif
   return c;
 }
