@@ -596,7 +596,8 @@ int sparvar_kv_dequantize(int32_t B, int32_t H_kv, int32_t d, sparvar_dtype_t dt
  *   q: [B,H,n_q,d] (plane stride q_bh_stride), magnitudes below 2^120; o:
  *   [B,H,n_q,d] contiguous; lse (nullable): [B,H,n_q] fp32.
  *   kv_len (nullable): device int32 [B]; entry b attends to its first
- *   min(max(kv_len[b], 0), n_kv) tokens. With none, o = 0 and lse = -inf.
+ *   min(max(kv_len[b], 0), n_kv) tokens. With none, o = 0 and lse = -inf; a row
+ *   with a NaN among its query or keys has NaN in both.
  *   workspace (nullable, 16-byte aligned): workspace_bytes of device memory, at
  *   least what sparvar_dense_attn_q8_workspace gives for the same sizes on this
  *   device (0: none is used). With it, calls of few rows cut the keys into parts

@@ -256,6 +256,12 @@ __device__ __forceinline__ void put_piece(char* at0, char* at1, const u32x4& raw
   *reinterpret_cast<u32x4*>(at1) = u32x4{w[4], w[5], w[6], w[7]};
 }
 
+// Log of the softmax denominator, of a maximum in the exp2 domain and a sum: -inf where there were
+// no keys, and NaN where one scored NaN (a sum of NaN is no empty one).
+__device__ __forceinline__ float lse_of(float m, float l) {
+  return l == 0.f ? -INFINITY : (m + __builtin_log2f(l)) * kLn2;
+}
+
 // What a wave found for its rows: the part's unnormalised sums, maximum and sum, or the output.
 template <int D>
 __device__ __forceinline__ void store_rows(const Q8IO& io, const f32x16 (&acc)[D / 32], float m, float l, bool qvalid, int half,
@@ -285,7 +291,7 @@ __device__ __forceinline__ void store_rows(const Q8IO& io, const f32x16 (&acc)[D
       w.y = pack_bf16x2(acc[dt][4 * j + 2] * inv, acc[dt][4 * j + 3] * inv);
       *reinterpret_cast<uint2*>(op + 32 * dt + 8 * j + 4 * half) = w;
     }
-  if (io.lse && half == 0) io.lse[orow] = l > 0.f ? (m + __builtin_log2f(l)) * kLn2 : -INFINITY;
+  if (io.lse && half == 0) io.lse[orow] = lse_of(m, l);
 }
 
 // Query fragments for the products with K's codes: the row divided by a power of two (its
@@ -625,7 +631,7 @@ __global__ __launch_bounds__(QW * KS * 64) __attribute__((amdgpu_waves_per_eu(2)
       w.y = pack_bf16x2(out[4 * i + 2] * inv, out[4 * i + 3] * inv);
       *reinterpret_cast<uint2*>(io.o + orow * D + channel_of(split * (D / 8 / KS) + i, half)) = w;
     }
-    if (io.lse && split == 0 && half == 0) io.lse[orow] = l_g > 0.f ? (m_g + __builtin_log2f(l_g)) * kLn2 : -INFINITY;
+    if (io.lse && split == 0 && half == 0) io.lse[orow] = lse_of(m_g, l_g);
     return;
   }
   const float l_tot = sum_halves(l_run);
@@ -790,7 +796,7 @@ void attn_q8_rows_kernel(Q8IO io, DenseQ8Src<32> src) {
   }
   if (qvalid && wave == 0 && half == 0) {
     if (io.part_o) io.part_ml[prow] = make_float2(m_g, l_g);
-    else if (io.lse) io.lse[orow] = l_g > 0.f ? (m_g + __builtin_log2f(l_g)) * kLn2 : -INFINITY;
+    else if (io.lse) io.lse[orow] = lse_of(m_g, l_g);
   }
 }
 
@@ -853,7 +859,7 @@ __global__ __launch_bounds__(256) void join_parts_kernel(Q8IO io, int32_t parts)
   w.x = pack_bf16x2(r.x * inv, r.y * inv);
   w.y = pack_bf16x2(r.z * inv, r.w * inv);
   *reinterpret_cast<uint2*>(io.o + (int64_t)row * D + 4 * c) = w;
-  if (io.lse && c == 0) io.lse[row] = l > 0.f ? (m + __builtin_log2f(l)) * kLn2 : -INFINITY;
+  if (io.lse && c == 0) io.lse[row] = lse_of(m, l);
 }
 
 template <int D>
