@@ -615,6 +615,15 @@ int sparvar_dense_attn_q8_fwd(int32_t B, int32_t H, int32_t H_kv, int32_t n_q, i
                               hipStream_t stream);
 
 /*
+ * Form that a dense call of these sizes takes on this device, with a workspace
+ * (nonzero) or without: form[0] waves of 32 rows a workgroup (0: the form of few
+ * rows), form[1] sets of them that share its keys, form[2] parts of the keys.
+ * Host-only; form is a host array of three entries.
+ */
+int sparvar_dense_attn_q8_form(int32_t B, int32_t H, int32_t H_kv, int32_t n_q, int32_t n_kv, int32_t d,
+                               int32_t workspace, int32_t* form);
+
+/*
  * sparvar_block_sparse_attn_fwd over an 8-bit cache (bf16 queries and outputs):
  * the same rows, launch orders of rows and outputs, on the values that the codes
  * stand for, queries' magnitudes below 2^120 and held as by the dense call's form

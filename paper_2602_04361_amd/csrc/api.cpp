@@ -1118,6 +1118,18 @@ int sparvar_dense_attn_q8_fwd(int32_t B, int32_t H, int32_t H_kv, int32_t n_q, i
   return hip_status(launch_dense_attn_q8(a, stream), "dense 8-bit attention launch");
 }
 
+int sparvar_dense_attn_q8_form(int32_t B, int32_t H, int32_t H_kv, int32_t n_q, int32_t n_kv, int32_t d,
+                               int32_t workspace, int32_t* form) {
+  const int st = check_dense_q8(B, H, H_kv, n_q, n_kv, d);
+  if (st) return st;
+  if (!form) return fail(SPARVAR_ERR_INVALID, "form is NULL");
+  const Q8Form f = dense_q8_form(B, H, H_kv, n_q, n_kv, d, device_cus(), workspace != 0);
+  form[0] = f.waves;
+  form[1] = f.sets;
+  form[2] = f.parts;
+  return ok();
+}
+
 int sparvar_block_sparse_attn_q8_fwd(const sparvar_geometry_t* g, int32_t k, int32_t B, int32_t H,
                                      int32_t H_kv, int32_t d, sparvar_dtype_t dtype, const void* q_k,
                                      int64_t q_bh_stride, const sparvar_q8_cache_t* q8, void* o, float* lse,

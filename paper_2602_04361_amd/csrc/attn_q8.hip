@@ -950,6 +950,11 @@ int64_t dense_q8_workspace(int32_t B, int32_t H, int32_t H_kv, int32_t n_q, int3
   return p.parts > 1 ? 4 * part_floats(p.parts, (int64_t)B * H * n_q, d) : 0;
 }
 
+Q8Form dense_q8_form(int32_t B, int32_t H, int32_t H_kv, int32_t n_q, int32_t n_kv, int32_t d, int num_cu, bool workspace) {
+  const DenseQ8Plan p = dense_plan(B * H_kv, H / H_kv, n_q, n_kv, d, num_cu, workspace);
+  return Q8Form{p.waves, p.sets, p.parts};
+}
+
 hipError_t launch_dense_attn_q8(const DenseQ8Args& a, hipStream_t stream) {
   const int32_t group = a.H / a.H_kv;
   const DenseQ8Plan p = dense_plan(a.B * a.H_kv, group, a.n_q, a.n_kv, a.d, a.num_cu, a.workspace != nullptr);

@@ -192,6 +192,10 @@ struct DenseQ8Args {
 // Bytes of workspace that a call of these sizes takes (0: it walks its keys in one part).
 int64_t dense_q8_workspace(int32_t B, int32_t H, int32_t H_kv, int32_t n_q, int32_t n_kv, int32_t d, int num_cu);
 hipError_t launch_dense_attn_q8(const DenseQ8Args& a, hipStream_t stream);
+struct Q8Form {
+  int32_t waves, sets, parts;
+};
+Q8Form dense_q8_form(int32_t B, int32_t H, int32_t H_kv, int32_t n_q, int32_t n_kv, int32_t d, int num_cu, bool workspace);
 
 struct SparseQ8Args {
   const GeoTable* G;

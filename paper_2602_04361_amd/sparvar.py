@@ -47,6 +47,7 @@ EXPORTS = [
     "sparvar_kv_quantize",
     "sparvar_kv_dequantize",
     "sparvar_dense_attn_q8_workspace",
+    "sparvar_dense_attn_q8_form",
     "sparvar_dense_attn_q8_fwd",
     "sparvar_block_sparse_attn_q8_fwd",
     "sparvar_status_string",
@@ -167,6 +168,7 @@ def load_library(path: str = LIB_PATH):
         "sparvar_kv_quantize": (ctypes.c_int, [i32, i32, i32, ctypes.c_int, i32, i32, vp, vp, i64, Q8, vp]),
         "sparvar_kv_dequantize": (ctypes.c_int, [i32, i32, i32, ctypes.c_int, i32, i32, Q8, vp, vp, i64, vp]),
         "sparvar_dense_attn_q8_workspace": (i64, [i32, i32, i32, i32, i32, i32]),
+        "sparvar_dense_attn_q8_form": (ctypes.c_int, [i32, i32, i32, i32, i32, i32, i32, ctypes.POINTER(i32)]),
         "sparvar_dense_attn_q8_fwd": (ctypes.c_int, [i32, i32, i32, i32, i32, i32, ctypes.c_int, vp, i64, Q8, vp, vp, vp,
                                                      f32, vp, i64, vp]),
         "sparvar_block_sparse_attn_q8_fwd": (ctypes.c_int, [G, i32, i32, i32, i32, i32, ctypes.c_int, vp, i64, Q8, vp, vp,
@@ -709,6 +711,13 @@ def sparvar_dense_attn_q8_workspace(B, H, H_kv, n_q, n_kv, d):
     if n < 0:
         _check(int(n))
     return int(n)
+
+
+def sparvar_dense_attn_q8_form(B, H, H_kv, n_q, n_kv, d, workspace):
+    """(waves, sets, parts) that a dense call of these sizes walks with, with a workspace or without; see sparvar.h."""
+    form = (ctypes.c_int32 * 3)()
+    _check(load_library().sparvar_dense_attn_q8_form(B, H, H_kv, n_q, n_kv, d, int(workspace), form))
+    return tuple(form)
 
 
 def _q8_attn(q, q8, o, lse, *others):

@@ -1,0 +1,89 @@
+"""Every form that a call over an 8-bit cache can take is run by a case that is known to take it: the library says which one
+(host only), so a case that a change of the rules moves to another form fails here."""
+import numpy as np
+import pytest
+import torch
+
+from gpu_helpers import note, scale_of
+from paper_2602_04361_amd import sparvar as sv
+
+
+def sampled(n, seed, most=192):
+    """All of n rows, or the first, the last and a sample of them."""
+    if n <= most:
+        return np.arange(n)
+    r = np.random.default_rng(seed)
+    return np.unique(np.concatenate([[0, 1, n - 2, n - 1], r.choice(n, most - 4, replace=False)]))
+
+
+# (waves, sets, more than one part), d: B, H, H_kv, n_q, n_kv, scale block, lengths (None: n_kv; 0 and 70 leave parts empty)
+DENSE = [
+    ((0, 1, False), 64, (2, 2, 1, 5, 65, 16, [65, 0])), ((0, 1, False), 128, (1, 4, 2, 7, 33, 64, None)),
+    ((0, 1, True), 64, (3, 1, 1, 32, 647, 32, [647, 0, 70])), ((0, 1, True), 128, (3, 1, 1, 33, 513, 64, [513, 65, 0])),
+    ((2, 4, False), 64, (1, 4, 2, 2122, 965, 64, None)), ((2, 4, False), 128, (3, 2, 2, 1381, 649, 32, [649, 70, 0])),
+    ((4, 2, False), 64, (1, 8, 2, 3130, 2174, 128, [2101])), ((4, 2, False), 128, (3, 3, 3, 1821, 970, 64, [970, 70, 0])),
+    ((4, 1, False), 64, (1, 4, 4, 4123, 34, 16, [33])), ((4, 1, False), 128, (3, 4, 2, 1370, 520, 64, [520, 0, 449])),
+    ((4, 1, True), 64, (3, 8, 4, 161, 2983, 64, [2983, 0, 70])), ((4, 1, True), 128, (3, 8, 4, 165, 2126, 32, [2126, 65, 1])),
+    ((4, 1, True), 64, (1, 2, 1, 1428, 4889, 128, None)), ((4, 1, True), 128, (1, 8, 2, 513, 2422, 16, [2400])),
+    ((8, 1, False), 64, (3, 4, 4, 3433, 1284, 64, [1284, 0, 63])), ((8, 1, False), 128, (3, 6, 3, 1856, 513, 64, [513, 0, 300])),
+    ((8, 1, True), 64, (3, 6, 3, 917, 3877, 64, [3877, 70, 0])), ((8, 1, True), 128, (3, 6, 3, 450, 4267, 32, [4267, 64, 0])),
+]
+
+
+def test_dense_cases_take_their_forms():
+    seen = set()
+    for (waves, sets, cut), d, (B, H, Hkv, nq, nkv, _, _) in DENSE:
+        w, s, parts = sv.sparvar_dense_attn_q8_form(B, H, Hkv, nq, nkv, d, True)
+        assert (w, s, parts > 1) == (waves, sets, cut), (d, B, H, Hkv, nq, nkv)
+        size = sv.sparvar_dense_attn_q8_workspace(B, H, Hkv, nq, nkv, d)
+        assert size == (4 * parts * B * H * nq * (d + 2) if cut else 0)
+        assert sv.sparvar_dense_attn_q8_form(B, H, Hkv, nq, nkv, d, False)[2] == 1
+        seen.add((w, s, parts > 1, d))
+    # sets of waves take no parts
+    assert seen == {(w, s, cut, d) for d in (64, 128) for w, s, cuts in
+                    [(0, 1, (False, True)), (4, 1, (False, True)), (8, 1, (False, True)), (4, 2, (False,)), (2, 4, (False,))]
+                    for cut in cuts}
+
+
+def test_form_arguments():
+    with pytest.raises(sv.SparvarError):
+        sv.sparvar_dense_attn_q8_form(1, 3, 2, 1, 1000, 64, True)
+    assert sv.load_library().sparvar_dense_attn_q8_form(1, 4, 2, 1, 1000, 64, 1, None) == sv.ERR_INVALID
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("form,d,sizes", DENSE)
+def test_dense_form(form, d, sizes):
+    """With a workspace of NaN, lengths of their own, a capacity past the cache of NaN codes."""
+    from test_gpu_q8_attn import check_rows, make_cache
+
+    B, H, Hkv, nq, nkv, G, lens = sizes
+    note(f"[q8 forms] dense {form} d={d} {sizes}")
+    w, s, parts = sv.sparvar_dense_attn_q8_form(B, H, Hkv, nq, nkv, d, True)
+    assert (w, s, parts > 1) == form
+    q8, k, v = make_cache(B, Hkv, nkv, d, G, nq + nkv, cap=nkv + 70)
+    g = torch.Generator(device="cuda").manual_seed(nq)
+    q = torch.randn(B, H, nq + 3, d, generator=g, device="cuda").bfloat16()[:, :, :nq]
+    o, lse = torch.full((B, H, nq, d), 5.0, device="cuda").bfloat16(), torch.full((B, H, nq), 5.0, device="cuda")
+    size = sv.sparvar_dense_attn_q8_workspace(B, H, Hkv, nq, nkv, d)
+    work = torch.full((max(size, 16) + 64,), 0xff, dtype=torch.uint8, device="cuda")
+    kv_len = None if lens is None else torch.tensor(lens, dtype=torch.int32, device="cuda")
+    sv.sparvar_dense_attn_q8_fwd(q, q8, nkv, o, lse=lse, kv_len=kv_len, workspace=work[:max(size, 16)])
+    torch.cuda.synchronize()
+    assert (work[max(size, 16):] == 0xff).all()
+    at = sampled(nq, nq)
+    for b in range(B):
+        n = nkv if lens is None else lens[b]
+        for h in range(H):
+            check_rows(o[b, h].double().cpu().numpy()[at], lse[b, h].double().cpu().numpy()[at],
+                       q[b, h].double().cpu().numpy()[at], k[b, h // (H // Hkv), :n], v[b, h // (H // Hkv), :n], scale_of(d),
+                       what=f"entry {b} head {h}")
+    # every row, by the form without parts: both calls are within their bounds of the same values
+    alone, alone_l = torch.empty_like(o), torch.empty_like(lse)
+    sv.sparvar_dense_attn_q8_fwd(q, q8, nkv, alone, lse=alone_l, kv_len=kv_len)
+    torch.cuda.synchronize()
+    assert torch.equal(torch.isinf(lse), torch.isinf(alone_l)) and torch.isfinite(o.float()).all()
+    full = ~torch.isinf(lse)
+    assert (lse[full] - alone_l[full]).abs().max() <= 4e-4
+    vmax = np.abs(v).max()  # sum p |v| and |o| are at most this
+    assert (o.float() - alone.float()).abs().max() <= 2 * 1.02 * 2.0 ** -8 * 2 * vmax
