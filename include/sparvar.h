@@ -636,6 +636,14 @@ int sparvar_block_sparse_attn_q8_fwd(const sparvar_geometry_t* g, int32_t k, int
                                      float softmax_scale, const int32_t* row_ptr, const int32_t* col_idx,
                                      const int32_t* schedule, hipStream_t stream);
 
+/*
+ * Form that such a call takes on this device: form[0] waves of 32 queries a
+ * workgroup, form[1] parts of a row, walked side by side in the workgroup.
+ * Host-only; form is a host array of two entries.
+ */
+int sparvar_block_sparse_attn_q8_form(const sparvar_geometry_t* g, int32_t k, int32_t B, int32_t H,
+                                      int32_t H_kv, int32_t d, int32_t* form);
+
 /* Static description of a status code. */
 const char* sparvar_status_string(int status);
 /* Message of the last failed call on this thread ("" if none). */

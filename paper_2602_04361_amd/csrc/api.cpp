@@ -1169,4 +1169,20 @@ int sparvar_block_sparse_attn_q8_fwd(const sparvar_geometry_t* g, int32_t k, int
   return hip_status(launch_sparse_attn_q8(a, stream), "block-sparse 8-bit attention launch");
 }
 
+int sparvar_block_sparse_attn_q8_form(const sparvar_geometry_t* g, int32_t k, int32_t B, int32_t H,
+                                      int32_t H_kv, int32_t d, int32_t* form) {
+  GeoTable T;
+  int st = build_table(g, &T);
+  if (st) return st;
+  if (k < 1 || k > T.L) return fail(SPARVAR_ERR_INVALID, "scale %d outside [1, %d]", k, T.L);
+  if ((st = check_dtype_d(SPARVAR_BF16, d))) return st;
+  if ((st = check_heads(B, H, H_kv))) return st;
+  if ((int64_t)B * H * T.h[k - 1] * T.w[k - 1] >= (int64_t(1) << 31)) return fail(SPARVAR_ERR_INVALID, "B*H*N_k too large");
+  if (!form) return fail(SPARVAR_ERR_INVALID, "form is NULL");
+  const Q8Form f = sparse_q8_form(T, k, B * H, d, device_cus());
+  form[0] = f.waves;
+  form[1] = f.sets;
+  return ok();
+}
+
 }  // extern "C"

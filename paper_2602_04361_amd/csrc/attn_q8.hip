@@ -1001,10 +1001,27 @@ hipError_t launch_dense_attn_q8(const DenseQ8Args& a, hipStream_t stream) {
   return a.d == 128 ? join_parts<128>(io, p.parts, a.num_cu, stream) : join_parts<64>(io, p.parts, a.num_cu, stream);
 }
 
+Q8Form sparse_q8_form(const GeoTable& G, int32_t k, int32_t BH, int32_t d, int num_cu) {
+  const int32_t tile_q = G.eh[k - 1] * G.ew[k - 1];
+  const int nw = waves_for(tile_q);
+  const int32_t items = BH * tiles_of(G, k) * ((tile_q + nw * kQPerWave - 1) / (nw * kQPerWave));
+  // Tiles of 33 to 64 queries (8 x 8): launches of few waves a SIMD walk their rows in two parts
+  // (64 x 64 scale, d = 128: 512 workgroups 39.0 us against 50.7, 640 57.0 / 53.6; d = 64: 512
+  // 27.5 / 38.4, 768 33.9 / 39.7, 896 44.1 / 42.3; past that within 8% of each other, with the
+  // rounds that either makes), up to one workgroup a CU in four, where the cache is long enough
+  // for rows that give back what the join costs (256 workgroups, 10521 tokens: d = 128 26.9 in
+  // four against 29.4, d = 64 18.8 / 21.1; 921 tokens 20.9 / 21.1 and 14.2 / 15.1; 521 17.4 /
+  // 16.3 and 12.2 / 12.0; past one workgroup a CU, 320: 47.6 / 38.1 and 32.9 / 26.6).
+  int32_t sets = 1;
+  if (nw == 2 && items <= (d == 64 ? 3 : 2) * num_cu) sets = items <= num_cu && G.C[k] >= 640 ? 4 : 2;
+  return Q8Form{nw, sets, 1};
+}
+
 hipError_t launch_sparse_attn_q8(const SparseQ8Args& a, hipStream_t stream) {
   const GeoTable& G = *a.G;
   const int32_t tile_q = G.eh[a.k - 1] * G.ew[a.k - 1], G_k = tiles_of(G, a.k);
-  const int nw = waves_for(tile_q);
+  const Q8Form form = sparse_q8_form(G, a.k, a.BH, a.d, a.num_cu);
+  const int nw = form.waves;
   const int32_t qpw = nw * kQPerWave, slabs = (tile_q + qpw - 1) / qpw;
   Q8IO io;
   io.q = static_cast<const bf16_bits*>(a.q);
@@ -1031,16 +1048,7 @@ hipError_t launch_sparse_attn_q8(const SparseQ8Args& a, hipStream_t stream) {
   src.q_per_wg = qpw;
   src.slabs = slabs;
   src.n_rows = a.BH * G_k;
-  // Tiles of 33 to 64 queries (8 x 8): launches of few waves a SIMD walk their rows in two parts
-  // (64 x 64 scale, d = 128: 512 workgroups 39.0 us against 50.7, 640 57.0 / 53.6; d = 64: 512
-  // 27.5 / 38.4, 768 33.9 / 39.7, 896 44.1 / 42.3; past that within 8% of each other, with the
-  // rounds that either makes), up to one workgroup a CU in four, where the cache is long enough
-  // for rows that give back what the join costs (256 workgroups, 10521 tokens: d = 128 26.9 in
-  // four against 29.4, d = 64 18.8 / 21.1; 921 tokens 20.9 / 21.1 and 14.2 / 15.1; 521 17.4 /
-  // 16.3 and 12.2 / 12.0; past one workgroup a CU, 320: 47.6 / 38.1 and 32.9 / 26.6).
-  int ks = 1;
-  if (nw == 2 && io.n_items <= (a.d == 64 ? 3 : 2) * a.num_cu)
-    ks = io.n_items <= a.num_cu && G.C[a.k] >= 640 ? 4 : 2;
+  const int ks = form.sets;
 #define SV_SPARSE(DD, NN, KK) \
   if (a.d == DD && nw == NN && ks == KK) return launch_one<DD, NN, KK>(io, src, stream);
   SV_SPARSE(64, 1, 1) SV_SPARSE(64, 2, 1) SV_SPARSE(64, 2, 2) SV_SPARSE(64, 2, 4) SV_SPARSE(64, 4, 1) SV_SPARSE(64, 8, 1)

@@ -211,6 +211,8 @@ struct SparseQ8Args {
   int num_cu;
 };
 hipError_t launch_sparse_attn_q8(const SparseQ8Args& a, hipStream_t stream);
+// Waves of a tile and parts of a row (its sets) of a block-sparse call at scale k.
+Q8Form sparse_q8_form(const GeoTable& G, int32_t k, int32_t BH, int32_t d, int num_cu);
 
 // Work items of the bf16 block-sparse launch at scale k (with the default
 // waves, chunk and stages): one query tile per workgroup (gh = gw = 0), or groups

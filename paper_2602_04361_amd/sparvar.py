@@ -50,6 +50,7 @@ EXPORTS = [
     "sparvar_dense_attn_q8_form",
     "sparvar_dense_attn_q8_fwd",
     "sparvar_block_sparse_attn_q8_fwd",
+    "sparvar_block_sparse_attn_q8_form",
     "sparvar_status_string",
     "sparvar_last_error",
     "sparvar_set_launch_option",
@@ -173,6 +174,7 @@ def load_library(path: str = LIB_PATH):
                                                      f32, vp, i64, vp]),
         "sparvar_block_sparse_attn_q8_fwd": (ctypes.c_int, [G, i32, i32, i32, i32, i32, ctypes.c_int, vp, i64, Q8, vp, vp,
                                                             f32, vp, vp, vp, vp]),
+        "sparvar_block_sparse_attn_q8_form": (ctypes.c_int, [G, i32, i32, i32, i32, i32, ctypes.POINTER(i32)]),
         "sparvar_status_string": (ctypes.c_char_p, [ctypes.c_int]),
         "sparvar_last_error": (ctypes.c_char_p, []),
         "sparvar_set_launch_option": (ctypes.c_int, [i32, i32]),
@@ -765,3 +767,10 @@ def sparvar_block_sparse_attn_q8_fwd(geom, k, q_k, q8, o, row_ptr, col_idx, lse=
                                                 q8.ref, _ptr(o), _ptr(lse), _scale(softmax_scale, d), _ptr(row_ptr),
                                                 _ptr(col_idx), _ptr(schedule), _stream(stream)))
     return o, lse
+
+
+def sparvar_block_sparse_attn_q8_form(geom, k, B, H, H_kv, d):
+    """(waves, parts of a row) that a block-sparse call of these sizes walks with; see sparvar.h."""
+    form = (ctypes.c_int32 * 2)()
+    _check(load_library().sparvar_block_sparse_attn_q8_form(geom.ref, k, B, H, H_kv, d, form))
+    return tuple(form)

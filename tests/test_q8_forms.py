@@ -45,7 +45,36 @@ def test_dense_cases_take_their_forms():
                     for cut in cuts}
 
 
+# (waves, parts of a row), d: sides h, w, block edge, scale, B, H, H_kv, scale block. Tiles of 33 to 64 queries take parts by
+# the number of workgroups; of up to 32, 65 to 128 and more they take none
+S5 = [1, 2, 4, 8]
+SPARSE = [
+    ((1, 1), 64, (S5 + [13], S5 + [11], 4, 5, 1, 3, 3, 16)), ((1, 1), 128, (S5 + [13], S5 + [16], 5, 5, 2, 2, 1, 64)),
+    ((2, 1), 64, ([1, 4, 30], [1, 4, 30], 8, 3, 2, 26, 26, 64)), ((2, 1), 128, ([1, 4, 30], [1, 4, 27], 8, 3, 2, 18, 9, 32)),
+    ((2, 2), 64, ([1, 4, 30], [1, 4, 30], 8, 3, 2, 20, 20, 64)), ((2, 2), 128, ([1, 4, 30], [1, 4, 30], 8, 3, 1, 20, 10, 128)),
+    ((2, 4), 64, (S5 + [16, 25], S5 + [16, 29], 8, 6, 1, 4, 2, 64)), ((2, 4), 128, (S5 + [16, 29], S5 + [16, 25], 8, 6, 1, 3, 3, 16)),
+    # 65 to 128 queries: edges of 9 to 11, and blocks of 16 on a scale 5 to 8 wide
+    ((4, 1), 64, (S5 + [23], S5 + [20], 9, 5, 2, 3, 1, 32)), ((4, 1), 128, (S5 + [24], S5 + [25], 11, 5, 1, 4, 4, 64)),
+    ((4, 1), 64, ([1, 8, 37], [1, 5, 5], 16, 3, 2, 2, 2, 16)), ((4, 1), 128, ([1, 20, 33], [1, 4, 8], 16, 3, 1, 2, 1, 128)),
+    ((8, 1), 64, (S5 + [20], S5 + [35], 16, 5, 1, 2, 2, 64)), ((8, 1), 128, (S5 + [20], S5 + [20], 16, 5, 2, 2, 1, 32)),
+    ((8, 1), 64, ([1, 45], [1, 50], 20, 2, 1, 2, 2, 64)), ((8, 1), 128, ([1, 45], [1, 41], 20, 2, 1, 2, 1, 16)),  # two slabs a tile
+]
+
+
+def test_sparse_cases_take_their_forms():
+    seen = set()
+    for form, d, (h, w, b, k, B, H, Hkv, _) in SPARSE:
+        assert sv.sparvar_block_sparse_attn_q8_form(sv.Geometry(h, w, b, 1), k, B, H, Hkv, d) == form, (d, h, w, b)
+        seen.add((*form, d))
+    assert seen == {(*f, d) for d in (64, 128) for f in [(1, 1), (2, 1), (2, 2), (2, 4), (4, 1), (8, 1)]}
+
+
 def test_form_arguments():
+    g = sv.Geometry([1, 8], [1, 8], 8, 1)
+    for bad in ((3, 1, 2, 2, 64), (2, 1, 3, 2, 64), (2, 1, 2, 2, 96)):
+        with pytest.raises(sv.SparvarError):
+            sv.sparvar_block_sparse_attn_q8_form(g, *bad)
+    assert sv.load_library().sparvar_block_sparse_attn_q8_form(g.ref, 2, 1, 2, 2, 64, None) == sv.ERR_INVALID
     with pytest.raises(sv.SparvarError):
         sv.sparvar_dense_attn_q8_form(1, 3, 2, 1, 1000, 64, True)
     assert sv.load_library().sparvar_dense_attn_q8_form(1, 4, 2, 1, 1000, 64, 1, None) == sv.ERR_INVALID
@@ -87,3 +116,16 @@ def test_dense_form(form, d, sizes):
     assert (lse[full] - alone_l[full]).abs().max() <= 4e-4
     vmax = np.abs(v).max()  # sum p |v| and |o| are at most this
     assert (o.float() - alone.float()).abs().max() <= 2 * 1.02 * 2.0 ** -8 * 2 * vmax
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("order", [False, True])
+@pytest.mark.parametrize("form,d,sizes", SPARSE)
+def test_sparse_form(form, d, sizes, order):
+    """Random rows, three of them empty, ids out of range among the others, codes past the cache NaN."""
+    from test_gpu_q8_attn import run_sparse
+
+    h, w, b, k, B, H, Hkv, G = sizes
+    note(f"[q8 forms] sparse {form} d={d} {sizes} order={order}")
+    assert sv.sparvar_block_sparse_attn_q8_form(sv.Geometry(h, w, b, 1), k, B, H, Hkv, d) == form
+    run_sparse(h, w, b, k, B, H, Hkv, d, G, seed=d + b + sum(w), empty=(0, 3, 8), order=order)
