@@ -238,11 +238,16 @@ class Q8SparsePath(SparsePath):
       l in steps: block-sparse attention over the cache
                  (sparvar_block_sparse_attn_q8_fwd); any other l > S: dense.
     heads: a NormRope whose table has a row for every cache token, or None.
-    block: tokens of a scale of the cache.
+    block: tokens of a scale of the cache. Queries and outputs are bf16, the decision
+    is the fused one, and every step's rows come from one mapping launch: SparsePath's
+    options that choose among these (dtype, fused_decision, local_lists, use_schedule)
+    are not taken.
     """
 
-    def __init__(self, geom: sv.Geometry, S, steps, B, H, d, topk, radius, heads=None, block=64, device="cuda", **kw):
-        super().__init__(geom, S, steps, B, H, d, topk, radius, device=device, **kw)
+    def __init__(self, geom: sv.Geometry, S, steps, B, H, d, topk, radius, heads=None, block=64, device="cuda", *,
+                 prev_dilation=0, softmax_scale=None, projection="point"):
+        super().__init__(geom, S, steps, B, H, d, topk, radius, prev_dilation=prev_dilation, device=device,
+                         softmax_scale=softmax_scale, projection=projection)
         self.heads = heads
         bf = dict(dtype=torch.bfloat16, device=device)
         total = self.info[len(geom.h)]["n_tokens_le"]
