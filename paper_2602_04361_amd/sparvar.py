@@ -519,6 +519,13 @@ def sparvar_block_sparse_attn_fwd(geom, k, q_k, k_lek, v_lek, o, row_ptr, col_id
 
 
 # ---------------------------------------------------------------- 8-bit cache
+def _whole(name, *values):
+    """Numbers that the caller gives, within the 32 bits that the C calls take (ctypes would cut off the rest)."""
+    for v in values:
+        if not -0x80000000 <= v <= 0x7FFFFFFF:
+            raise SparvarError(ERR_INVALID, f"{name}: {v} does not fit 32 bits")
+
+
 def _here(first, *others):
     """Every tensor is on the current device (None among the others: not given)."""
     dev = first.get_device()
@@ -635,6 +642,7 @@ def sparvar_qkv_append(q, k, v, t0, heads, q_out, k_cache=None, v_cache=None, q8
     """Norms, rotation (heads, a NormRope or None) and the append of tokens [t0, t0 + n): queries to q_out [B,H,n,d], keys
     and values to k_cache, v_cache or to an 8-bit cache q8; see sparvar.h."""
     lib = load_library()
+    _whole("t0", t0)
     B, n, H, d = q.shape
     kv_shape = k.shape
     H_kv = kv_shape[2]
@@ -688,6 +696,7 @@ def _kv_planes(k, v):
 def sparvar_kv_quantize(k_src, v_src, t0, q8, stream=None):
     """Write rows of k_src, v_src [B,H_kv,n,d] to tokens [t0, t0 + n) of an 8-bit cache; see sparvar.h."""
     lib = load_library()
+    _whole("t0", t0)
     B, H_kv, n, d = k_src.shape
     stride, dev = _kv_planes(k_src, v_src)
     _check_q8(q8, B, H_kv, d, dev)
@@ -699,6 +708,7 @@ def sparvar_kv_quantize(k_src, v_src, t0, q8, stream=None):
 def sparvar_kv_dequantize(q8, t0, k_dst, v_dst, stream=None):
     """Read tokens [t0, t0 + n) of an 8-bit cache back to k_dst, v_dst [B,H_kv,n,d]; see sparvar.h."""
     lib = load_library()
+    _whole("t0", t0)
     B, H_kv, n, d = k_dst.shape
     stride, dev = _kv_planes(k_dst, v_dst)
     _check_q8(q8, B, H_kv, d, dev)
@@ -709,6 +719,7 @@ def sparvar_kv_dequantize(q8, t0, k_dst, v_dst, stream=None):
 
 def sparvar_dense_attn_q8_workspace(B, H, H_kv, n_q, n_kv, d):
     """Bytes of workspace with which a dense call of these sizes cuts its keys into parts (0: it does not)."""
+    _whole("sizes", B, H, H_kv, n_q, n_kv, d)
     n = load_library().sparvar_dense_attn_q8_workspace(B, H, H_kv, n_q, n_kv, d)
     if n < 0:
         _check(int(n))
@@ -717,6 +728,7 @@ def sparvar_dense_attn_q8_workspace(B, H, H_kv, n_q, n_kv, d):
 
 def sparvar_dense_attn_q8_form(B, H, H_kv, n_q, n_kv, d, workspace):
     """(waves, sets, parts) that a dense call of these sizes walks with, with a workspace or without; see sparvar.h."""
+    _whole("sizes", B, H, H_kv, n_q, n_kv, d)
     form = (ctypes.c_int32 * 3)()
     _check(load_library().sparvar_dense_attn_q8_form(B, H, H_kv, n_q, n_kv, d, int(workspace), form))
     return tuple(form)
@@ -737,6 +749,7 @@ def sparvar_dense_attn_q8_fwd(q, q8, n_kv, o, lse=None, kv_len=None, softmax_sca
     """Dense attention over the first n_kv tokens (kv_len[b] of them, int32, for entry b) of an 8-bit cache; workspace: a
     contiguous tensor of at least sparvar_dense_attn_q8_workspace() bytes, or None; see sparvar.h."""
     lib = load_library()
+    _whole("n_kv", n_kv)
     B, H, n_q, d = q.shape
     dt = _q8_attn(q, q8, o, lse, kv_len, workspace)
     if kv_len is not None:
@@ -756,6 +769,7 @@ def sparvar_block_sparse_attn_q8_fwd(geom, k, q_k, q8, o, row_ptr, col_idx, lse=
                                      stream=None):
     """Block-sparse attention of scale-k queries over the kept blocks of an 8-bit cache; see sparvar.h."""
     lib = load_library()
+    _whole("k", k)
     B, H, n, d = q_k.shape
     if 1 <= k <= len(geom.h) and n != geom.h[k - 1] * geom.w[k - 1]:
         raise SparvarError(ERR_INVALID, f"q_k has {n} rows, scale {k} has {geom.h[k - 1] * geom.w[k - 1]} tokens")
@@ -771,6 +785,7 @@ def sparvar_block_sparse_attn_q8_fwd(geom, k, q_k, q8, o, row_ptr, col_idx, lse=
 
 def sparvar_block_sparse_attn_q8_form(geom, k, B, H, H_kv, d):
     """(waves, parts of a row) that a block-sparse call of these sizes walks with; see sparvar.h."""
+    _whole("sizes", k, B, H, H_kv, d)
     form = (ctypes.c_int32 * 2)()
     _check(load_library().sparvar_block_sparse_attn_q8_form(geom.ref, k, B, H, H_kv, d, form))
     return tuple(form)
