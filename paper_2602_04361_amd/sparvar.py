@@ -771,12 +771,21 @@ def sparvar_block_sparse_attn_q8_fwd(geom, k, q_k, q8, o, row_ptr, col_idx, lse=
     lib = load_library()
     _whole("k", k)
     B, H, n, d = q_k.shape
-    if 1 <= k <= len(geom.h) and n != geom.h[k - 1] * geom.w[k - 1]:
-        raise SparvarError(ERR_INVALID, f"q_k has {n} rows, scale {k} has {geom.h[k - 1] * geom.w[k - 1]} tokens")
-    dt = _q8_attn(q_k, q8, o, lse, row_ptr, col_idx, schedule)
+    if not 1 <= k <= len(geom.h):
+        raise SparvarError(ERR_INVALID, f"scale {k} outside [1, {len(geom.h)}]")
+    h, w, e = geom.h[k - 1], geom.w[k - 1], geom.block_edge
+    if n != h * w:
+        raise SparvarError(ERR_INVALID, f"q_k has {n} rows, scale {k} has {h * w} tokens")
     i32 = _torch().int32
     if row_ptr.dtype != i32 or col_idx.dtype != i32 or (schedule is not None and schedule.dtype != i32):
         raise SparvarError(ERR_INVALID, "row_ptr, col_idx and schedule must be int32")
+    # (what row_ptr holds is device data: rows that end past col_idx are the caller's)
+    rows = B * H * -(-h // max(1, min(h, e))) * -(-w // max(1, min(w, e)))
+    if row_ptr.numel() <= rows or not row_ptr.is_contiguous() or not col_idx.is_contiguous():
+        raise SparvarError(ERR_INVALID, f"row_ptr must hold {rows + 1} entries, and it and col_idx must be contiguous")
+    if schedule is not None and (schedule.numel() < rows or not schedule.is_contiguous()):
+        raise SparvarError(ERR_INVALID, f"schedule must hold {rows} entries and be contiguous")
+    dt = _q8_attn(q_k, q8, o, lse, row_ptr, col_idx, schedule)
     _check(lib.sparvar_block_sparse_attn_q8_fwd(geom.ref, k, B, H, q8.H_kv, d, dt, _ptr(q_k), _plane_stride(q_k, "q_k"),
                                                 q8.ref, _ptr(o), _ptr(lse), _scale(softmax_scale, d), _ptr(row_ptr),
                                                 _ptr(col_idx), _ptr(schedule), _stream(stream)))

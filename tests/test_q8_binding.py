@@ -28,3 +28,19 @@ def test_numbers_past_32_bits(extra):
     refused("32 bits", sv.sparvar_dense_attn_q8_workspace, 1, 2, 2, 1, 64 + extra, 64)
     refused("32 bits", sv.sparvar_dense_attn_q8_form, 1, 2, 2, 64 + extra, 64, 64, True)
     refused("32 bits", sv.sparvar_block_sparse_attn_q8_form, g, 1, 1 + extra, 2, 2, 64)
+
+
+def test_rows_of_a_block_sparse_call():
+    """row_ptr of too few rows, strided arrays, a short launch order: the kernel would read past them."""
+    k, c = planes(), sv.Q8Cache.empty(1, 2, 64, 64, 32, device="cpu")
+    g, o = sv.Geometry([8], [8], 4, 0), torch.empty_like(planes())  # 2 planes of 4 tiles
+    ptr, ids, order = (torch.zeros(n, dtype=torch.int32) for n in (9, 20, 8))
+    call = sv.sparvar_block_sparse_attn_q8_fwd
+    refused("row_ptr", call, g, 1, k, c, o, ptr[:8], ids)
+    refused("row_ptr", call, g, 1, k, c, o, torch.zeros(18, dtype=torch.int32)[::2], ids)
+    refused("contiguous", call, g, 1, k, c, o, ptr, torch.zeros(40, dtype=torch.int32)[::2])
+    refused("schedule", call, g, 1, k, c, o, ptr, ids, schedule=order[:7])
+    refused("schedule", call, g, 1, k, c, o, ptr, ids, schedule=torch.zeros(16, dtype=torch.int32)[::2])
+    refused("int32", call, g, 1, k, c, o, ptr.long(), ids)
+    refused("scale 2", call, g, 2, k, c, o, ptr, ids)
+    refused("not on a GPU", call, g, 1, k, c, o, ptr, ids, schedule=order)  # these are right
