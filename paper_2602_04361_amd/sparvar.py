@@ -562,6 +562,11 @@ def _same(name, t, shape, dtype):
         raise SparvarError(ERR_INVALID, f"{name} must be a contiguous {list(shape)} tensor")
 
 
+def _check_block(block):
+    if block not in (16, 32, 64, 128):
+        raise SparvarError(ERR_INVALID, f"scale block {block} is not 16, 32, 64 or 128")
+
+
 class Q8Cache:
     """Host-side sparvar_q8_cache_t over device tensors: codes k, v [B,H_kv,capacity,d] (float8_e4m3fn, or their bytes as
     uint8) and scale bytes k_scale, v_scale [B,H_kv,ceil(capacity / block)] (uint8 or float8_e8m0fnu)."""
@@ -573,8 +578,7 @@ class Q8Cache:
                                ("v_scale", v_scale, (torch.uint8, torch.float8_e8m0fnu))):
             if t.dtype not in types:
                 raise SparvarError(ERR_UNSUPPORTED, f"{name} is {t.dtype}")
-        if block not in (16, 32, 64, 128):
-            raise SparvarError(ERR_INVALID, f"scale block {block} is not 16, 32, 64 or 128")
+        _check_block(block)
         self.bh_stride = _plane_stride(k, "k")
         self.B, self.H_kv, self.capacity, self.d = k.shape
         if k.shape != v.shape or _plane_stride(v, "v") != self.bh_stride:
@@ -595,6 +599,9 @@ class Q8Cache:
     def empty(cls, B, H_kv, capacity, d, block=64, device="cuda"):
         """A cache of unwritten tokens."""
         torch = _torch()
+        _check_block(block)
+        if min(B, H_kv, capacity, d) < 1:
+            raise SparvarError(ERR_INVALID, f"a cache of [{B},{H_kv},{capacity},{d}] is empty")
         code = dict(dtype=torch.float8_e4m3fn, device=device)
         scale = dict(dtype=torch.uint8, device=device)
         blocks = -(-capacity // block)

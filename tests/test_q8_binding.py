@@ -44,3 +44,10 @@ def test_rows_of_a_block_sparse_call():
     refused("int32", call, g, 1, k, c, o, ptr.long(), ids)
     refused("scale 2", call, g, 2, k, c, o, ptr, ids)
     refused("not on a GPU", call, g, 1, k, c, o, ptr, ids, schedule=order)  # these are right
+
+
+@pytest.mark.parametrize("bad", [dict(block=0), dict(block=-16), dict(block=48), dict(capacity=0), dict(capacity=-5),
+                                 dict(B=0), dict(H_kv=0)])
+def test_empty_cache_of_bad_sizes(bad):
+    """An error of the framework's own, before anything is allocated."""
+    refused("scale block|is empty", sv.Q8Cache.empty, **{**dict(B=1, H_kv=2, capacity=64, d=64, block=32, device="cpu"), **bad})
