@@ -885,14 +885,17 @@ struct DenseQ8Plan {
 // 128, us by the forms with few, 4 and 8 waves: 2 x 16 heads, 256 x 521 keys 9.1 / 15.6 / 22.5,
 // 400 x 921 16.8 / 21.7 / 31.4, 1024 x 2521 64 / 49.6 / 70, 1600 x 4121 158 / 119.7 / 115.2,
 // 2304 x 6425 314 / 277 / 342, 4096 x 10521 - / 612 / 592; 8 heads, 1024 x 2521 21.3 / 46.8 /
-// 70. Sets are for launches of up to a workgroup a CU, which then has two waves a SIMD. Two sets
-// of four waves against one: 256 workgroups of 10521 keys 160 / 174 (d = 64 104 / 124), 192 of
-// 5575 80.5 / 95, 256 of 2521 46.0 / 49.6; 384 workgroups 297 / 282. Four sets of two against the
-// best of the others: d = 64, 16 heads, 646 x 2755 20.3 / 22.9, 1024 x 2521 19.7 / 22.6, d = 128,
-// 12 heads, 1024 x 2521 28.2 / 30.8; 8 heads, 1024 x 2521 28.0 / 21; without a workspace, 4 heads,
-// 4096 x 10521 96.6 / 114 (90 in four parts of the others). One token of 8 heads, 10521 keys of
-// one head: 281 us in one part, 11.5 in 21, 13.7 in 83; one token of 4 x 32 heads, up to 42521
-// keys of 8 heads: 76.8 in 8 parts, 58.4 in 16, 62.2 in 32.
+// 70. Sets are for launches of up to a workgroup a CU, which then has two waves a SIMD, and for no
+// larger ones, where the other forms beat their estimate (d = 128, by four sets of two and by
+// what is taken now: 2304 x 6425, 2 x 16 heads 329 / 281, 8 heads 178 / 157, 2 x 12 heads, 1600 x
+// 4121 123 / 105; d = 64, 12 heads, 4096 x 10521 184 / 190). Two sets of four waves against one:
+// 256 workgroups of 10521 keys 160 / 174 (d = 64 104 / 124), 192 of 5575 80.5 / 95, 256 of 2521
+// 46.0 / 49.6; 384 workgroups 297 / 282. Four sets of two against the best of the others: d = 64,
+// 16 heads, 646 x 2755 20.3 / 22.9, 1024 x 2521 19.7 / 22.6, d = 128, 12 heads, 1024 x 2521 28.2 /
+// 30.8; 8 heads, 1024 x 2521 28.0 / 21; without a workspace, 4 heads, 4096 x 10521 96.6 / 114 (90
+// in four parts of the others). One token of 8 heads, 10521 keys of one head: 281 us in one part,
+// 11.5 in 21, 13.7 in 83; one token of 4 x 32 heads, up to 42521 keys of 8 heads:
+// 76.8 in 8 parts, 58.4 in 16, 62.2 in 32.
 struct DenseForm {
   int waves, sets;
   float f0, f, a, c;
@@ -913,6 +916,7 @@ DenseQ8Plan dense_plan(int32_t planes, int32_t group, int32_t n_q, int32_t n_kv,
   for (const DenseForm& f : kDenseForms[d == 128]) {
     const int64_t per = f.waves ? 32 * f.waves : 32, slabs = (rows + per - 1) / per, items = planes * slabs;
     auto consider = [&](int64_t parts) {
+      if (f.sets > 1 && items > num_cu) return;
       if (parts > 1 && (!may_split || f.sets > 1 || parts > chunks || parts > kMostParts)) return;
       const float m = (float)((items * parts + num_cu - 1) / num_cu), even = (float)(items * parts) / (float)num_cu;
       const float walk = (float)((chunks + parts * f.sets - 1) / (parts * f.sets)) * (f.a + f.c * m);

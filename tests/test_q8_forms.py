@@ -129,3 +129,19 @@ def test_sparse_form(form, d, sizes, order):
     note(f"[q8 forms] sparse {form} d={d} {sizes} order={order}")
     assert sv.sparvar_block_sparse_attn_q8_form(sv.Geometry(h, w, b, 1), k, B, H, Hkv, d) == form
     run_sparse(h, w, b, k, B, H, Hkv, d, G, seed=d + b + sum(w), empty=(0, 3, 8), order=order)
+
+
+def test_sets_are_for_launches_of_up_to_a_workgroup_a_cu():
+    """In larger ones the other forms are faster; the estimate alone took sets for 1152 workgroups (36 slabs of 64 rows of 32
+    planes: 329 us, 281 by slabs of 128 in parts)."""
+    taken = set()
+    for B, H in ((1, 4), (1, 8), (1, 16), (2, 6), (2, 8), (2, 12), (2, 16)):
+        for d in (64, 128):
+            for nq, nkv in ((400, 921), (1024, 2521), (1093, 4545), (1382, 4020), (1600, 4121), (2304, 6425), (2563, 9290),
+                            (3024, 8955), (3493, 8877), (4096, 10521)):
+                for ws in (False, True):
+                    waves, sets, _ = sv.sparvar_dense_attn_q8_form(B, H, H, nq, nkv, d, ws)
+                    if sets > 1:
+                        assert B * H * -(-nq // (32 * waves)) <= 256, (B, H, d, nq, nkv, ws)
+                        taken.add((waves, sets))
+    assert taken == {(4, 2), (2, 4)}
