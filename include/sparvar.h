@@ -559,7 +559,8 @@ typedef struct sparvar_norm_rope {
  *   k_cache, v_cache: [B,H_kv,>= t0+n,d] of `dtype`, plane stride cache_bh_stride,
  *   or NULL and q8 an 8-bit cache (exactly one of the two).
  *   heads (nullable): neither norm nor rotation. table_rows >= t0 + n.
- * No output may overlap an input. |x| below 2^60 (sums of squares in 32 bits).
+ * No output may overlap an input. Sums of squares in 32 bits: |x| below 2^60, and
+ * where eps is below 2^-60 (L2) or 2^-120 (RMS), rows of a norm above 2^-50.
  */
 int sparvar_qkv_append(int32_t B, int32_t H, int32_t H_kv, int32_t d, sparvar_dtype_t dtype, int32_t n,
                        int32_t t0, const void* q, int64_t q_batch_stride, int64_t q_token_stride,

@@ -10,11 +10,16 @@
 // same values would have. A lane loads 16 or 32 codes of V of one token, so of one scale.
 //
 // Large calls are bound by the matrix cores and the softmax's VALU work, which share the clock
-// that power allows: 4096 x 10521, 2 x 16 heads, d = 128: 559-592 us, 1.19-1.26 PFLOP/s, where a
-// large bf16 matrix product reaches 1.23-1.34; MFMA busy 57% of the cycles, no bank conflicts.
+// that power allows: 4096 x 10521, 2 x 16 heads, d = 128: 582-611 us, 1.16-1.21 PFLOP/s, where a
+// large bf16 matrix product reaches 1.23-1.37; MFMA busy 58% of the cycles, no bank conflicts.
 // (With K converted to bf16 in LDS as well 633-677 us; with the waves in two groups a phase
-// apart, products beside softmax, 575 where this one takes 592: not kept.) Few rows against a
+// apart, products beside softmax, 575 where this one took 592: not kept.) Few rows against a
 // long cache are bound by memory: 4.8 TB/s.
+//
+// Scores, maxima, sums and O are held in 32 bits. The probabilities are rounded to bf16 for the
+// product with V, each off by at most 2^-8 of itself, as in the bf16 kernels (the sum that
+// divides them is that of the 32-bit ones): outputs are off by 0.0023 of their size against 64
+// bits, 0.0017 of that the rounding of the outputs themselves.
 #include "attn_chunk.h"
 #include "attn_sources.h"
 #include "q8.h"

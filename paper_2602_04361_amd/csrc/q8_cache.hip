@@ -5,7 +5,9 @@
 // operations an element (keys to codes take more, and show it). 2 x 16 heads of 128, bf16:
 // append of 4096 tokens to a bf16 cache 44 us, 4.6 TB/s (a large copy reaches 4.8), to an 8-bit
 // cache 46 us, 3.6 TB/s; 10521 tokens to codes 48 us, 5.4 TB/s; 2521 tokens back 10 us, 6.1 TB/s
-// (the last-level cache holds them). A single token is launch latency, 10 us a call. A row of d channels is held by d / 8 lanes of 8 channels,
+// (the last-level cache holds them). From 32 bits, 4096 tokens to a 32-bit cache 81 us, to an
+// 8-bit one 62, 10521 tokens to codes 79, back 75: 4.9 to 5.7 TB/s. A single token is the cost of
+// a call, 9 us, 5 of them the kernel. A row of d channels is held by d / 8 lanes of 8 channels,
 // so that a row's sum of squares is a few exchanges inside a wave and both channels
 // of a rotation pair sit in one lane: lane u of a row has channels [8u, 8u + 8) where
 // pairs are neighbours and [4u, 4u + 4) and d/2 + [4u, 4u + 4) where they are halves
