@@ -10,8 +10,9 @@
 // same values would have. A lane loads 16 or 32 codes of V of one token, so of one scale.
 //
 // Large calls are bound by the matrix cores and the softmax's VALU work, which share the clock
-// that power allows: 4096 x 10521, 2 x 16 heads, d = 128: 582-611 us, 1.16-1.21 PFLOP/s, where a
-// large bf16 matrix product reaches 1.23-1.37; MFMA busy 58% of the cycles, no bank conflicts.
+// that power allows: 4096 x 10521, 2 x 16 heads, d = 128: 557-611 us from card to card, 1.16-1.27
+// PFLOP/s, where a large bf16 matrix product reaches 1.23-1.37; MFMA busy 58% of the cycles, no
+// bank conflicts.
 // (With K converted to bf16 in LDS as well 633-677 us; with the waves in two groups a phase
 // apart, products beside softmax, 575 where this one took 592: not kept.) Few rows against a
 // long cache are bound by memory: 4.8 TB/s.
