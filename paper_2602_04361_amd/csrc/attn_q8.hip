@@ -21,227 +21,19 @@
 // product with V, each off by at most 2^-8 of itself, as in the bf16 kernels (the sum that
 // divides them is that of the 32-bit ones): outputs are off by 0.0023 of their size against 64
 // bits, 0.0017 of that the rounding of the outputs themselves.
-#include "attn_chunk.h"
-#include "attn_sources.h"
+#include "attn_codes.h"
 #include "q8.h"
 
 namespace sparvar {
 
 namespace {
 
-struct Q8IO {
-  const bf16_bits* q;
-  bf16_bits* o;
-  float* lse;
-  int64_t q_bh_stride;
+struct Q8IO : RowsIO {
   Q8View c;
-  int32_t o_rows;   // rows of an output plane
-  int32_t n_items;  // workgroups doing work
-  int32_t swizzle;
-  float scale_log2;
-  float* part_o;    // dense calls in parts: [part, row, D] unnormalised sums, and
-  float2* part_ml;  // [part, row] maximum (exp2 domain) and sum
-  int32_t rows;     // rows of all output planes
 };
-
-// Dense calls: the rows of the query heads that share a key head, head after head, cut
-// into slabs; the keys of a batch entry in `parts` runs of whole chunks.
 template <int KC>
-struct DenseQ8Src {
-  static constexpr bool kSparse = false;
-  int32_t n_q, n_kv, H_kv, group, slabs, q_per_wg, parts;
-  const int32_t* kv_len;
-  template <int NT>
-  static constexpr int table_bytes() { return 16; }
-  __device__ __forceinline__ int32_t part_of(int32_t item) const { return (item / slabs) % parts; }
-  __device__ __forceinline__ QuerySet queries(int32_t item, int wave) const {
-    QuerySet s;
-    s.bh = item / (slabs * parts);  // plane of keys
-    s.qbase = 0;
-    s.qnc = n_q;
-    s.qstride = 0;
-    const int32_t q0 = item % slabs * q_per_wg, rows = group * n_q;
-    s.q1 = q0 + q_per_wg < rows ? q0 + q_per_wg : rows;
-    s.q0 = q0 + wave * kQPerWave;
-    return s;
-  }
-  __device__ __forceinline__ int32_t kv_plane(const QuerySet& s) const { return s.bh; }
-  __device__ __forceinline__ void place(const QuerySet& s, int32_t i, int32_t& plane, int32_t& row) const {
-    const int32_t h = i / n_q;
-    plane = s.bh * group + h;
-    row = i - h * n_q;
-  }
-  __device__ __forceinline__ DenseCursor<KC> cursor(int32_t item, const QuerySet& s) const {
-    int32_t n = n_kv;
-    if (kv_len) {
-      const int32_t len = kv_len[s.bh / H_kv];
-      n = len < 0 ? 0 : (len < n_kv ? len : n_kv);
-    }
-    const int32_t per = ((n + KC - 1) / KC + parts - 1) / parts * KC, first = part_of(item) * per;
-    return DenseCursor<KC>{first, first + per < n ? first + per : n};
-  }
-};
-
-// Chunks of a CSR row whose blocks are packed: the row's tokens, block after block, cut every 64.
-// A block cut at its scale's edge (24 tokens of an 8 x 8 block, say) then takes no more room in a
-// chunk than it has tokens, where the block table of the bf16 kernels gives it a chunk: block
-// sparse 48 x 36, d = 64, 83% of whose table's slots held a token, 30.5 -> 27.5 us, 32 x 18 with
-// 54% 15.7 -> 12.5, 64 x 64 with 98% 120.3 -> 121.4. tok is the token of the lane's slot (the
-// last one's past count).
-struct PackedChunk {
-  uint32_t tok;
-  int32_t count;
-};
-
-// Token of slot base + step, base the lane's and step the same for all: as one instruction, so that
-// no register holds a slot (base is taken again at each load: the compiler would keep every sum).
-__device__ __forceinline__ int32_t slot_base(const Chunk&, int32_t slot) { return slot; }
-__device__ __forceinline__ uint32_t token_at(const Chunk& c, int32_t base, int32_t step) {
-  return (uint32_t)chunk_token(c, chunk_slot(base + step, c.count));
-}
-__device__ __forceinline__ int32_t slot_base(const PackedChunk&, int32_t slot) {
-  int32_t b = slot * 4;
-#if defined(__HIP_DEVICE_COMPILE__)
-  asm volatile("" : "+v"(b));
-#endif
-  return b;
-}
-__device__ __forceinline__ uint32_t token_at(const PackedChunk& c, int32_t base, int32_t step) {
-  return (uint32_t)__builtin_amdgcn_ds_bpermute(base + step * 4, (int32_t)c.tok);
-}
-
-// Where the blocks of a fill stand: for each that has tokens {first token, first position,
-// width of its scale << 8 | its own width, ceil(2^20 / its width)}, and the positions apart.
-template <int NT>
-struct PackedLds {  // byte offsets
-  static constexpr int kInfo = 0;
-  static constexpr int kStart = kInfo + NT * 16;
-  static constexpr int kWt = kStart + (NT + 1) * 4 + 12;
-  static constexpr int kGeo = kWt + 16 * 4;
-  static constexpr int kBytes = kGeo + (int)((sizeof(GeoTable) + 15) / 16 * 16);
-};
-
-template <int NT>
-struct PackedCursor {
-  using L = PackedLds<NT>;
-  static constexpr int kGroup = NT < 512 ? NT : 511;  // entries of a fill: their count in 9 bits, their tokens in 22
-  const int32_t* col;
-  int32_t nb, pos, end;       // ids below nb are blocks; entries of the row not yet decoded
-  int32_t n, total;           // blocks and tokens of this fill
-  int32_t blk, at, stop;      // block of the wave's next position, that position, the end of its part
-  char* lds;
-
-  __device__ __forceinline__ bool more() const { return pos < end; }
-
-  // Decodes the next kGroup entries, a thread each (false: none left). Entries that are no blocks
-  // are left out, so that no two blocks share a position.
-  __device__ __forceinline__ bool fill() {
-    int4* info = reinterpret_cast<int4*>(lds + L::kInfo);
-    int32_t* start = reinterpret_cast<int32_t*>(lds + L::kStart);
-    const GeoTable& G = *reinterpret_cast<const GeoTable*>(lds + L::kGeo);
-    const int tid = fresh_tid();
-    total = 0;
-    while (pos < end && total == 0) {
-      __syncthreads();
-      const int32_t v = tid < kGroup && pos + tid < end ? col[pos + tid] : -1;
-      Tile t{0, 0, 1, 1};
-      if (v >= 0 && v < nb) t = block_tile(G, v);
-      const int32_t size = t.nr * t.nc;  // at most 4096
-      int32_t sum;
-      const int32_t before = block_excl_scan<NT>(size > 0 ? 1 << 22 | size : 0, reinterpret_cast<int32_t*>(lds + L::kWt), sum);
-      n = __builtin_amdgcn_readfirstlane((uint32_t)sum >> 22);
-      total = __builtin_amdgcn_readfirstlane(sum & 0x3fffff);
-      // (last blocks first: the full blocks of late scales then begin on a chunk's first slot, and
-      // most chunks hold one; 64 x 64 127 us with the few tokens of the first scales in front)
-      if (size > 0) {
-        const int32_t i = n - 1 - (before >> 22), first = total - size - (before & 0x3fffff);
-        info[i] = make_int4(t.base, first, t.stride << 8 | t.nc, ((1 << 20) + t.nc - 1) / t.nc);
-        start[i] = first;
-      }
-      if (tid == 0) start[n] = total;
-      __syncthreads();
-      pos += kGroup;
-    }
-    blk = 0;
-    at = 0;
-    stop = total;
-    return total > 0;
-  }
-
-  __device__ __forceinline__ int32_t take_part(int s, int ks) {
-    const int32_t* start = reinterpret_cast<const int32_t*>(lds + L::kStart);
-    const int32_t per = ((total + 63) / 64 + ks - 1) / ks;
-    at = s * per * 64;
-    stop = at + per * 64 < total ? at + per * 64 : total;
-    if (at < total) {
-      int32_t upto = 0;
-      for (int32_t i = 0; i < n; i += 64) {
-        const int32_t j = i + (fresh_tid() & 63);
-        upto += __builtin_popcountll(__builtin_amdgcn_ballot_w64(j < n && start[j < n ? j : n] <= at));
-      }
-      blk = upto - 1;
-    }
-    return per;
-  }
-
-  __device__ __forceinline__ bool next(PackedChunk& c) {
-    if (at >= stop) return false;
-    const int lane = fresh_tid() & 63;
-    const int4* info = reinterpret_cast<const int4*>(lds + L::kInfo);
-    const int32_t* start = reinterpret_cast<const int32_t*>(lds + L::kStart);
-    c.count = stop - at < 64 ? stop - at : 64;
-    // the blocks that begin inside the chunk, at most 63
-    const int32_t s = start[blk + 1 + lane < n ? blk + 1 + lane : n];
-    const int32_t inside = __builtin_popcountll(__builtin_amdgcn_ballot_w64(blk + 1 + lane < n && s < at + c.count));
-    int32_t own = blk;
-    for (int32_t i = 0; i < inside; ++i) own += at + lane >= __builtin_amdgcn_readlane(s, i) ? 1 : 0;
-    const int4 b = info[own];
-    const uint32_t r = (uint32_t)(at + lane - b.y);
-    const uint32_t q = __umul24(r, (uint32_t)b.w) >> 20;  // r / width: r < 4096, width <= 64
-    c.tok = (uint32_t)b.x + r + __umul24(q, (uint32_t)((b.z >> 8) - (b.z & 0xff)));
-    if (c.count < 64) c.tok = lane < c.count ? c.tok : (uint32_t)__builtin_amdgcn_readlane(c.tok, c.count - 1);
-    at += 64;
-    blk += inside + (__builtin_amdgcn_readlane(s, inside) <= at && blk + 1 + inside < n ? 1 : 0);
-    return true;
-  }
-};
-
-// Restricts a walk to part s of ks; returns the chunks of the longest part.
-template <int NT>
-__device__ __forceinline__ int32_t take_part(PackedCursor<NT>& c, int s, int ks) { return c.take_part(s, ks); }
-template <int KC>
-__device__ __forceinline__ int32_t take_part(DenseCursor<KC>& c, int s, int ks) {
-  const int32_t chunks = c.n > c.pos ? (c.n - c.pos + KC - 1) / KC : 0, per = (chunks + ks - 1) / ks;
-  c.pos += s * per * KC;
-  c.n = c.pos + per * KC < c.n ? c.pos + per * KC : c.n;
-  return per;
-}
-
-struct SparseQ8Src : SparseSrc<64> {
-  int32_t group;
-  template <int NT>
-  static constexpr int table_bytes() { return PackedLds<NT>::kBytes; }
-  template <int NT>
-  __device__ __forceinline__ PackedCursor<NT> packed_cursor(int32_t item, char* lds) const {
-    const int32_t r = row_of(item);
-    PackedCursor<NT> c;
-    constexpr int kWords = (int)(sizeof(GeoTable) / 4);
-    const int32_t* from = reinterpret_cast<const int32_t*>(&G);  // (the first fill starts with a barrier)
-    for (int i = threadIdx.x; i < kWords; i += NT) reinterpret_cast<int32_t*>(lds + PackedLds<NT>::kGeo)[i] = from[i];
-    c.col = col_idx;
-    c.nb = G.NB[k];
-    c.pos = row_ptr[r];
-    c.end = row_ptr[r + 1];
-    c.lds = lds;
-    return c;
-  }
-  __device__ __forceinline__ int32_t part_of(int32_t) const { return 0; }
-  __device__ __forceinline__ int32_t kv_plane(const QuerySet& s) const { return s.bh / group; }
-  __device__ __forceinline__ void place(const QuerySet& s, int32_t i, int32_t& plane, int32_t& row) const {
-    plane = s.bh;
-    row = s.qbase + (i / s.qnc) * s.qstride + i % s.qnc;
-  }
-};
+struct DenseQ8Src : DenseRowsSrc<KC> {};
+struct SparseQ8Src : SparseRowsSrc {};
 
 // Which codes of a wave's 16 rows a lane loads and converts: four lanes take a row, 16 codes
 // each (col) and at D = 128 the 16 that lie 64 channels further, so that a token's address and
@@ -261,93 +53,6 @@ __device__ __forceinline__ void put_piece(char* at0, char* at1, const u32x4& raw
   *reinterpret_cast<u32x4*>(at0) = u32x4{w[0], w[1], w[2], w[3]};
   *reinterpret_cast<u32x4*>(at1) = u32x4{w[4], w[5], w[6], w[7]};
 }
-
-// Log of the softmax denominator, of a maximum in the exp2 domain and a sum: -inf where there were
-// no keys, and NaN where one scored NaN (a sum of NaN is no empty one).
-__device__ __forceinline__ float lse_of(float m, float l) {
-  return l == 0.f ? -INFINITY : (m + __builtin_log2f(l)) * kLn2;
-}
-
-// What a wave found for its rows: the part's unnormalised sums, maximum and sum, or the output.
-template <int D>
-__device__ __forceinline__ void store_rows(const Q8IO& io, const f32x16 (&acc)[D / 32], float m, float l, bool qvalid, int half,
-                                           int32_t plane, int32_t qrow, int32_t part) {
-  if (!qvalid) return;
-  const int64_t orow = (int64_t)plane * io.o_rows + qrow;
-  if (io.part_o) {
-    const int64_t prow = (int64_t)part * io.rows + orow;
-    float* op = io.part_o + prow * D;
-#pragma unroll
-    for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        *reinterpret_cast<float4*>(op + 32 * dt + 8 * j + 4 * half) =
-            make_float4(acc[dt][4 * j], acc[dt][4 * j + 1], acc[dt][4 * j + 2], acc[dt][4 * j + 3]);
-    if (half == 0) io.part_ml[prow] = make_float2(m, l);
-    return;
-  }
-  const float inv = l > 0.f ? 1.f / l : 0.f;
-  bf16_bits* op = io.o + orow * D;
-#pragma unroll
-  for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      uint2 w;
-      w.x = pack_bf16x2(acc[dt][4 * j] * inv, acc[dt][4 * j + 1] * inv);
-      w.y = pack_bf16x2(acc[dt][4 * j + 2] * inv, acc[dt][4 * j + 3] * inv);
-      *reinterpret_cast<uint2*>(op + 32 * dt + 8 * j + 4 * half) = w;
-    }
-  if (io.lse && half == 0) io.lse[orow] = lse_of(m, l);
-}
-
-// Query fragments for the products with K's codes: the row divided by a power of two (its
-// largest magnitude then in (224, 448]) as the sum of two e4m3 values. bf16 has 8 significant
-// bits and e4m3 4. What the larger part leaves is at most 16, so the smaller one is stored
-// times 2^4, under a scale byte of its own: its last place is 2^-13. The sum is the query itself
-// for elements from 2^-6 on, among them all from 2^-13 of the row's largest; below, it is off by
-// at most half that place, 2^-14 / 224 < 2^-21 of the largest. Rows of one channel of 100 beside
-// normals times 0.1, keys of normals times 4: the split alone, in exact sums, moves the LSE by
-// 3e-5 (without the 2^4 by 2e-3). The rate is that of one bf16 product (two e4m3 ones at twice
-// its rate), and K needs no conversion. Step t of a half covers channels 64 t + 32 half .. + 32,
-// as the K fragments do.
-typedef __attribute__((ext_vector_type(8))) int i32x8;
-
-template <int D>
-struct QFragF8 {
-  i32x8 hi[D / 64], lo[D / 64];
-  int32_t scale;  // E8M0 bytes: of hi, and above it of lo
-  __device__ __forceinline__ void load(const bf16_bits* row, int half) {
-    u32x4 raw[D / 16];
-    float top = 0.f;
-#pragma unroll
-    for (int t = 0; t < D / 64; ++t)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        raw[4 * t + i] = ldg16(row + 64 * t + 32 * half + 8 * i);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          top = fmaxf(top, fabsf(__uint_as_float(raw[4 * t + i][e] << 16)));
-          top = fmaxf(top, fabsf(__uint_as_float(raw[4 * t + i][e] & 0xffff0000u)));
-        }
-      }
-    const int32_t e2 = block_exponent(max_halves(top));
-    const float inv = pow2f(-e2);
-    scale = (e2 + 127) | (e2 + 123) << 8;
-#pragma unroll
-    for (int t = 0; t < D / 64; ++t)
-#pragma unroll
-      for (int w = 0; w < 8; ++w) {
-        const uint32_t a = raw[4 * t + w / 2][2 * (w & 1)], b = raw[4 * t + w / 2][2 * (w & 1) + 1];
-        const float x[4] = {__uint_as_float(a << 16) * inv, __uint_as_float(a & 0xffff0000u) * inv,
-                            __uint_as_float(b << 16) * inv, __uint_as_float(b & 0xffff0000u) * inv};
-        const uint32_t h = codes4(x[0], x[1], x[2], x[3]);
-        float y[4];
-        decode4(h, 1.f, y);
-        hi[t][w] = (int)h;
-        lo[t][w] = (int)codes4((x[0] - y[0]) * 16.f, (x[1] - y[1]) * 16.f, (x[2] - y[2]) * 16.f, (x[3] - y[3]) * 16.f);
-      }
-  }
-};
 
 // c += K Q^T over 64 channels: a the codes of 32 keys (scale byte ks of the lane's key). Of the
 // queries' scale, byte 0 goes with hi and byte 1 with lo.
@@ -370,49 +75,6 @@ __device__ __forceinline__ i32x8 two_units(u32x4 a, u32x4 b) {
 template <int D>
 __device__ __forceinline__ int code_swizzle(int r) {
   return D == 128 ? (r >> 1) & 7 : (r >> 2) & 3;
-}
-
-// V^T fragment of step ks2, channels 32 dt .. of a V tile (rows of D bf16 values).
-template <int D, int KC>
-struct VOffsets {
-  int off[2][D / 32];
-  __device__ __forceinline__ void init(int l32, int half, int lane) {
-    FragOffsets<D, KC> fo;
-    fo.init(l32, half, lane);
-#pragma unroll
-    for (int i = 0; i < D / 32; ++i) {  // (V alone, no K tile before it)
-      off[0][i] = fo.v_off[0][i] - KC * D * 2;
-      off[1][i] = fo.v_off[1][i] - KC * D * 2;
-    }
-  }
-  __device__ __forceinline__ bf16x8 read(const char* tile, int ks2, int dt) const {
-    const i16x4 lo = lds_read_tr(tile + off[0][dt] + ks2 * 16 * D * 2);
-    const i16x4 hi = lds_read_tr(tile + off[1][dt] + ks2 * 16 * D * 2);
-    u32x4 av;
-    av[0] = __builtin_bit_cast(uint32_t, __builtin_shufflevector(lo, lo, 0, 1));
-    av[1] = __builtin_bit_cast(uint32_t, __builtin_shufflevector(lo, lo, 2, 3));
-    av[2] = __builtin_bit_cast(uint32_t, __builtin_shufflevector(hi, hi, 0, 1));
-    av[3] = __builtin_bit_cast(uint32_t, __builtin_shufflevector(hi, hi, 2, 3));
-    return as_bf16x8(av);
-  }
-};
-
-// Softmax of a chunk of scores: masks past count, moves the running maximum when a row's grew
-// by more than 2^8 (the sums are rescaled then), and packs the probabilities.
-template <int D, int KC>
-__device__ __forceinline__ void softmax_chunk(f32x16 (&st)[KC / 32], int32_t count, int half, float scale_log2, float& m_run,
-                                              float& l_run, f32x16 (&acc)[D / 32], bf16x8 (&pf)[KC / 16]) {
-  if (count < KC) mask_tail<KC>(st, count, half);
-  const float mx = row_max<KC>(st, scale_log2);
-  if (__builtin_amdgcn_ballot_w64(mx > m_run + 8.f)) {
-    const float m_new = fmaxf(m_run, mx);
-    const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
-    l_run *= alpha;
-#pragma unroll
-    for (int i = 0; i < D / 32; ++i) acc[i] *= alpha;
-    m_run = m_new;
-  }
-  l_run += exp_pack<KC>(st, scale_log2, m_run, pf);
 }
 
 // QW waves of 32 queries walk the keys in chunks of 64, or (KS > 1) KS such sets, each a part of
@@ -655,14 +317,6 @@ __global__ __launch_bounds__(QW * KS * 64) __attribute__((amdgpu_waves_per_eu(2)
 // copy reaches 4.8); by the 64-key kernel with parts 91 us.
 constexpr int kRowWaves = 4;
 
-// LDS of one wave, written by some lanes and read by others: its instructions run in
-// order, so only the compiler has to keep them so.
-__device__ __forceinline__ void wave_fence() {
-#if defined(__HIP_DEVICE_COMPILE__)
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-#endif
-}
-
 template <int D>
 __global__ __launch_bounds__(kRowWaves * 64) __attribute__((amdgpu_waves_per_eu(2)))
 void attn_q8_rows_kernel(Q8IO io, DenseQ8Src<32> src) {
@@ -814,7 +468,7 @@ void attn_q8_rows_kernel(Q8IO io, DenseQ8Src<32> src) {
 // us with the launch). A whole call of 32768 rows of 64 channels in two parts takes 40 us that
 // way, 60 with a workgroup a row; 9040 rows in three 28.6 and 34.
 template <int D, bool ALL>
-__global__ __launch_bounds__(256) void join_parts_kernel(Q8IO io, int32_t parts) {
+__global__ __launch_bounds__(256) void join_parts_kernel(RowsIO io, int32_t parts) {
   constexpr int C = D / 4, P = 256 / C, side = ALL ? P : 1;
   __shared__ float4 sums[ALL ? P : 1][C];
   __shared__ float ls[P];
@@ -869,19 +523,12 @@ __global__ __launch_bounds__(256) void join_parts_kernel(Q8IO io, int32_t parts)
 }
 
 template <int D>
-hipError_t join_parts(const Q8IO& io, int32_t parts, int num_cu, hipStream_t stream) {
+hipError_t join_parts(const RowsIO& io, int32_t parts, int num_cu, hipStream_t stream) {
   constexpr int P = 1024 / D;  // rows of a workgroup, or threads of a row's channel group
   if (io.rows <= 8 * num_cu || parts > 8) hipLaunchKernelGGL((join_parts_kernel<D, true>), dim3(io.rows), dim3(256), 0, stream, io, parts);
   else hipLaunchKernelGGL((join_parts_kernel<D, false>), dim3((io.rows + P - 1) / P), dim3(256), 0, stream, io, parts);
   return hipGetLastError();
 }
-
-// The form of a dense call: waves of 32 rows in a workgroup (0: the kernel for few rows, 32 rows a
-// workgroup) and sets of them that share its keys, slabs of rows, parts of the keys.
-struct DenseQ8Plan {
-  int waves, sets;
-  int32_t slabs, parts;
-};
 
 // Expected time of a form, in us. With m workgroups on the busiest CU, which share it: f0 + f m
 // for starting and storing, and for every 64 keys of a part a + c m; at least what the codes
@@ -902,48 +549,15 @@ struct DenseQ8Plan {
 // in four parts of the others). One token of 8 heads, 10521 keys of one head: 281 us in one part,
 // 11.5 in 21, 13.7 in 83; one token of 4 x 32 heads, up to 42521 keys of 8 heads:
 // 76.8 in 8 parts, 58.4 in 16, 62.2 in 32.
-struct DenseForm {
-  int waves, sets;
-  float f0, f, a, c;
-};
 constexpr DenseForm kDenseForms[2][5] = {
     // d = 64, d = 128
     {{0, 1, 3.f, .6f, .05f, .20f}, {2, 4, 2.5f, 3.f, 0.f, 1.38f}, {4, 1, 3.f, 1.3f, .2f, .53f}, {4, 2, 4.5f, 4.4f, 0.f, 1.15f},
      {8, 1, 4.f, 4.4f, 0.f, 1.12f}},
     {{0, 1, 2.f, 2.2f, .15f, .35f}, {2, 4, 5.f, 4.5f, 0.f, 1.92f}, {4, 1, 3.5f, 3.f, .3f, .92f}, {4, 2, 5.5f, 6.f, 0.f, 1.8f},
      {8, 1, 5.f, 6.f, 0.f, 1.77f}}};
-constexpr int kMostParts = 128;
-
-DenseQ8Plan dense_plan(int32_t planes, int32_t group, int32_t n_q, int32_t n_kv, int32_t d, int num_cu, bool may_split) {
-  const int64_t rows = (int64_t)group * n_q, chunks = ((int64_t)n_kv + 63) / 64;
-  const float memory = (float)planes * n_kv * d * (2.f / 5e6f);
-  DenseQ8Plan best{0, 1, 1, 1};
-  float best_us = INFINITY;
-  for (const DenseForm& f : kDenseForms[d == 128]) {
-    const int64_t per = f.waves ? 32 * f.waves : 32, slabs = (rows + per - 1) / per, items = planes * slabs;
-    auto consider = [&](int64_t parts) {
-      if (f.sets > 1 && items > num_cu) return;
-      if (parts > 1 && (!may_split || f.sets > 1 || parts > chunks || parts > kMostParts)) return;
-      const float m = (float)((items * parts + num_cu - 1) / num_cu), even = (float)(items * parts) / (float)num_cu;
-      const float walk = (float)((chunks + parts * f.sets - 1) / (parts * f.sets)) * (f.a + f.c * m);
-      const float read = memory * (m / even) * (1.f + .25f / m);
-      float us = f.f0 + f.f * m + (walk > read ? walk : read);
-      if (parts > 1) us += 3.f + .08f * parts + (float)parts * planes * rows * d * (8.f / 6e6f);
-      if (us < best_us) {
-        best_us = us;
-        best = DenseQ8Plan{f.waves, f.sets, (int32_t)slabs, (int32_t)parts};
-      }
-    };
-    // one part; growing numbers of parts while there is less than one workgroup a CU; whole
-    // workgroups a CU
-    for (int64_t parts = 1; parts == 1 || items * parts < num_cu; parts += parts < 4 ? 1 : parts / 4) consider(parts);
-    for (int64_t m = 1; m <= 8; ++m)
-      if (m * num_cu / items > 1) consider(m * num_cu / items);
-  }
-  return best;
+DensePlan dense_plan(int32_t planes, int32_t group, int32_t n_q, int32_t n_kv, int32_t d, int num_cu, bool may_split) {
+  return plan_dense(kDenseForms[d == 128], 2.f * d, planes, group, n_q, n_kv, d, num_cu, may_split);
 }
-
-int32_t padded_grid(const Q8IO& io) { return io.swizzle ? (io.n_items + 7) / 8 * 8 : io.n_items; }
 
 template <int D, int QW, int KS, class Src>
 hipError_t launch_one(const Q8IO& io, const Src& src, hipStream_t stream) {
@@ -951,23 +565,25 @@ hipError_t launch_one(const Q8IO& io, const Src& src, hipStream_t stream) {
   return hipGetLastError();
 }
 
-int64_t part_floats(int32_t parts, int64_t rows, int32_t d) { return (int64_t)parts * rows * (d + 2); }
-
 }  // namespace
 
+hipError_t launch_join_parts(const RowsIO& io, int32_t d, int32_t parts, int num_cu, hipStream_t stream) {
+  return d == 128 ? join_parts<128>(io, parts, num_cu, stream) : join_parts<64>(io, parts, num_cu, stream);
+}
+
 int64_t dense_q8_workspace(int32_t B, int32_t H, int32_t H_kv, int32_t n_q, int32_t n_kv, int32_t d, int num_cu) {
-  const DenseQ8Plan p = dense_plan(B * H_kv, H / H_kv, n_q, n_kv, d, num_cu, true);
+  const DensePlan p = dense_plan(B * H_kv, H / H_kv, n_q, n_kv, d, num_cu, true);
   return p.parts > 1 ? 4 * part_floats(p.parts, (int64_t)B * H * n_q, d) : 0;
 }
 
 Q8Form dense_q8_form(int32_t B, int32_t H, int32_t H_kv, int32_t n_q, int32_t n_kv, int32_t d, int num_cu, bool workspace) {
-  const DenseQ8Plan p = dense_plan(B * H_kv, H / H_kv, n_q, n_kv, d, num_cu, workspace);
+  const DensePlan p = dense_plan(B * H_kv, H / H_kv, n_q, n_kv, d, num_cu, workspace);
   return Q8Form{p.waves, p.sets, p.parts};
 }
 
 hipError_t launch_dense_attn_q8(const DenseQ8Args& a, hipStream_t stream) {
   const int32_t group = a.H / a.H_kv;
-  const DenseQ8Plan p = dense_plan(a.B * a.H_kv, group, a.n_q, a.n_kv, a.d, a.num_cu, a.workspace != nullptr);
+  const DensePlan p = dense_plan(a.B * a.H_kv, group, a.n_q, a.n_kv, a.d, a.num_cu, a.workspace != nullptr);
   Q8IO io;
   io.q = static_cast<const bf16_bits*>(a.q);
   io.o = static_cast<bf16_bits*>(a.o);
@@ -1008,7 +624,7 @@ hipError_t launch_dense_attn_q8(const DenseQ8Args& a, hipStream_t stream) {
 #undef SV_DENSE
   }
   if (e != hipSuccess || p.parts == 1) return e;
-  return a.d == 128 ? join_parts<128>(io, p.parts, a.num_cu, stream) : join_parts<64>(io, p.parts, a.num_cu, stream);
+  return launch_join_parts(io, a.d, p.parts, a.num_cu, stream);
 }
 
 Q8Form sparse_q8_form(const GeoTable& G, int32_t k, int32_t BH, int32_t d, int num_cu) {

@@ -139,6 +139,12 @@ struct Q8View {
   int32_t lg;
 };
 
+// A 4-bit cache: e2m1 codes, two a byte, and E8M0 scale bytes, one a token and 32 channels.
+struct Q4View {
+  uint8_t *k, *v, *ks, *vs;
+  int64_t bh_stride, sc_stride;  // bytes between planes of codes, of scales
+};
+
 struct HeadMap {  // norm, weight and rotation of query and key vectors
   int32_t norm, layout;
   float eps;
@@ -192,9 +198,10 @@ struct DenseQ8Args {
 // Bytes of workspace that a call of these sizes takes (0: it walks its keys in one part).
 int64_t dense_q8_workspace(int32_t B, int32_t H, int32_t H_kv, int32_t n_q, int32_t n_kv, int32_t d, int num_cu);
 hipError_t launch_dense_attn_q8(const DenseQ8Args& a, hipStream_t stream);
-struct Q8Form {
+struct CodesForm {
   int32_t waves, sets, parts;
 };
+using Q8Form = CodesForm;
 Q8Form dense_q8_form(int32_t B, int32_t H, int32_t H_kv, int32_t n_q, int32_t n_kv, int32_t d, int num_cu, bool workspace);
 
 struct SparseQ8Args {
@@ -213,6 +220,92 @@ struct SparseQ8Args {
 hipError_t launch_sparse_attn_q8(const SparseQ8Args& a, hipStream_t stream);
 // Waves of a tile and parts of a row (its sets) of a block-sparse call at scale k.
 Q8Form sparse_q8_form(const GeoTable& G, int32_t k, int32_t BH, int32_t d, int num_cu);
+
+struct KvQuantizeQ4Args {
+  int32_t planes, d, n, t0;
+  bool bf16;
+  const void *k, *v;
+  int64_t bh_stride;  // elements
+  Q4View c4;
+};
+hipError_t launch_kv_quantize_q4(const KvQuantizeQ4Args& a, hipStream_t stream);
+
+struct KvDequantizeQ4Args {
+  int32_t planes, d, n, t0;
+  bool bf16;
+  void *k, *v;
+  int64_t bh_stride;  // elements
+  Q4View c4;
+};
+hipError_t launch_kv_dequantize_q4(const KvDequantizeQ4Args& a, hipStream_t stream);
+
+struct DenseQ4Args {
+  int32_t B, H, H_kv, n_q, n_kv, d;
+  const void* q;
+  void* o;
+  float* lse;
+  int64_t q_bh_stride;
+  Q4View c4;
+  const int32_t* kv_len;
+  float softmax_scale;
+  float* workspace;  // nullable: one part
+  int swizzle;
+  int num_cu;
+};
+int64_t dense_q4_workspace(int32_t B, int32_t H, int32_t H_kv, int32_t n_q, int32_t n_kv, int32_t d, int num_cu);
+hipError_t launch_dense_attn_q4(const DenseQ4Args& a, hipStream_t stream);
+CodesForm dense_q4_form(int32_t B, int32_t H, int32_t H_kv, int32_t n_q, int32_t n_kv, int32_t d, int num_cu, bool workspace);
+
+struct SparseQ4Args {
+  const GeoTable* G;
+  int32_t k, BH, H, H_kv, d;
+  const void* q;
+  void* o;
+  float* lse;
+  int64_t q_bh_stride;
+  Q4View c4;
+  float softmax_scale;
+  const int32_t *row_ptr, *col_idx, *schedule;
+  int swizzle;
+  int num_cu;
+};
+hipError_t launch_sparse_attn_q4(const SparseQ4Args& a, hipStream_t stream);
+CodesForm sparse_q4_form(const GeoTable& G, int32_t k, int32_t BH, int32_t d, int num_cu);
+
+// Attention weight that each key of a cache got: w = decay * w_old + the sum over the queries of its
+// head group. Keys in 16 or 32 bits, or (k NULL) the codes of c4.
+struct KeyWeightsArgs {
+  int32_t B, H, H_kv, n_q, n_kv, n_old, d;
+  bool bf16;
+  const void *q, *k;
+  int64_t q_bh_stride, k_bh_stride;  // elements
+  Q4View c4;
+  const float* lse;
+  const int32_t* kv_len;
+  const float* w_old;
+  float* w;
+  int64_t w_bh_stride;
+  float softmax_scale, decay;
+  int num_cu;
+};
+hipError_t launch_key_weights(const KeyWeightsArgs& a, hipStream_t stream);
+
+// Tokens kept by weight, moved to a cache of their own. A row of the cache is `row` bytes of K and V
+// each and (4-bit caches) `srow` bytes of scales.
+struct KvEvictArgs {
+  int32_t B, H_kv, n, n_keep, n_first, n_last;
+  const int32_t* kv_len;
+  const float* w;
+  float* w_out;
+  int32_t* kept;
+  int64_t w_bh_stride, w_out_bh_stride;
+  int32_t row, srow;
+  const void *k_src, *v_src, *ks_src, *vs_src;
+  void *k_dst, *v_dst, *ks_dst, *vs_dst;
+  int64_t src_stride, dst_stride, ssrc_stride, sdst_stride;  // bytes between planes
+  int num_cu;
+};
+hipError_t launch_kv_evict(const KvEvictArgs& a, hipStream_t stream);
 
 // Work items of the bf16 block-sparse launch at scale k (with the default
 // waves, chunk and stages): one query tile per workgroup (gh = gw = 0), or groups

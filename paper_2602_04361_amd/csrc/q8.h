@@ -68,4 +68,55 @@ __device__ __forceinline__ void decode4_bf16(uint32_t w, float s, uint32_t& lo, 
 #endif
 }
 
+// Query fragments for the products with K's codes: the row divided by a power of two (its
+// largest magnitude then in (224, 448]) as the sum of two e4m3 values. bf16 has 8 significant
+// bits and e4m3 4. What the larger part leaves is at most 16, so the smaller one is stored
+// times 2^4, under a scale byte of its own: its last place is 2^-13. The sum is the query itself
+// for elements from 2^-6 on, among them all from 2^-13 of the row's largest; below, it is off by
+// at most half that place, 2^-14 / 224 < 2^-21 of the largest. Rows of one channel of 100 beside
+// normals times 0.1, keys of normals times 4: the split alone, in exact sums, moves the LSE by
+// 3e-5 (without the 2^4 by 2e-3). The rate is that of one bf16 product (two e4m3 ones at twice
+// its rate), and K needs no conversion. Step t of a half covers channels 64 t + 32 half .. + 32,
+// as K fragments of 8-bit codes do, or (MIXED: beside 4-bit codes, whose lanes hold the 32 channels of
+// one half in a row) the 16 from 64 t + 16 half on and the 16 from 32 further, where the instruction
+// looks for an 8-bit operand's.
+typedef __attribute__((ext_vector_type(8))) int i32x8;
+
+template <int D, bool MIXED = false>
+struct QFragF8 {
+  i32x8 hi[D / 64], lo[D / 64];
+  int32_t scale;  // E8M0 bytes: of hi, and above it of lo
+  __device__ __forceinline__ void load(const bf16_bits* row, int half) {
+    u32x4 raw[D / 16];
+    float top = 0.f;
+#pragma unroll
+    for (int t = 0; t < D / 64; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        raw[4 * t + i] = ldg16(row + 64 * t + (MIXED ? 16 * half + 8 * i + 16 * (i >> 1) : 32 * half + 8 * i));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          top = fmaxf(top, fabsf(__uint_as_float(raw[4 * t + i][e] << 16)));
+          top = fmaxf(top, fabsf(__uint_as_float(raw[4 * t + i][e] & 0xffff0000u)));
+        }
+      }
+    const int32_t e2 = block_exponent(max_halves(top));
+    const float inv = pow2f(-e2);
+    scale = (e2 + 127) | (e2 + 123) << 8;
+#pragma unroll
+    for (int t = 0; t < D / 64; ++t)
+#pragma unroll
+      for (int w = 0; w < 8; ++w) {
+        const uint32_t a = raw[4 * t + w / 2][2 * (w & 1)], b = raw[4 * t + w / 2][2 * (w & 1) + 1];
+        const float x[4] = {__uint_as_float(a << 16) * inv, __uint_as_float(a & 0xffff0000u) * inv,
+                            __uint_as_float(b << 16) * inv, __uint_as_float(b & 0xffff0000u) * inv};
+        const uint32_t h = codes4(x[0], x[1], x[2], x[3]);
+        float y[4];
+        decode4(h, 1.f, y);
+        hi[t][w] = (int)h;
+        lo[t][w] = (int)codes4((x[0] - y[0]) * 16.f, (x[1] - y[1]) * 16.f, (x[2] - y[2]) * 16.f, (x[3] - y[3]) * 16.f);
+      }
+  }
+};
+
 }  // namespace sparvar
