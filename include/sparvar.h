@@ -645,6 +645,123 @@ int sparvar_block_sparse_attn_q8_fwd(const sparvar_geometry_t* g, int32_t k, int
 int sparvar_block_sparse_attn_q8_form(const sparvar_geometry_t* g, int32_t k, int32_t B, int32_t H,
                                       int32_t H_kv, int32_t d, int32_t* form);
 
+/*
+ * ---- 4-bit key/value cache.
+ *
+ * A 4-bit cache holds K and V as e2m1 codes (1 + 2 + 1 bits: 0, 0.5, 1, 1.5, 2, 3,
+ * 4, 6 and their negatives), two a byte, the even channel in the low half, with one
+ * power-of-two scale for each token of a head and 32 channels, K and V apart:
+ * value = code * 2^(scale byte - 127) (E8M0 bytes). A group's exponent is the
+ * smallest e with max|x| <= 7 * 2^e, clamped to [-100, 112]; codes are x * 2^-e
+ * rounded to nearest even, what is above 6 becoming 6, so that no code is off by more
+ * than half the step at its place (magnitudes above 7 * 2^112 saturate, infinities
+ * too). A group that holds a NaN has the scale byte 255, and all of it is NaN. Every
+ * value is exact in bf16.
+ *
+ * Tokens do not depend on each other: rows may be written in any order and again.
+ * Calls that write one cache, or read what another writes, are ordered by the caller.
+ * The struct is host memory read during the call; its pointers are device memory.
+ */
+typedef struct sparvar_q4_cache {
+  int32_t capacity;        /* tokens a plane holds */
+  void* k;                 /* codes [B,H_kv,capacity,d/2] bytes, plane stride bh_stride */
+  void* v;
+  int64_t bh_stride;       /* >= capacity * d/2, a multiple of 16 */
+  uint8_t* k_scale;        /* E8M0 bytes [B,H_kv,capacity,d/32], d/32-byte aligned */
+  uint8_t* v_scale;
+  int64_t scale_bh_stride; /* >= capacity * d/32, a multiple of d/32 */
+} sparvar_q4_cache_t;
+
+/*
+ * Writes rows [0, n) of k_src and v_src ([B,H_kv,n,d] of `dtype`, plane stride
+ * src_bh_stride) to tokens [t0, t0 + n) of a 4-bit cache, and reads such tokens back
+ * to rows [0, n) of k_dst and v_dst (exact in both types). A step's rows come from
+ * sparvar_qkv_append with a 16-bit cache.
+ */
+int sparvar_kv_quantize_q4(int32_t B, int32_t H_kv, int32_t d, sparvar_dtype_t dtype, int32_t n, int32_t t0,
+                           const void* k_src, const void* v_src, int64_t src_bh_stride,
+                           const sparvar_q4_cache_t* q4, hipStream_t stream);
+int sparvar_kv_dequantize_q4(int32_t B, int32_t H_kv, int32_t d, sparvar_dtype_t dtype, int32_t n, int32_t t0,
+                             const sparvar_q4_cache_t* q4, void* k_dst, void* v_dst, int64_t dst_bh_stride,
+                             hipStream_t stream);
+
+/*
+ * sparvar_dense_attn_q8_fwd and its companions over a 4-bit cache: the same
+ * arguments, the same treatment of queries, lengths and workspaces, on the values
+ * that the codes stand for.
+ */
+int64_t sparvar_dense_attn_q4_workspace(int32_t B, int32_t H, int32_t H_kv, int32_t n_q, int32_t n_kv,
+                                        int32_t d); /* bytes, < 0 on error */
+int sparvar_dense_attn_q4_fwd(int32_t B, int32_t H, int32_t H_kv, int32_t n_q, int32_t n_kv, int32_t d,
+                              sparvar_dtype_t dtype, const void* q, int64_t q_bh_stride,
+                              const sparvar_q4_cache_t* q4, const int32_t* kv_len, void* o, float* lse,
+                              float softmax_scale, void* workspace, int64_t workspace_bytes,
+                              hipStream_t stream);
+int sparvar_dense_attn_q4_form(int32_t B, int32_t H, int32_t H_kv, int32_t n_q, int32_t n_kv, int32_t d,
+                               int32_t workspace, int32_t* form);
+
+/* sparvar_block_sparse_attn_q8_fwd and its form over a 4-bit cache. */
+int sparvar_block_sparse_attn_q4_fwd(const sparvar_geometry_t* g, int32_t k, int32_t B, int32_t H,
+                                     int32_t H_kv, int32_t d, sparvar_dtype_t dtype, const void* q_k,
+                                     int64_t q_bh_stride, const sparvar_q4_cache_t* q4, void* o, float* lse,
+                                     float softmax_scale, const int32_t* row_ptr, const int32_t* col_idx,
+                                     const int32_t* schedule, hipStream_t stream);
+int sparvar_block_sparse_attn_q4_form(const sparvar_geometry_t* g, int32_t k, int32_t B, int32_t H,
+                                      int32_t H_kv, int32_t d, int32_t* form);
+
+/*
+ * ---- A cache within a budget: what each key is worth, and eviction by it.
+ *
+ * Attention weight that the first n_kv keys of a cache got from a set of queries,
+ * added to what they had: for every key j of key head g,
+ *   w[b,g,j] = decay * w_old[b,g,j] (0 from n_old on)
+ *            + sum over the query heads h of g and their queries i of
+ *              exp(softmax_scale * q[b,h,i] . k[b,g,j] - lse[b,h,i]),
+ * lse as attention over the same keys gives it. In 32 bits, on the keys' values (a
+ * 4-bit cache's exactly), in an order that depends on the sizes alone.
+ *   q: [B,H,n_q,d] of `dtype` (plane stride q_bh_stride); lse: [B,H,n_q] fp32; a
+ *   query whose lse is -inf (it had no keys) adds nothing, one whose lse is NaN
+ *   makes the weights of its keys NaN.
+ *   k: [B,H_kv,>= n_kv,d] of `dtype` (plane stride k_bh_stride), or NULL and q4 a
+ *   4-bit cache (exactly one of the two; bf16 queries then; its v is not read).
+ *   kv_len (nullable): device int32 [B]; of entry b the first
+ *   min(max(kv_len[b], 0), n_kv) keys are weighed, the others' w is left as it was.
+ *   w_old (NULL: n_old = 0), w: fp32 [B,H_kv,>= n_kv], plane stride w_bh_stride
+ *   (elements); w_old may be w itself and must not overlap it otherwise.
+ *   decay: finite, >= 0.
+ */
+int sparvar_key_weights(int32_t B, int32_t H, int32_t H_kv, int32_t n_q, int32_t n_kv, int32_t d,
+                        sparvar_dtype_t dtype, const void* q, int64_t q_bh_stride, const void* k,
+                        int64_t k_bh_stride, const sparvar_q4_cache_t* q4, const float* lse,
+                        const int32_t* kv_len, const float* w_old, int32_t n_old, float decay, float* w,
+                        int64_t w_bh_stride, float softmax_scale, hipStream_t stream);
+
+/*
+ * Moves the tokens worth keeping to a cache of their own, a plane at a time. Of a
+ * plane's first len tokens (len = n, or min(max(kv_len[b], 0), n)) all are kept where
+ * len <= n_keep; otherwise n_keep: the first n_first, the last n_last, and of those
+ * between the ones of largest weight (of equal ones the first; a NaN counts as the
+ * largest). They move to rows 0, 1, .. of the destination, in order; what follows
+ * there is left as it was.
+ *   w: fp32 [B,H_kv,>= n], plane stride w_bh_stride; n_first + n_last <= n_keep.
+ *   k_src, v_src: [B,H_kv,>= n,d] of `dtype` (plane stride src_bh_stride); k_dst,
+ *   v_dst: [B,H_kv,>= n_keep,d] (plane stride dst_bh_stride); or these NULL and
+ *   q4_src, q4_dst 4-bit caches (dtype is not looked at then): codes and scales move
+ *   as they are.
+ *   kept: int32 [B,H_kv,n_keep] contiguous: the source token of each row, -1 after
+ *   the last; w_out: fp32 [B,H_kv,>= n_keep], plane stride w_out_bh_stride: their
+ *   weights.
+ * No output may overlap an input. A kept key has been rotated where it stood, so
+ * attention over the destination needs no positions; block-sparse rows, which name
+ * tokens by their place, do not hold for it.
+ */
+int sparvar_kv_evict(int32_t B, int32_t H_kv, int32_t d, sparvar_dtype_t dtype, int32_t n, int32_t n_keep,
+                     int32_t n_first, int32_t n_last, const int32_t* kv_len, const float* w,
+                     int64_t w_bh_stride, const void* k_src, const void* v_src, int64_t src_bh_stride,
+                     void* k_dst, void* v_dst, int64_t dst_bh_stride, const sparvar_q4_cache_t* q4_src,
+                     const sparvar_q4_cache_t* q4_dst, int32_t* kept, float* w_out, int64_t w_out_bh_stride,
+                     hipStream_t stream);
+
 /* Static description of a status code. */
 const char* sparvar_status_string(int status);
 /* Message of the last failed call on this thread ("" if none). */

@@ -3,3 +3,4 @@ from .sparvar_oracle import *  # noqa: F401,F403
 from .cs4a_oracle import *  # noqa: F401,F403
 from .csla_oracle import *  # noqa: F401,F403
 from .q8_oracle import *  # noqa: F401,F403
+from .q4_oracle import *  # noqa: F401,F403

@@ -23,7 +23,8 @@ CSRC = os.path.join(PKG, "csrc")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(BUILD, "libsparvar_host_sanitized.so")
 ROCM = "/opt/rocm"
-KERNEL_OBJECTS = ["attention.o", "select.o", "decision.o", "cs4a.o", "csla.o", "kv.o", "q8_cache.o", "attn_q8.o", "index.o"]
+KERNEL_OBJECTS = ["attention.o", "select.o", "decision.o", "cs4a.o", "csla.o", "kv.o", "q8_cache.o", "attn_q8.o",
+                  "q4_cache.o", "attn_q4.o", "weights.o", "evict.o", "index.o"]
 SAN = ["-fsanitize=address,undefined", "-fno-omit-frame-pointer", "-fno-sanitize-recover=undefined"]
 
 

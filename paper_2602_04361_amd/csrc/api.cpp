@@ -327,6 +327,34 @@ int check_q8(const sparvar_q8_cache_t* c, int32_t d, int64_t tokens, Q8View* v) 
   return SPARVAR_OK;
 }
 
+// A 4-bit cache: the struct's own consistency, and room for `tokens` tokens.
+int check_q4(const sparvar_q4_cache_t* c, int32_t d, int64_t tokens, Q4View* v) {
+  if (!c) return fail(SPARVAR_ERR_INVALID, "the 4-bit cache is NULL");
+  if (c->capacity < 1) return fail(SPARVAR_ERR_INVALID, "cache capacity %d < 1", c->capacity);
+  if ((int64_t)c->capacity * d >= (int64_t(1) << 31))
+    return fail(SPARVAR_ERR_INVALID, "4-bit cache of %d tokens x %d exceeds 2^31 codes a plane", c->capacity, d);
+  if (tokens > c->capacity)
+    return fail(SPARVAR_ERR_CAPACITY, "%lld tokens exceed the cache's capacity %d", (long long)tokens, c->capacity);
+  if (!c->k || !c->v || !c->k_scale || !c->v_scale) return fail(SPARVAR_ERR_INVALID, "a pointer of the 4-bit cache is NULL");
+  if (!aligned16(c->k) || !aligned16(c->v)) return fail(SPARVAR_ERR_INVALID, "cache codes are not 16-byte aligned");
+  if (c->bh_stride < (int64_t)c->capacity * (d / 2) || c->bh_stride % 16 != 0)
+    return fail(SPARVAR_ERR_INVALID, "code plane stride %lld < %lld or not a multiple of 16", (long long)c->bh_stride,
+                (long long)c->capacity * (d / 2));
+  const int32_t g = d / 32;
+  if (reinterpret_cast<uintptr_t>(c->k_scale) % g != 0 || reinterpret_cast<uintptr_t>(c->v_scale) % g != 0)
+    return fail(SPARVAR_ERR_INVALID, "cache scales are not %d-byte aligned", g);
+  if (c->scale_bh_stride < (int64_t)c->capacity * g || c->scale_bh_stride % g != 0)
+    return fail(SPARVAR_ERR_INVALID, "scale plane stride %lld < %lld or not a multiple of %d", (long long)c->scale_bh_stride,
+                (long long)c->capacity * g, g);
+  v->k = static_cast<uint8_t*>(c->k);
+  v->v = static_cast<uint8_t*>(c->v);
+  v->ks = c->k_scale;
+  v->vs = c->v_scale;
+  v->bh_stride = c->bh_stride;
+  v->sc_stride = c->scale_bh_stride;
+  return SPARVAR_OK;
+}
+
 // Batch, heads and appended tokens: every count of planes, rows and workgroups below 2^31.
 int check_tokens(int32_t B, int32_t H, int32_t H_kv, int32_t d, int32_t n, int32_t t0) {
   if (B < 1 || H < 1 || H_kv < 1 || n < 1) return fail(SPARVAR_ERR_INVALID, "B, heads and n must be >= 1");
@@ -359,7 +387,7 @@ int check_rows(const void* p, int64_t batch, int64_t token, int64_t row, int32_t
   return SPARVAR_OK;
 }
 
-int check_dense_q8(int32_t B, int32_t H, int32_t H_kv, int32_t n_q, int32_t n_kv, int32_t d) {
+int check_dense_codes(int32_t B, int32_t H, int32_t H_kv, int32_t n_q, int32_t n_kv, int32_t d) {
   int st = check_dtype_d(SPARVAR_BF16, d);
   if (st) return st;
   if ((st = check_heads(B, H, H_kv))) return st;
@@ -1075,7 +1103,7 @@ int sparvar_kv_dequantize(int32_t B, int32_t H_kv, int32_t d, sparvar_dtype_t dt
 
 int64_t sparvar_dense_attn_q8_workspace(int32_t B, int32_t H, int32_t H_kv, int32_t n_q, int32_t n_kv,
                                         int32_t d) {
-  const int st = check_dense_q8(B, H, H_kv, n_q, n_kv, d);
+  const int st = check_dense_codes(B, H, H_kv, n_q, n_kv, d);
   if (st) return st;
   ok();
   return dense_q8_workspace(B, H, H_kv, n_q, n_kv, d, device_cus());
@@ -1087,7 +1115,7 @@ int sparvar_dense_attn_q8_fwd(int32_t B, int32_t H, int32_t H_kv, int32_t n_q, i
                               float softmax_scale, void* workspace, int64_t workspace_bytes,
                               hipStream_t stream) {
   if (dtype != SPARVAR_BF16) return fail(SPARVAR_ERR_UNSUPPORTED, "attention over an 8-bit cache takes bf16 queries only");
-  int st = check_dense_q8(B, H, H_kv, n_q, n_kv, d);
+  int st = check_dense_codes(B, H, H_kv, n_q, n_kv, d);
   if (st) return st;
   if ((st = check_softmax_scale(softmax_scale))) return st;
   if ((st = check_plane(q, q_bh_stride, n_q, d, 2, "q"))) return st;
@@ -1120,7 +1148,7 @@ int sparvar_dense_attn_q8_fwd(int32_t B, int32_t H, int32_t H_kv, int32_t n_q, i
 
 int sparvar_dense_attn_q8_form(int32_t B, int32_t H, int32_t H_kv, int32_t n_q, int32_t n_kv, int32_t d,
                                int32_t workspace, int32_t* form) {
-  const int st = check_dense_q8(B, H, H_kv, n_q, n_kv, d);
+  const int st = check_dense_codes(B, H, H_kv, n_q, n_kv, d);
   if (st) return st;
   if (!form) return fail(SPARVAR_ERR_INVALID, "form is NULL");
   const Q8Form f = dense_q8_form(B, H, H_kv, n_q, n_kv, d, device_cus(), workspace != 0);
@@ -1183,6 +1211,290 @@ int sparvar_block_sparse_attn_q8_form(const sparvar_geometry_t* g, int32_t k, in
   form[0] = f.waves;
   form[1] = f.sets;
   return ok();
+}
+
+int sparvar_kv_quantize_q4(int32_t B, int32_t H_kv, int32_t d, sparvar_dtype_t dtype, int32_t n, int32_t t0,
+                        const void* k_src, const void* v_src, int64_t src_bh_stride,
+                        const sparvar_q4_cache_t* q4, hipStream_t stream) {
+  int st = check_dtype_d(dtype, d);
+  if (st) return st;
+  if ((st = check_tokens(B, H_kv, H_kv, d, n, t0))) return st;
+  const int elem = dtype == SPARVAR_BF16 ? 2 : 4;
+  if ((st = check_plane(k_src, src_bh_stride, n, d, elem, "k_src"))) return st;
+  if ((st = check_plane(v_src, src_bh_stride, n, d, elem, "v_src"))) return st;
+  KvQuantizeQ4Args a;
+  if ((st = check_q4(q4, d, (int64_t)t0 + n, &a.c4))) return st;
+  a.planes = B * H_kv;
+  a.d = d;
+  a.n = n;
+  a.t0 = t0;
+  a.bf16 = dtype == SPARVAR_BF16;
+  a.k = k_src;
+  a.v = v_src;
+  a.bh_stride = src_bh_stride;
+  return hip_status(launch_kv_quantize_q4(a, stream), "kv quantize (4 bits) launch");
+}
+
+int sparvar_kv_dequantize_q4(int32_t B, int32_t H_kv, int32_t d, sparvar_dtype_t dtype, int32_t n, int32_t t0,
+                          const sparvar_q4_cache_t* q4, void* k_dst, void* v_dst, int64_t dst_bh_stride,
+                          hipStream_t stream) {
+  int st = check_dtype_d(dtype, d);
+  if (st) return st;
+  if ((st = check_tokens(B, H_kv, H_kv, d, n, t0))) return st;
+  const int elem = dtype == SPARVAR_BF16 ? 2 : 4;
+  if ((st = check_plane(k_dst, dst_bh_stride, n, d, elem, "k_dst"))) return st;
+  if ((st = check_plane(v_dst, dst_bh_stride, n, d, elem, "v_dst"))) return st;
+  KvDequantizeQ4Args a;
+  if ((st = check_q4(q4, d, (int64_t)t0 + n, &a.c4))) return st;
+  a.planes = B * H_kv;
+  a.d = d;
+  a.n = n;
+  a.t0 = t0;
+  a.bf16 = dtype == SPARVAR_BF16;
+  a.k = k_dst;
+  a.v = v_dst;
+  a.bh_stride = dst_bh_stride;
+  return hip_status(launch_kv_dequantize_q4(a, stream), "kv dequantize (4 bits) launch");
+}
+
+int64_t sparvar_dense_attn_q4_workspace(int32_t B, int32_t H, int32_t H_kv, int32_t n_q, int32_t n_kv,
+                                        int32_t d) {
+  const int st = check_dense_codes(B, H, H_kv, n_q, n_kv, d);
+  if (st) return st;
+  ok();
+  return dense_q4_workspace(B, H, H_kv, n_q, n_kv, d, device_cus());
+}
+
+int sparvar_dense_attn_q4_fwd(int32_t B, int32_t H, int32_t H_kv, int32_t n_q, int32_t n_kv, int32_t d,
+                              sparvar_dtype_t dtype, const void* q, int64_t q_bh_stride,
+                              const sparvar_q4_cache_t* q4, const int32_t* kv_len, void* o, float* lse,
+                              float softmax_scale, void* workspace, int64_t workspace_bytes,
+                              hipStream_t stream) {
+  if (dtype != SPARVAR_BF16) return fail(SPARVAR_ERR_UNSUPPORTED, "attention over a 4-bit cache takes bf16 queries only");
+  int st = check_dense_codes(B, H, H_kv, n_q, n_kv, d);
+  if (st) return st;
+  if ((st = check_softmax_scale(softmax_scale))) return st;
+  if ((st = check_plane(q, q_bh_stride, n_q, d, 2, "q"))) return st;
+  if ((st = check_plane(o, (int64_t)n_q * d, n_q, d, 2, "o"))) return st;
+  DenseQ4Args a;
+  if ((st = check_q4(q4, d, n_kv, &a.c4))) return st;
+  a.num_cu = device_cus();
+  const int64_t need = workspace ? dense_q4_workspace(B, H, H_kv, n_q, n_kv, d, a.num_cu) : 0;
+  if (need > 0) {
+    if (workspace_bytes < need)
+      return fail(SPARVAR_ERR_CAPACITY, "workspace of %lld bytes < %lld", (long long)workspace_bytes, (long long)need);
+    if (!aligned16(workspace)) return fail(SPARVAR_ERR_INVALID, "workspace is not 16-byte aligned");
+  }
+  a.B = B;
+  a.H = H;
+  a.H_kv = H_kv;
+  a.n_q = n_q;
+  a.n_kv = n_kv;
+  a.d = d;
+  a.q = q;
+  a.o = o;
+  a.lse = lse;
+  a.q_bh_stride = q_bh_stride;
+  a.kv_len = kv_len;
+  a.softmax_scale = softmax_scale;
+  a.workspace = need > 0 ? static_cast<float*>(workspace) : nullptr;
+  a.swizzle = opt(SPARVAR_OPT_SWIZZLE);
+  return hip_status(launch_dense_attn_q4(a, stream), "dense 4-bit attention launch");
+}
+
+int sparvar_dense_attn_q4_form(int32_t B, int32_t H, int32_t H_kv, int32_t n_q, int32_t n_kv, int32_t d,
+                               int32_t workspace, int32_t* form) {
+  const int st = check_dense_codes(B, H, H_kv, n_q, n_kv, d);
+  if (st) return st;
+  if (!form) return fail(SPARVAR_ERR_INVALID, "form is NULL");
+  const CodesForm f = dense_q4_form(B, H, H_kv, n_q, n_kv, d, device_cus(), workspace != 0);
+  form[0] = f.waves;
+  form[1] = f.sets;
+  form[2] = f.parts;
+  return ok();
+}
+
+int sparvar_block_sparse_attn_q4_fwd(const sparvar_geometry_t* g, int32_t k, int32_t B, int32_t H,
+                                     int32_t H_kv, int32_t d, sparvar_dtype_t dtype, const void* q_k,
+                                     int64_t q_bh_stride, const sparvar_q4_cache_t* q4, void* o, float* lse,
+                                     float softmax_scale, const int32_t* row_ptr, const int32_t* col_idx,
+                                     const int32_t* schedule, hipStream_t stream) {
+  GeoTable T;
+  int st = build_table(g, &T);
+  if (st) return st;
+  if (k < 1 || k > T.L) return fail(SPARVAR_ERR_INVALID, "scale %d outside [1, %d]", k, T.L);
+  if (dtype != SPARVAR_BF16) return fail(SPARVAR_ERR_UNSUPPORTED, "attention over a 4-bit cache takes bf16 queries only");
+  if ((st = check_dtype_d(dtype, d))) return st;
+  if ((st = check_heads(B, H, H_kv))) return st;
+  const int32_t Nk = T.h[k - 1] * T.w[k - 1];
+  if ((int64_t)B * H * Nk >= (int64_t(1) << 31)) return fail(SPARVAR_ERR_INVALID, "B*H*N_k too large");
+  if ((st = check_softmax_scale(softmax_scale))) return st;
+  if (!row_ptr || !col_idx) return fail(SPARVAR_ERR_INVALID, "row_ptr/col_idx is NULL");
+  if ((st = check_plane(q_k, q_bh_stride, Nk, d, 2, "q_k"))) return st;
+  if ((st = check_plane(o, (int64_t)Nk * d, Nk, d, 2, "o"))) return st;
+  SparseQ4Args a;
+  if ((st = check_q4(q4, d, T.C[k], &a.c4))) return st;
+  a.G = &T;
+  a.k = k;
+  a.BH = B * H;
+  a.H = H;
+  a.H_kv = H_kv;
+  a.d = d;
+  a.q = q_k;
+  a.o = o;
+  a.lse = lse;
+  a.q_bh_stride = q_bh_stride;
+  a.softmax_scale = softmax_scale;
+  a.row_ptr = row_ptr;
+  a.col_idx = col_idx;
+  a.schedule = schedule;
+  a.swizzle = opt(SPARVAR_OPT_SWIZZLE);
+  a.num_cu = device_cus();
+  return hip_status(launch_sparse_attn_q4(a, stream), "block-sparse 4-bit attention launch");
+}
+
+int sparvar_block_sparse_attn_q4_form(const sparvar_geometry_t* g, int32_t k, int32_t B, int32_t H,
+                                      int32_t H_kv, int32_t d, int32_t* form) {
+  GeoTable T;
+  int st = build_table(g, &T);
+  if (st) return st;
+  if (k < 1 || k > T.L) return fail(SPARVAR_ERR_INVALID, "scale %d outside [1, %d]", k, T.L);
+  if ((st = check_dtype_d(SPARVAR_BF16, d))) return st;
+  if ((st = check_heads(B, H, H_kv))) return st;
+  if ((int64_t)B * H * T.h[k - 1] * T.w[k - 1] >= (int64_t(1) << 31)) return fail(SPARVAR_ERR_INVALID, "B*H*N_k too large");
+  if (!form) return fail(SPARVAR_ERR_INVALID, "form is NULL");
+  const CodesForm f = sparse_q4_form(T, k, B * H, d, device_cus());
+  form[0] = f.waves;
+  form[1] = f.sets;
+  return ok();
+}
+
+int sparvar_key_weights(int32_t B, int32_t H, int32_t H_kv, int32_t n_q, int32_t n_kv, int32_t d,
+                        sparvar_dtype_t dtype, const void* q, int64_t q_bh_stride, const void* k,
+                        int64_t k_bh_stride, const sparvar_q4_cache_t* q4, const float* lse,
+                        const int32_t* kv_len, const float* w_old, int32_t n_old, float decay, float* w,
+                        int64_t w_bh_stride, float softmax_scale, hipStream_t stream) {
+  int st = check_dtype_d(dtype, d);
+  if (st) return st;
+  if ((st = check_heads(B, H, H_kv))) return st;
+  if (n_q < 1 || n_kv < 1) return fail(SPARVAR_ERR_INVALID, "n_q and n_kv must be >= 1");
+  if ((int64_t)B * H * n_q >= (int64_t(1) << 31)) return fail(SPARVAR_ERR_INVALID, "B*H*n_q too large");
+  if (n_kv >= 0x7fffff00) return fail(SPARVAR_ERR_INVALID, "n_kv = %d too large", n_kv);
+  if ((int64_t)B * H_kv * ((n_kv + 31) / 32) >= (int64_t(1) << 31)) return fail(SPARVAR_ERR_INVALID, "too many keys for one launch");
+  if ((st = check_softmax_scale(softmax_scale))) return st;
+  if (!std::isfinite(decay) || decay < 0.f) return fail(SPARVAR_ERR_INVALID, "decay %g is not finite and >= 0", decay);
+  const int elem = dtype == SPARVAR_BF16 ? 2 : 4;
+  if ((st = check_plane(q, q_bh_stride, n_q, d, elem, "q"))) return st;
+  if ((k != nullptr) == (q4 != nullptr)) return fail(SPARVAR_ERR_INVALID, "either k or a 4-bit cache is required");
+  KeyWeightsArgs a;
+  a.c4 = Q4View{};
+  if (q4) {
+    if (dtype != SPARVAR_BF16) return fail(SPARVAR_ERR_UNSUPPORTED, "weights over a 4-bit cache take bf16 queries only");
+    if ((st = check_q4(q4, d, n_kv, &a.c4))) return st;
+  } else if ((st = check_plane(k, k_bh_stride, n_kv, d, elem, "k"))) {
+    return st;
+  }
+  if (!lse || !w) return fail(SPARVAR_ERR_INVALID, "lse or w is NULL");
+  if (n_old < 0 || n_old > n_kv) return fail(SPARVAR_ERR_INVALID, "n_old = %d outside [0, %d]", n_old, n_kv);
+  if (n_old > 0 && !w_old) return fail(SPARVAR_ERR_INVALID, "w_old is NULL and n_old = %d", n_old);
+  if (w_bh_stride < n_kv) return fail(SPARVAR_ERR_INVALID, "w plane stride %lld < %d", (long long)w_bh_stride, n_kv);
+  a.B = B;
+  a.H = H;
+  a.H_kv = H_kv;
+  a.n_q = n_q;
+  a.n_kv = n_kv;
+  a.n_old = n_old;
+  a.d = d;
+  a.bf16 = dtype == SPARVAR_BF16;
+  a.q = q;
+  a.k = k;
+  a.q_bh_stride = q_bh_stride;
+  a.k_bh_stride = k_bh_stride;
+  a.lse = lse;
+  a.kv_len = kv_len;
+  a.w_old = w_old;
+  a.w = w;
+  a.w_bh_stride = w_bh_stride;
+  a.softmax_scale = softmax_scale;
+  a.decay = decay;
+  a.num_cu = device_cus();
+  return hip_status(launch_key_weights(a, stream), "key weights launch");
+}
+
+int sparvar_kv_evict(int32_t B, int32_t H_kv, int32_t d, sparvar_dtype_t dtype, int32_t n, int32_t n_keep,
+                     int32_t n_first, int32_t n_last, const int32_t* kv_len, const float* w,
+                     int64_t w_bh_stride, const void* k_src, const void* v_src, int64_t src_bh_stride,
+                     void* k_dst, void* v_dst, int64_t dst_bh_stride, const sparvar_q4_cache_t* q4_src,
+                     const sparvar_q4_cache_t* q4_dst, int32_t* kept, float* w_out, int64_t w_out_bh_stride,
+                     hipStream_t stream) {
+  const bool q4 = q4_src || q4_dst;
+  int st = check_dtype_d(q4 ? SPARVAR_BF16 : dtype, d);
+  if (st) return st;
+  if ((st = check_heads(B, H_kv, H_kv))) return st;
+  if (n < 1 || n_keep < 1) return fail(SPARVAR_ERR_INVALID, "n and n_keep must be >= 1");
+  if (n >= 0x7ffe0000 || n_keep >= 0x7ffe0000) return fail(SPARVAR_ERR_INVALID, "n = %d or n_keep = %d too large", n, n_keep);
+  if (n_first < 0 || n_last < 0 || (int64_t)n_first + n_last > n_keep)
+    return fail(SPARVAR_ERR_INVALID, "n_first = %d and n_last = %d must be >= 0 and n_keep = %d at most together", n_first, n_last, n_keep);
+  if ((int64_t)B * H_kv * ((int64_t)n_keep / 64 + 1) >= (int64_t(1) << 31))
+    return fail(SPARVAR_ERR_INVALID, "too many rows for one launch");
+  if (!w || !kept || !w_out) return fail(SPARVAR_ERR_INVALID, "w, kept or w_out is NULL");
+  if (w == w_out) return fail(SPARVAR_ERR_INVALID, "w_out is w");
+  if (w_bh_stride < n) return fail(SPARVAR_ERR_INVALID, "w plane stride %lld < %d", (long long)w_bh_stride, n);
+  if (w_out_bh_stride < n_keep) return fail(SPARVAR_ERR_INVALID, "w_out plane stride %lld < %d", (long long)w_out_bh_stride, n_keep);
+  KvEvictArgs a;
+  if (q4) {
+    if (k_src || v_src || k_dst || v_dst) return fail(SPARVAR_ERR_INVALID, "either k and v or 4-bit caches are required");
+    Q4View s, t;
+    if ((st = check_q4(q4_src, d, n, &s))) return st;
+    if ((st = check_q4(q4_dst, d, n_keep, &t))) return st;
+    if (s.k == t.k || s.v == t.v || s.ks == t.ks || s.vs == t.vs) return fail(SPARVAR_ERR_INVALID, "the destination is the source");
+    a.row = d / 2;
+    a.srow = d / 32;
+    a.k_src = s.k;
+    a.v_src = s.v;
+    a.ks_src = s.ks;
+    a.vs_src = s.vs;
+    a.k_dst = t.k;
+    a.v_dst = t.v;
+    a.ks_dst = t.ks;
+    a.vs_dst = t.vs;
+    a.src_stride = s.bh_stride;
+    a.dst_stride = t.bh_stride;
+    a.ssrc_stride = s.sc_stride;
+    a.sdst_stride = t.sc_stride;
+  } else {
+    const int elem = dtype == SPARVAR_BF16 ? 2 : 4;
+    if ((st = check_plane(k_src, src_bh_stride, n, d, elem, "k_src"))) return st;
+    if ((st = check_plane(v_src, src_bh_stride, n, d, elem, "v_src"))) return st;
+    if ((st = check_plane(k_dst, dst_bh_stride, n_keep, d, elem, "k_dst"))) return st;
+    if ((st = check_plane(v_dst, dst_bh_stride, n_keep, d, elem, "v_dst"))) return st;
+    if (k_src == k_dst || v_src == v_dst) return fail(SPARVAR_ERR_INVALID, "the destination is the source");
+    a.row = d * elem;
+    a.srow = 0;
+    a.k_src = k_src;
+    a.v_src = v_src;
+    a.k_dst = k_dst;
+    a.v_dst = v_dst;
+    a.ks_src = a.vs_src = nullptr;
+    a.ks_dst = a.vs_dst = nullptr;
+    a.src_stride = src_bh_stride * elem;
+    a.dst_stride = dst_bh_stride * elem;
+    a.ssrc_stride = a.sdst_stride = 0;
+  }
+  a.B = B;
+  a.H_kv = H_kv;
+  a.n = n;
+  a.n_keep = n_keep;
+  a.n_first = n_first;
+  a.n_last = n_last;
+  a.kv_len = kv_len;
+  a.w = w;
+  a.w_out = w_out;
+  a.kept = kept;
+  a.w_bh_stride = w_bh_stride;
+  a.w_out_bh_stride = w_out_bh_stride;
+  a.num_cu = device_cus();
+  return hip_status(launch_kv_evict(a, stream), "evict launch");
 }
 
 }  // extern "C"

@@ -1,0 +1,375 @@
+// Attention weight of a cache's keys: w[j] = decay w_old[j] + sum over the queries i of the head
+// group of exp(scale q_i k_j - lse_i), lse the log of the softmax denominators that attention gave.
+//
+// S = Q K^T by MFMA with the queries as rows, so that a lane's column is one key and its registers
+// are 16 queries of it: a key's sum stays in a lane (one exchange between the halves at the end),
+// and no sum is made by atomics. Half the products of attention, the same exponentials. K is held
+// in registers; 4-bit keys become bf16 on their way there, which is exact. Scores, sums and weights
+// are held in 32 bits.
+//
+// A sum over channels may run in any order: a lane's fragments are 16-byte units of its half of a
+// row, the same ones of Q (rows in LDS) and K (registers), eight bf16 or four fp32 channels each.
+#include "device_common.h"
+#include "launch.h"
+#include "q4.h"
+
+namespace sparvar {
+
+namespace {
+
+enum class Keys { kBf16, kF32, kQ4 };
+
+struct WeightsIO {
+  const char* q;
+  const char* k;
+  const uint8_t* ks;
+  const float* lse;
+  const float* w_old;
+  float* w;
+  const int32_t* kv_len;
+  int64_t q_bh_stride, k_bh_stride, ks_bh_stride, w_bh_stride;  // bytes (w: elements)
+  int32_t n_q, rows, group, H_kv;  // rows = group * n_q: those of a key head
+  int32_t n_kv, n_old, slabs;      // workgroups a plane
+  int32_t flat;                    // the rows of a group follow one another in memory
+  float scale_log2, decay;
+};
+
+template <Keys KT>
+struct Traits {
+  static constexpr int kElem = KT == Keys::kF32 ? 4 : 2;
+};
+
+// Byte offset of query row i of a group.
+template <int D, int ELEM>
+__device__ __forceinline__ int64_t query_at(const WeightsIO& io, int32_t i) {
+  if (io.flat) return (int64_t)i * (D * ELEM);
+  const int32_t h = i / io.n_q;
+  return h * io.q_bh_stride + (int64_t)(i - h * io.n_q) * (D * ELEM);
+}
+
+// LSE of row i in the exp2 domain; +inf, which makes every weight zero, for rows that are not there
+// and rows that had no keys.
+__device__ __forceinline__ float lse2_of(const WeightsIO& io, const float* lse, int32_t i) {
+  const float l = i < io.rows ? lse[i] : -INFINITY;
+  return l == -INFINITY ? INFINITY : l * kLog2e;
+}
+
+// The units of a lane's half of a key, as they lie in memory.
+template <Keys KT, int D>
+struct RawKey {
+  static constexpr int kPieces = KT == Keys::kQ4 ? D / 64 : D * Traits<KT>::kElem / 32;
+  u32x4 p[kPieces];
+  uint32_t sc;
+  __device__ __forceinline__ void load(const char* k, const uint8_t* ks, uint32_t tok, int half) {
+    if constexpr (KT == Keys::kQ4) {
+#pragma unroll
+      for (int i = 0; i < kPieces; ++i) p[i] = ldg16(k + (int64_t)tok * (D / 2) + half * (D / 4) + 16 * i);
+      if constexpr (D == 128) sc = *reinterpret_cast<const uint16_t*>(ks + (int64_t)tok * 4 + 2 * half);
+      else sc = ks[(int64_t)tok * 2 + half];
+    } else {
+      constexpr int kHalf = D * Traits<KT>::kElem / 2;
+#pragma unroll
+      for (int i = 0; i < kPieces; ++i) p[i] = ldg16(k + (int64_t)tok * (2 * kHalf) + half * kHalf + 16 * i);
+    }
+  }
+};
+
+// The same as operands.
+template <Keys KT, int D>
+struct KeyFrag {
+  static constexpr int kUnits = D * Traits<KT>::kElem / 32;  // of a half
+  u32x4 u[kUnits];
+  __device__ __forceinline__ void take(const RawKey<KT, D>& r) {
+    if constexpr (KT == Keys::kQ4) {
+#pragma unroll
+      for (int i = 0; i < kUnits; ++i) u[i] = q4_decode8_bf16(r.p[i / 4][i & 3], q4_scale((r.sc >> (8 * (i / 4))) & 0xff));
+    } else {
+#pragma unroll
+      for (int i = 0; i < kUnits; ++i) u[i] = r.p[i];
+    }
+  }
+};
+
+template <Keys KT>
+__device__ __forceinline__ f32x16 unit_product(u32x4 a, u32x4 b, f32x16 c) {
+  if constexpr (KT == Keys::kF32) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c = mfma_f32(__uint_as_float(a[i]), __uint_as_float(b[i]), c);
+    return c;
+  } else {
+    return mfma_bf16(as_bf16x8(a), as_bf16x8(b), c);
+  }
+}
+
+// Sum of the 16 probabilities of a lane.
+__device__ __forceinline__ float tile_sum(const f32x16& st, const float (&lse2)[16], float scale_log2) {
+  float p[16];
+#pragma unroll
+  for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[r], scale_log2, -lse2[r]));
+#pragma unroll
+  for (int n = 8; n > 0; n >>= 1)
+#pragma unroll
+    for (int r = 0; r < n; ++r) p[r] += p[r + n];
+  return p[0];
+}
+
+// LSEs of the 16 rows of a lane's registers, of a tile's 32 in LDS.
+__device__ __forceinline__ void load_lse(const float* tile, int half, float (&lse2)[16]) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const float4 v = *reinterpret_cast<const float4*>(tile + 8 * j + 4 * half);
+    lse2[4 * j] = v.x, lse2[4 * j + 1] = v.y, lse2[4 * j + 2] = v.z, lse2[4 * j + 3] = v.w;
+  }
+}
+
+__device__ __forceinline__ int32_t length_of(const WeightsIO& io, int32_t plane) {
+  if (!io.kv_len) return io.n_kv;
+  const int32_t len = io.kv_len[plane / io.H_kv];
+  return len < 0 ? 0 : (len < io.n_kv ? len : io.n_kv);
+}
+
+__device__ __forceinline__ void store_weight(const WeightsIO& io, int32_t plane, int32_t key, float sum) {
+  const int64_t at = (int64_t)plane * io.w_bh_stride + key;
+  io.w[at] = key < io.n_old ? __builtin_fmaf(io.decay, io.w_old[at], sum) : sum;
+}
+
+// 16-byte unit u of LDS row r at u ^ this.
+template <int U>
+__device__ __forceinline__ int row_swizzle(int r) {
+  return unit_swizzle(r) & (U - 1);
+}
+
+// Many rows: WK waves hold 32 KN keys each, and WR such sets of waves take every WR-th tile of 32
+// rows. The rows stream through LDS, RS at a time, two stages.
+template <Keys KT, int D, int WK, int WR, int KN>
+__global__ __launch_bounds__(WK * WR * 64) __attribute__((amdgpu_waves_per_eu(2))) void key_weights_kernel(WeightsIO io) {
+  constexpr int NT = WK * WR * 64, NW = WK * WR, RS = WR > 2 ? 32 * WR : 64;
+  constexpr int kElem = Traits<KT>::kElem, kRow = D * kElem, U = kRow / 16;
+  constexpr int kLoads = RS * U / NT;
+  static_assert(RS * U % NT == 0, "a stage must split evenly over the workgroup");
+  __shared__ __attribute__((aligned(16))) char stage0[RS * kRow];
+  __shared__ __attribute__((aligned(16))) char stage1[RS * kRow];
+  __shared__ __attribute__((aligned(16))) float lses[2][RS];
+  __shared__ float sums[WR > 1 ? WR : 1][WK * KN * 32];
+
+  const int32_t slab = blockIdx.x % io.slabs, plane = blockIdx.x / io.slabs;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l32 = lane & 31, half = lane >> 5, wk = wave % WK, wr = wave / WK;
+  const int32_t len = length_of(io, plane);
+  const int32_t key0 = slab * (WK * KN * 32);
+  if (key0 >= len) return;
+
+  const char* kp = io.k + (int64_t)plane * io.k_bh_stride;
+  const uint8_t* ksp = io.ks + (int64_t)plane * io.ks_bh_stride;
+  const char* qp = io.q + (int64_t)plane * io.group * io.q_bh_stride;
+  const float* lp = io.lse + (int64_t)plane * io.rows;
+  const int32_t stages = (io.rows + RS - 1) / RS;
+  auto issue = [&](int32_t s, char* to) {
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+      const int first = (j * NW + wave) * 64, slot = first + lane, r = slot / U;
+      const int32_t i = s * RS + r;
+      dma16(qp + query_at<D, kElem>(io, i < io.rows ? i : io.rows - 1) + 16 * ((slot % U) ^ row_swizzle<U>(r)), to + first * 16);
+    }
+  };
+  issue(0, stage0);
+  if (tid < RS) lses[0][tid] = lse2_of(io, lp, tid);
+  KeyFrag<KT, D> kf[KN];
+  {
+    RawKey<KT, D> raw[KN];
+#pragma unroll
+    for (int n = 0; n < KN; ++n) {
+      const int32_t key = key0 + (wk * KN + n) * 32 + l32;
+      raw[n].load(kp, ksp, (uint32_t)(key < len ? key : len - 1), half);
+    }
+#pragma unroll
+    for (int n = 0; n < KN; ++n) kf[n].take(raw[n]);
+  }
+  float sum[KN];
+#pragma unroll
+  for (int n = 0; n < KN; ++n) sum[n] = 0.f;
+
+  auto step = [&](int32_t s, const char* now, char* then) {
+    __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
+    __syncthreads();
+    float lse_next = 0.f;
+    if (s + 1 < stages) {
+      issue(s + 1, then);
+      if (tid < RS) lse_next = lse2_of(io, lp, (s + 1) * RS + tid);
+    }
+#pragma unroll
+    for (int t = 0; t < RS / 32 / WR; ++t) {
+      const int rt = t * WR + wr;
+      const char* row = now + (rt * 32 + l32) * kRow;
+      const int sw = row_swizzle<U>(l32);
+      float lse2[16];
+      load_lse(&lses[s & 1][rt * 32], half, lse2);
+      f32x16 st[KN];
+#pragma unroll
+      for (int n = 0; n < KN; ++n) st[n] = zero16();
+#pragma unroll
+      for (int u = 0; u < U / 2; ++u) {
+        const u32x4 a = *reinterpret_cast<const u32x4*>(row + 16 * ((half * (U / 2) + u) ^ sw));
+#pragma unroll
+        for (int n = 0; n < KN; ++n) st[n] = unit_product<KT>(a, kf[n].u[u], st[n]);
+      }
+#pragma unroll
+      for (int n = 0; n < KN; ++n) sum[n] += tile_sum(st[n], lse2, io.scale_log2);
+    }
+    if (s + 1 < stages && tid < RS) lses[(s + 1) & 1][tid] = lse_next;
+  };
+  for (int32_t s = 0; s < stages; s += 2) {
+    step(s, stage0, stage1);
+    if (s + 1 < stages) step(s + 1, stage1, stage0);
+  }
+#pragma unroll
+  for (int n = 0; n < KN; ++n) sum[n] = sum_halves(sum[n]);
+  if constexpr (WR == 1) {
+#pragma unroll
+    for (int n = 0; n < KN; ++n) {
+      const int32_t key = key0 + (wk * KN + n) * 32 + l32;
+      if (key < len && half == (n & 1)) store_weight(io, plane, key, sum[n]);
+    }
+  } else {
+    if (half == 0) {
+#pragma unroll
+      for (int n = 0; n < KN; ++n) sums[wr][(wk * KN + n) * 32 + l32] = sum[n];
+    }
+    __syncthreads();
+    const int32_t key = key0 + tid;
+    if (tid < WK * KN * 32 && key < len) {
+      float t = 0.f;
+#pragma unroll
+      for (int r = 0; r < WR; ++r) t += sums[r][tid];
+      store_weight(io, plane, key, t);
+    }
+  }
+}
+
+// Few rows (up to 128 of a key head; single tokens against a long cache): bound by K's way from
+// memory. All rows lie in LDS; every wave walks tiles of 32 keys by itself, the next one's in flight.
+constexpr int kFewWaves = 4;
+// (their LDS below 64 KB)
+template <Keys KT>
+constexpr int kFewRows = KT == Keys::kF32 ? 96 : 128;
+
+template <Keys KT, int D>
+__global__ __launch_bounds__(kFewWaves * 64) __attribute__((amdgpu_waves_per_eu(2)))
+void key_weights_few_kernel(WeightsIO io, int32_t tiles) {
+  constexpr int NT = kFewWaves * 64;
+  constexpr int kElem = Traits<KT>::kElem, kRow = D * kElem, U = kRow / 16;
+  extern __shared__ __attribute__((aligned(16))) char smem[];  // row tiles, then their LSEs
+  const int32_t slab = blockIdx.x % io.slabs, plane = blockIdx.x / io.slabs;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l32 = lane & 31, half = lane >> 5;
+  const int32_t len = length_of(io, plane);
+  const int32_t first = slab * tiles, end_tile = (len + 31) / 32, end = first + tiles < end_tile ? first + tiles : end_tile;
+  if (first >= end) return;
+
+  const char* kp = io.k + (int64_t)plane * io.k_bh_stride;
+  const uint8_t* ksp = io.ks + (int64_t)plane * io.ks_bh_stride;
+  const char* qp = io.q + (int64_t)plane * io.group * io.q_bh_stride;
+  const float* lp = io.lse + (int64_t)plane * io.rows;
+  const int32_t row_tiles = (io.rows + 31) / 32;
+  float* lses = reinterpret_cast<float*>(smem + row_tiles * 32 * kRow);
+
+  RawKey<KT, D> raw;
+  auto load = [&](int32_t t) {
+    const int32_t key = t * 32 + l32;
+    raw.load(kp, ksp, (uint32_t)(key < len ? key : len - 1), half);
+  };
+  int32_t t = first + wave;
+  if (t < end) load(t);
+  for (int32_t slot = tid; slot < row_tiles * 32 * U; slot += NT) {
+    const int32_t r = slot / U, i = r < io.rows ? r : io.rows - 1;
+    const u32x4 v = ldg16(qp + query_at<D, kElem>(io, i) + 16 * (slot % U));
+    *reinterpret_cast<u32x4*>(smem + r * kRow + 16 * ((slot % U) ^ row_swizzle<U>(r))) = v;
+  }
+  if (tid < row_tiles * 32) lses[tid] = lse2_of(io, lp, tid);
+  __syncthreads();
+  const int sw = row_swizzle<U>(l32);
+  for (; t < end; t += kFewWaves) {
+    KeyFrag<KT, D> kf;
+    kf.take(raw);
+    if (t + kFewWaves < end) load(t + kFewWaves);
+    float sum = 0.f;
+    for (int32_t rt = 0; rt < row_tiles; ++rt) {
+      const char* row = smem + (rt * 32 + l32) * kRow;
+      float lse2[16];
+      load_lse(lses + rt * 32, half, lse2);
+      f32x16 st = zero16();
+#pragma unroll
+      for (int u = 0; u < U / 2; ++u)
+        st = unit_product<KT>(*reinterpret_cast<const u32x4*>(row + 16 * ((half * (U / 2) + u) ^ sw)), kf.u[u], st);
+      sum += tile_sum(st, lse2, io.scale_log2);
+    }
+    sum = sum_halves(sum);
+    const int32_t key = t * 32 + l32;
+    if (half == 0 && key < len) store_weight(io, plane, key, sum);
+  }
+}
+
+template <Keys KT, int D, int WK, int WR, int KN>
+hipError_t launch_many(WeightsIO io, int32_t planes, hipStream_t stream) {
+  constexpr int32_t keys = WK * KN * 32;
+  io.slabs = (io.n_kv + keys - 1) / keys;
+  hipLaunchKernelGGL((key_weights_kernel<KT, D, WK, WR, KN>), dim3(planes * io.slabs), dim3(WK * WR * 64), 0, stream, io);
+  return hipGetLastError();
+}
+
+template <Keys KT, int D>
+hipError_t launch_weights(WeightsIO io, int32_t planes, int num_cu, hipStream_t stream) {
+  constexpr int kRow = D * Traits<KT>::kElem;
+  if (io.rows <= kFewRows<KT>) {
+    const int32_t row_tiles = (io.rows + 31) / 32, all = (io.n_kv + 31) / 32;
+    // workgroups of at least a tile a wave, as many as eight a CU
+    int64_t tiles = ((int64_t)planes * all + 8 * num_cu - 1) / (8 * num_cu);
+    tiles = (tiles + kFewWaves - 1) / kFewWaves * kFewWaves;
+    io.slabs = (int32_t)((all + tiles - 1) / tiles);
+    const size_t lds = (size_t)row_tiles * 32 * (kRow + 4);
+    hipLaunchKernelGGL((key_weights_few_kernel<KT, D>), dim3(planes * io.slabs), dim3(kFewWaves * 64), lds, stream, io,
+                       (int32_t)tiles);
+    return hipGetLastError();
+  }
+  auto groups = [&](int32_t keys) { return (int64_t)planes * ((io.n_kv + keys - 1) / keys); };
+  if constexpr (KT != Keys::kF32) {
+    if (groups(256) >= 4 * num_cu) return launch_many<KT, D, 4, 1, 2>(io, planes, stream);
+  }
+  if (groups(128) >= 2 * num_cu) return launch_many<KT, D, 4, 1, 1>(io, planes, stream);
+  if (groups(64) >= 2 * num_cu) return launch_many<KT, D, 2, 2, 1>(io, planes, stream);
+  return launch_many<KT, D, 1, 4, 1>(io, planes, stream);
+}
+
+}  // namespace
+
+hipError_t launch_key_weights(const KeyWeightsArgs& a, hipStream_t stream) {
+  const int32_t elem = a.bf16 ? 2 : 4, group = a.H / a.H_kv;
+  WeightsIO io;
+  io.q = static_cast<const char*>(a.q);
+  io.k = a.k ? static_cast<const char*>(a.k) : reinterpret_cast<const char*>(a.c4.k);
+  io.ks = a.k ? nullptr : a.c4.ks;
+  io.lse = a.lse;
+  io.w_old = a.w_old;
+  io.w = a.w;
+  io.kv_len = a.kv_len;
+  io.q_bh_stride = a.q_bh_stride * elem;
+  io.k_bh_stride = a.k ? a.k_bh_stride * elem : a.c4.bh_stride;
+  io.ks_bh_stride = a.k ? 0 : a.c4.sc_stride;
+  io.w_bh_stride = a.w_bh_stride;
+  io.n_q = a.n_q;
+  io.rows = group * a.n_q;
+  io.group = group;
+  io.H_kv = a.H_kv;
+  io.n_kv = a.n_kv;
+  io.n_old = a.n_old;
+  io.slabs = 0;
+  io.flat = group == 1 || a.q_bh_stride == (int64_t)a.n_q * a.d;
+  io.scale_log2 = a.softmax_scale * kLog2e;
+  io.decay = a.decay;
+  const int32_t planes = a.B * a.H_kv;
+  if (!a.k) return a.d == 128 ? launch_weights<Keys::kQ4, 128>(io, planes, a.num_cu, stream) : launch_weights<Keys::kQ4, 64>(io, planes, a.num_cu, stream);
+  if (a.bf16) return a.d == 128 ? launch_weights<Keys::kBf16, 128>(io, planes, a.num_cu, stream) : launch_weights<Keys::kBf16, 64>(io, planes, a.num_cu, stream);
+  return a.d == 128 ? launch_weights<Keys::kF32, 128>(io, planes, a.num_cu, stream) : launch_weights<Keys::kF32, 64>(io, planes, a.num_cu, stream);
+}
+
+}  // namespace sparvar

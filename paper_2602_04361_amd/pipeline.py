@@ -295,3 +295,159 @@ class Q8SparsePath(SparsePath):
         """Every scale in order; projections: (q, k, v) of each."""
         for l, (q, k, v) in enumerate(projections, 1):
             self.step(l, q, k, v)
+
+
+class Q4SparsePath(SparsePath):
+    """One layer over a 4-bit cache that grows scale by scale, as C-ABI calls: Q8SparsePath's steps, with a scale's rows
+    appended to 16 bits first (sparvar_qkv_append), written from there (sparvar_kv_quantize_q4), and attention by
+    sparvar_dense_attn_q4_fwd and sparvar_block_sparse_attn_q4_fwd. heads as there."""
+
+    def __init__(self, geom: sv.Geometry, S, steps, B, H, d, topk, radius, heads=None, device="cuda", *, prev_dilation=0,
+                 softmax_scale=None, projection="point"):
+        super().__init__(geom, S, steps, B, H, d, topk, radius, prev_dilation=prev_dilation, device=device,
+                         softmax_scale=softmax_scale, projection=projection)
+        bf = dict(dtype=torch.bfloat16, device=device)
+        total = self.info[len(geom.h)]["n_tokens_le"]
+        self.q4 = sv.Q4Cache.empty(B, H, total, d, device)
+        self.kv_S = [torch.empty(B, H, self.info[S]["n_tokens_le"], d, **bf) for _ in range(2)]
+        self.q, self.heads, self.new = {}, {}, {}
+        most = max(i["n_tokens"] for i in self.info.values())
+        rows = [torch.empty(B * H * most * d, **bf) for _ in range(2)]
+        need = 0
+        self.out[self.S] = self.o_S
+        for l, i in self.info.items():
+            n = i["n_tokens"]
+            self.q[l] = torch.empty(B, H, n, d, **bf)
+            self.new[l] = [t[:B * H * n * d].view(B, H, n, d) for t in rows]
+            self.heads[l] = None if heads is None else heads.rows(i["token_offset"], n)
+            if l != self.S and l not in self.steps:
+                self.out[l] = torch.empty(B, H, n, d, **bf)
+                need = max(need, sv.sparvar_dense_attn_q4_workspace(B, H, H, n, i["n_tokens_le"], d))
+        self.workspace = torch.empty(need, dtype=torch.uint8, device=device) if need else None
+
+    def append(self, l, q, k, v):
+        kn, vn = self.new[l]
+        sv.sparvar_qkv_append(q, k, v, 0, self.heads[l], self.q[l], kn, vn)
+        sv.sparvar_kv_quantize_q4(kn, vn, self.info[l]["token_offset"], self.q4)
+
+    def dense(self, l):
+        sv.sparvar_dense_attn_q4_fwd(self.q[l], self.q4, self.info[l]["n_tokens_le"], self.out[l], softmax_scale=self.scale,
+                                     workspace=self.workspace)
+
+    def decision(self):
+        k, v = self.kv_S
+        sv.sparvar_kv_dequantize_q4(self.q4, 0, k, v)
+        sv.sparvar_decision_step(self.g, self.S, self.q[self.S], k, v, self.o_S, self.lse_S, self.scores, self.topk,
+                                 self.topk_idx, softmax_scale=self.scale)
+        self.map_all()
+
+    def attn_step(self, k):
+        rp, ci, _ = self.csr[k]
+        sv.sparvar_block_sparse_attn_q4_fwd(self.g, k, self.q[k], self.q4, self.out[k], rp, ci, softmax_scale=self.scale)
+
+    def step(self, l, q, k, v):
+        """Scale l from its projections to its attention output."""
+        self.append(l, q, k, v)
+        if l == self.S:
+            self.decision()
+        elif l in self.steps:
+            self.attn_step(l)
+        else:
+            self.dense(l)
+        return self.out[l]
+
+    def run(self, projections):
+        """Every scale in order; projections: (q, k, v) of each."""
+        for l, (q, k, v) in enumerate(projections, 1):
+            self.step(l, q, k, v)
+
+
+class BudgetPath:
+    """One dense layer whose 4-bit cache is held to a budget of tokens, as C-ABI calls.
+
+    step(q, k, v) takes the projections [B, n, heads, d] of the next n tokens (n <= n_max; a scale, or one token):
+      append:  norms and rotation to 16 bits (sparvar_qkv_append), rows to the cache (sparvar_kv_quantize_q4);
+      attend:  dense attention over the cache (sparvar_dense_attn_q4_fwd);
+      weigh:   what each cached key got of it, added to decay times what it had (sparvar_key_weights);
+      evict:   where more than `budget` tokens are held, the n_first first, the n_last last and those of largest weight
+               move to the other of two caches (sparvar_kv_evict), which is the cache from then on.
+    held: tokens in the cache; tokens [B, H_kv, held]: which of the sequence they are, a row for each key head.
+    heads: a NormRope whose table has a row for every token of the sequence, or None.
+    """
+
+    def __init__(self, B, H, H_kv, d, n_max, budget, n_first=0, n_last=0, heads=None, decay=1.0, device="cuda",
+                 softmax_scale=None):
+        if min(n_max, budget) < 1 or min(n_first, n_last) < 0 or n_first + n_last > budget:
+            raise ValueError("n_max and budget must be >= 1, n_first and n_last >= 0 and at most the budget together")
+        self.B, self.H, self.H_kv, self.d = B, H, H_kv, d
+        self.n_max, self.budget, self.n_first, self.n_last = int(n_max), int(budget), int(n_first), int(n_last)
+        self.heads, self.decay = heads, float(decay)
+        self.scale = float(torch.tensor(1.0 / math.sqrt(d), dtype=torch.float32)) if softmax_scale is None \
+            else float(softmax_scale)
+        cap = self.budget + self.n_max
+        self.caches = [sv.Q4Cache.empty(B, H_kv, cap, d, device) for _ in range(2)]
+        self.weights = [torch.empty(B, H_kv, cap, device=device) for _ in range(2)]
+        self.order = [torch.empty(B, H_kv, cap, dtype=torch.int64, device=device) for _ in range(2)]
+        self.kept = torch.empty(B, H_kv, self.budget, dtype=torch.int32, device=device)
+        bf = dict(dtype=torch.bfloat16, device=device)
+        self.rows = [torch.empty(B * h * self.n_max * d, **bf) for h in (H, H_kv, H_kv, H)]
+        self.lse_rows = torch.empty(B * H * self.n_max, device=device)
+        self.workspace = None
+        self.held = self.seen = 0
+
+    def _view(self, i, heads, n):
+        return self.rows[i][:self.B * heads * n * self.d].view(self.B, heads, n, self.d)
+
+    @property
+    def q4(self):
+        return self.caches[0]
+
+    @property
+    def w(self):
+        return self.weights[0]
+
+    @property
+    def tokens(self):
+        return self.order[0][:, :, :self.held]
+
+    def append(self, q, k, v):
+        n = q.shape[1]
+        if not 1 <= n <= self.n_max:
+            raise ValueError(f"a step of {n} tokens, n_max is {self.n_max}")
+        self.q, kn, vn = self._view(0, self.H, n), self._view(1, self.H_kv, n), self._view(2, self.H_kv, n)
+        heads = None if self.heads is None else self.heads.rows(self.seen, n)
+        sv.sparvar_qkv_append(q, k, v, 0, heads, self.q, kn, vn)
+        sv.sparvar_kv_quantize_q4(kn, vn, self.held, self.q4)
+        self.order[0][:, :, self.held:self.held + n] = torch.arange(self.seen, self.seen + n, device=self.kept.device)
+        self.old, self.held, self.seen = self.held, self.held + n, self.seen + n
+
+    def attend(self):
+        n = self.q.shape[2]
+        need = sv.sparvar_dense_attn_q4_workspace(self.B, self.H, self.H_kv, n, self.held, self.d)
+        if need and (self.workspace is None or self.workspace.numel() < need):
+            self.workspace = torch.empty(need, dtype=torch.uint8, device=self.kept.device)
+        self.out, self.lse = self._view(3, self.H, n), self.lse_rows[:self.B * self.H * n].view(self.B, self.H, n)
+        sv.sparvar_dense_attn_q4_fwd(self.q, self.q4, self.held, self.out, lse=self.lse, softmax_scale=self.scale,
+                                     workspace=self.workspace if need else None)
+
+    def weigh(self):
+        sv.sparvar_key_weights(self.q, self.held, self.lse, self.w, w_old=self.w, n_old=self.old, decay=self.decay, q4=self.q4,
+                               softmax_scale=self.scale)
+
+    def evict(self):
+        if self.held <= self.budget:
+            return
+        sv.sparvar_kv_evict(self.w, self.held, self.budget, self.n_first, self.n_last, self.kept, self.weights[1],
+                            q4_src=self.q4, q4_dst=self.caches[1])
+        torch.gather(self.order[0], 2, self.kept.long(), out=self.order[1][:, :, :self.budget])
+        for pair in (self.caches, self.weights, self.order):
+            pair.reverse()
+        self.held = self.budget
+
+    def step(self, q, k, v):
+        """The next tokens from their projections to their attention output [B, H, n, d] (valid until the next step)."""
+        self.append(q, k, v)
+        self.attend()
+        self.weigh()
+        self.evict()
+        return self.out

@@ -51,6 +51,15 @@ EXPORTS = [
     "sparvar_dense_attn_q8_fwd",
     "sparvar_block_sparse_attn_q8_fwd",
     "sparvar_block_sparse_attn_q8_form",
+    "sparvar_kv_quantize_q4",
+    "sparvar_kv_dequantize_q4",
+    "sparvar_dense_attn_q4_workspace",
+    "sparvar_dense_attn_q4_form",
+    "sparvar_dense_attn_q4_fwd",
+    "sparvar_block_sparse_attn_q4_fwd",
+    "sparvar_block_sparse_attn_q4_form",
+    "sparvar_key_weights",
+    "sparvar_kv_evict",
     "sparvar_status_string",
     "sparvar_last_error",
     "sparvar_set_launch_option",
@@ -107,6 +116,11 @@ class _CQ8Cache(ctypes.Structure):
     ]
 
 
+class _CQ4Cache(ctypes.Structure):
+    _fields_ = [("capacity", ctypes.c_int32), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("bh_stride", ctypes.c_int64),
+                ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p), ("scale_bh_stride", ctypes.c_int64)]
+
+
 class _CNormRope(ctypes.Structure):
     _fields_ = [
         ("norm", ctypes.c_int32),
@@ -132,7 +146,7 @@ def load_library(path: str = LIB_PATH):
     lib = ctypes.CDLL(path)
     i32, i64, f32, vp = ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_void_p
     G = ctypes.POINTER(_CGeometry)
-    Q8, NR = ctypes.POINTER(_CQ8Cache), ctypes.POINTER(_CNormRope)
+    Q8, NR, Q4 = ctypes.POINTER(_CQ8Cache), ctypes.POINTER(_CNormRope), ctypes.POINTER(_CQ4Cache)
     sig = {
         "sparvar_scale_info": (ctypes.c_int, [G, i32, ctypes.POINTER(_CScaleInfo)]),
         "sparvar_dense_attn_fwd": (ctypes.c_int, [i32, i32, i32, i32, i32, ctypes.c_int, vp, i64, vp, vp, i64, vp,
@@ -175,6 +189,19 @@ def load_library(path: str = LIB_PATH):
         "sparvar_block_sparse_attn_q8_fwd": (ctypes.c_int, [G, i32, i32, i32, i32, i32, ctypes.c_int, vp, i64, Q8, vp, vp,
                                                             f32, vp, vp, vp, vp]),
         "sparvar_block_sparse_attn_q8_form": (ctypes.c_int, [G, i32, i32, i32, i32, i32, ctypes.POINTER(i32)]),
+        "sparvar_kv_quantize_q4": (ctypes.c_int, [i32, i32, i32, ctypes.c_int, i32, i32, vp, vp, i64, Q4, vp]),
+        "sparvar_kv_dequantize_q4": (ctypes.c_int, [i32, i32, i32, ctypes.c_int, i32, i32, Q4, vp, vp, i64, vp]),
+        "sparvar_dense_attn_q4_workspace": (i64, [i32, i32, i32, i32, i32, i32]),
+        "sparvar_dense_attn_q4_form": (ctypes.c_int, [i32, i32, i32, i32, i32, i32, i32, ctypes.POINTER(i32)]),
+        "sparvar_dense_attn_q4_fwd": (ctypes.c_int, [i32, i32, i32, i32, i32, i32, ctypes.c_int, vp, i64, Q4, vp, vp, vp,
+                                                     f32, vp, i64, vp]),
+        "sparvar_block_sparse_attn_q4_fwd": (ctypes.c_int, [G, i32, i32, i32, i32, i32, ctypes.c_int, vp, i64, Q4, vp, vp,
+                                                            f32, vp, vp, vp, vp]),
+        "sparvar_block_sparse_attn_q4_form": (ctypes.c_int, [G, i32, i32, i32, i32, i32, ctypes.POINTER(i32)]),
+        "sparvar_key_weights": (ctypes.c_int, [i32, i32, i32, i32, i32, i32, ctypes.c_int, vp, i64, vp, i64, Q4, vp, vp, vp,
+                                               i32, f32, vp, i64, f32, vp]),
+        "sparvar_kv_evict": (ctypes.c_int, [i32, i32, i32, ctypes.c_int, i32, i32, i32, i32, vp, vp, i64, vp, vp, i64, vp,
+                                            vp, i64, Q4, Q4, vp, vp, i64, vp]),
         "sparvar_status_string": (ctypes.c_char_p, [ctypes.c_int]),
         "sparvar_last_error": (ctypes.c_char_p, []),
         "sparvar_set_launch_option": (ctypes.c_int, [i32, i32]),
@@ -625,12 +652,21 @@ class NormRope:
         if cos_sin is not None and cos_sin.shape[2] != 2:
             raise SparvarError(ERR_INVALID, "cos_sin must be [rows, d/2, 2]")
         self.q_weight, self.k_weight, self.cos_sin = q_weight, k_weight, cos_sin
+        self.norm, self.eps, self.layout = norm, float(eps), layout
         self.device = _shared_device("NormRope", q_weight, k_weight, cos_sin)
         self.q_shape, self.k_shape = (None if t is None else tuple(t.shape) for t in (q_weight, k_weight))
         self.d = None if cos_sin is None else 2 * cos_sin.shape[1]
         self.c = _CNormRope(NORMS[norm], ROPE_LAYOUTS[layout], float(eps), 0 if cos_sin is None else cos_sin.shape[0],
                             _ptr(q_weight), _ptr(k_weight), _ptr(cos_sin))
         self.ref = ctypes.byref(self.c)
+
+
+    def rows(self, t0, n):
+        """The same for a cache whose token 0 is token t0 of this one's table: its rows [t0, t0 + n)."""
+        cs = self.cos_sin
+        if cs is not None and not 0 <= t0 <= t0 + n <= cs.shape[0]:
+            raise SparvarError(ERR_CAPACITY, f"rotation table of {cs.shape[0]} rows has no rows [{t0}, {t0 + n})")
+        return NormRope(self.norm, self.eps, self.q_weight, self.k_weight, None if cs is None else cs[t0:t0 + n], self.layout)
 
 
 def _token_strides(t, name):
@@ -687,10 +723,13 @@ def sparvar_qkv_append(q, k, v, t0, heads, q_out, k_cache=None, v_cache=None, q8
     return q_out
 
 
-def _check_q8(q8, B, H_kv, d, dev):
-    if q8.planes != (B, H_kv, d):
-        raise SparvarError(ERR_INVALID, f"the cache is [{q8.B},{q8.H_kv},{q8.capacity},{q8.d}], not of [{B},{H_kv},.,{d}]")
-    _on(dev, q8)
+def _check_cache(c, B, H_kv, d, dev):
+    if c.planes != (B, H_kv, d):
+        raise SparvarError(ERR_INVALID, f"the cache is [{c.B},{c.H_kv},{c.capacity},{c.d}], not of [{B},{H_kv},.,{d}]")
+    _on(dev, c)
+
+
+_check_q8 = _check_cache
 
 
 def _kv_planes(k, v):
@@ -741,24 +780,21 @@ def sparvar_dense_attn_q8_form(B, H, H_kv, n_q, n_kv, d, workspace):
     return tuple(form)
 
 
-def _q8_attn(q, q8, o, lse, *others):
-    """The checks that both attention calls over an 8-bit cache share."""
+def _codes_attn(q, cache, o, lse, *others):
+    """The checks that the attention calls over a cache of codes share."""
     shape = q.shape
     dt = _dtype_code(q)
     _same("o", o, shape, q.dtype)
     if lse is not None:
         _same("lse", lse, shape[:3], _torch().float32)
-    _check_q8(q8, shape[0], q8.H_kv, shape[3], _here(q, o, lse, *others))
+    _check_cache(cache, shape[0], cache.H_kv, shape[3], _here(q, o, lse, *others))
     return dt
 
 
-def sparvar_dense_attn_q8_fwd(q, q8, n_kv, o, lse=None, kv_len=None, softmax_scale=None, workspace=None, stream=None):
-    """Dense attention over the first n_kv tokens (kv_len[b] of them, int32, for entry b) of an 8-bit cache; workspace: a
-    contiguous tensor of at least sparvar_dense_attn_q8_workspace() bytes, or None; see sparvar.h."""
-    lib = load_library()
+def _dense_codes(fn, q, cache, n_kv, o, lse, kv_len, softmax_scale, workspace, stream):
     _whole("n_kv", n_kv)
     B, H, n_q, d = q.shape
-    dt = _q8_attn(q, q8, o, lse, kv_len, workspace)
+    dt = _codes_attn(q, cache, o, lse, kv_len, workspace)
     if kv_len is not None:
         _same("kv_len", kv_len, (B,), _torch().int32)
     size = 0
@@ -766,16 +802,18 @@ def sparvar_dense_attn_q8_fwd(q, q8, n_kv, o, lse=None, kv_len=None, softmax_sca
         if not workspace.is_contiguous():
             raise SparvarError(ERR_INVALID, "workspace must be contiguous")
         size = workspace.nbytes
-    _check(lib.sparvar_dense_attn_q8_fwd(B, H, q8.H_kv, n_q, n_kv, d, dt, _ptr(q), _plane_stride(q, "q"), q8.ref,
-                                         _ptr(kv_len), _ptr(o), _ptr(lse), _scale(softmax_scale, d), _ptr(workspace), size,
-                                         _stream(stream)))
+    _check(fn(B, H, cache.H_kv, n_q, n_kv, d, dt, _ptr(q), _plane_stride(q, "q"), cache.ref, _ptr(kv_len), _ptr(o), _ptr(lse),
+              _scale(softmax_scale, d), _ptr(workspace), size, _stream(stream)))
     return o, lse
 
 
-def sparvar_block_sparse_attn_q8_fwd(geom, k, q_k, q8, o, row_ptr, col_idx, lse=None, schedule=None, softmax_scale=None,
-                                     stream=None):
-    """Block-sparse attention of scale-k queries over the kept blocks of an 8-bit cache; see sparvar.h."""
-    lib = load_library()
+def sparvar_dense_attn_q8_fwd(q, q8, n_kv, o, lse=None, kv_len=None, softmax_scale=None, workspace=None, stream=None):
+    """Dense attention over the first n_kv tokens (kv_len[b] of them, int32, for entry b) of an 8-bit cache; workspace: a
+    contiguous tensor of at least sparvar_dense_attn_q8_workspace() bytes, or None; see sparvar.h."""
+    return _dense_codes(load_library().sparvar_dense_attn_q8_fwd, q, q8, n_kv, o, lse, kv_len, softmax_scale, workspace, stream)
+
+
+def _sparse_codes(fn, geom, k, q_k, cache, o, row_ptr, col_idx, lse, schedule, softmax_scale, stream):
     _whole("k", k)
     B, H, n, d = q_k.shape
     if not 1 <= k <= len(geom.h):
@@ -792,11 +830,17 @@ def sparvar_block_sparse_attn_q8_fwd(geom, k, q_k, q8, o, row_ptr, col_idx, lse=
         raise SparvarError(ERR_INVALID, f"row_ptr must hold {rows + 1} entries, and it and col_idx must be contiguous")
     if schedule is not None and (schedule.numel() < rows or not schedule.is_contiguous()):
         raise SparvarError(ERR_INVALID, f"schedule must hold {rows} entries and be contiguous")
-    dt = _q8_attn(q_k, q8, o, lse, row_ptr, col_idx, schedule)
-    _check(lib.sparvar_block_sparse_attn_q8_fwd(geom.ref, k, B, H, q8.H_kv, d, dt, _ptr(q_k), _plane_stride(q_k, "q_k"),
-                                                q8.ref, _ptr(o), _ptr(lse), _scale(softmax_scale, d), _ptr(row_ptr),
-                                                _ptr(col_idx), _ptr(schedule), _stream(stream)))
+    dt = _codes_attn(q_k, cache, o, lse, row_ptr, col_idx, schedule)
+    _check(fn(geom.ref, k, B, H, cache.H_kv, d, dt, _ptr(q_k), _plane_stride(q_k, "q_k"), cache.ref, _ptr(o), _ptr(lse),
+              _scale(softmax_scale, d), _ptr(row_ptr), _ptr(col_idx), _ptr(schedule), _stream(stream)))
     return o, lse
+
+
+def sparvar_block_sparse_attn_q8_fwd(geom, k, q_k, q8, o, row_ptr, col_idx, lse=None, schedule=None, softmax_scale=None,
+                                     stream=None):
+    """Block-sparse attention of scale-k queries over the kept blocks of an 8-bit cache; see sparvar.h."""
+    return _sparse_codes(load_library().sparvar_block_sparse_attn_q8_fwd, geom, k, q_k, q8, o, row_ptr, col_idx, lse, schedule,
+                         softmax_scale, stream)
 
 
 def sparvar_block_sparse_attn_q8_form(geom, k, B, H, H_kv, d):
@@ -805,3 +849,197 @@ def sparvar_block_sparse_attn_q8_form(geom, k, B, H, H_kv, d):
     form = (ctypes.c_int32 * 2)()
     _check(load_library().sparvar_block_sparse_attn_q8_form(geom.ref, k, B, H, H_kv, d, form))
     return tuple(form)
+
+
+# ---------------------------------------------------------------- 4-bit cache
+class Q4Cache:
+    """Host-side sparvar_q4_cache_t over device tensors: packed codes k, v [B,H_kv,capacity,d/2] (uint8, or
+    float4_e2m1fn_x2) and scale bytes k_scale, v_scale [B,H_kv,capacity,d/32] (uint8 or float8_e8m0fnu)."""
+
+    def __init__(self, k, v, k_scale, v_scale):
+        torch = _torch()
+        codes = (torch.uint8, getattr(torch, "float4_e2m1fn_x2", torch.uint8))
+        for name, t, types in (("k", k, codes), ("v", v, codes), ("k_scale", k_scale, (torch.uint8, torch.float8_e8m0fnu)),
+                               ("v_scale", v_scale, (torch.uint8, torch.float8_e8m0fnu))):
+            if t.dtype not in types:
+                raise SparvarError(ERR_UNSUPPORTED, f"{name} is {t.dtype}")
+        self.bh_stride = _plane_stride(k, "k")
+        self.B, self.H_kv, self.capacity, half = k.shape
+        self.d = 2 * half
+        if self.d not in (64, 128):
+            raise SparvarError(ERR_UNSUPPORTED, f"head dim {self.d} not supported (64 or 128)")
+        if k.shape != v.shape or _plane_stride(v, "v") != self.bh_stride:
+            raise SparvarError(ERR_INVALID, "k and v must share their shape and plane stride")
+        scales = (self.B, self.H_kv, self.capacity, self.d // 32)
+        for name, t in (("k_scale", k_scale), ("v_scale", v_scale)):
+            if t.shape != scales or _plane_stride(t, name) != _plane_stride(k_scale, "k_scale"):
+                raise SparvarError(ERR_INVALID, f"{name} must be {list(scales)} with evenly spaced planes, as the other's")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.device = _shared_device("Q4Cache", k, v, k_scale, v_scale)
+        self.planes = (self.B, self.H_kv, self.d)
+        self.c = _CQ4Cache(self.capacity, k.data_ptr(), v.data_ptr(), self.bh_stride, k_scale.data_ptr(), v_scale.data_ptr(),
+                           _plane_stride(k_scale, "k_scale"))
+        self.ref = ctypes.byref(self.c)
+
+    @classmethod
+    def empty(cls, B, H_kv, capacity, d, device="cuda"):
+        """A cache of unwritten tokens."""
+        torch = _torch()
+        if d not in (64, 128):
+            raise SparvarError(ERR_UNSUPPORTED, f"head dim {d} not supported (64 or 128)")
+        if min(B, H_kv, capacity) < 1:
+            raise SparvarError(ERR_INVALID, f"a cache of [{B},{H_kv},{capacity},{d}] is empty")
+        return cls(*(torch.empty(B, H_kv, capacity, n, dtype=torch.uint8, device=device) for n in (d // 2, d // 2, d // 32, d // 32)))
+
+
+def sparvar_kv_quantize_q4(k_src, v_src, t0, q4, stream=None):
+    """Write rows of k_src, v_src [B,H_kv,n,d] to tokens [t0, t0 + n) of a 4-bit cache; see sparvar.h."""
+    lib = load_library()
+    _whole("t0", t0)
+    B, H_kv, n, d = k_src.shape
+    stride, dev = _kv_planes(k_src, v_src)
+    _check_cache(q4, B, H_kv, d, dev)
+    _check(lib.sparvar_kv_quantize_q4(B, H_kv, d, _dtype_code(k_src), n, t0, _ptr(k_src), _ptr(v_src), stride, q4.ref,
+                                      _stream(stream)))
+    return q4
+
+
+def sparvar_kv_dequantize_q4(q4, t0, k_dst, v_dst, stream=None):
+    """Read tokens [t0, t0 + n) of a 4-bit cache back to k_dst, v_dst [B,H_kv,n,d]; see sparvar.h."""
+    lib = load_library()
+    _whole("t0", t0)
+    B, H_kv, n, d = k_dst.shape
+    stride, dev = _kv_planes(k_dst, v_dst)
+    _check_cache(q4, B, H_kv, d, dev)
+    _check(lib.sparvar_kv_dequantize_q4(B, H_kv, d, _dtype_code(k_dst), n, t0, q4.ref, _ptr(k_dst), _ptr(v_dst), stride,
+                                        _stream(stream)))
+    return k_dst, v_dst
+
+
+def sparvar_dense_attn_q4_workspace(B, H, H_kv, n_q, n_kv, d):
+    """Bytes of workspace with which a dense call of these sizes cuts its keys into parts (0: it does not)."""
+    _whole("sizes", B, H, H_kv, n_q, n_kv, d)
+    n = load_library().sparvar_dense_attn_q4_workspace(B, H, H_kv, n_q, n_kv, d)
+    if n < 0:
+        _check(int(n))
+    return int(n)
+
+
+def sparvar_dense_attn_q4_form(B, H, H_kv, n_q, n_kv, d, workspace):
+    """(waves, sets, parts) that a dense call of these sizes walks with, with a workspace or without; see sparvar.h."""
+    _whole("sizes", B, H, H_kv, n_q, n_kv, d)
+    form = (ctypes.c_int32 * 3)()
+    _check(load_library().sparvar_dense_attn_q4_form(B, H, H_kv, n_q, n_kv, d, int(workspace), form))
+    return tuple(form)
+
+
+def sparvar_dense_attn_q4_fwd(q, q4, n_kv, o, lse=None, kv_len=None, softmax_scale=None, workspace=None, stream=None):
+    """Dense attention over the first n_kv tokens (kv_len[b] of them, int32, for entry b) of a 4-bit cache; workspace: a
+    contiguous tensor of at least sparvar_dense_attn_q4_workspace() bytes, or None; see sparvar.h."""
+    return _dense_codes(load_library().sparvar_dense_attn_q4_fwd, q, q4, n_kv, o, lse, kv_len, softmax_scale, workspace, stream)
+
+
+def sparvar_block_sparse_attn_q4_fwd(geom, k, q_k, q4, o, row_ptr, col_idx, lse=None, schedule=None, softmax_scale=None,
+                                     stream=None):
+    """Block-sparse attention of scale-k queries over the kept blocks of a 4-bit cache; see sparvar.h."""
+    return _sparse_codes(load_library().sparvar_block_sparse_attn_q4_fwd, geom, k, q_k, q4, o, row_ptr, col_idx, lse, schedule,
+                         softmax_scale, stream)
+
+
+def sparvar_block_sparse_attn_q4_form(geom, k, B, H, H_kv, d):
+    """(waves, parts of a row) that a block-sparse call of these sizes walks with; see sparvar.h."""
+    _whole("sizes", k, B, H, H_kv, d)
+    form = (ctypes.c_int32 * 2)()
+    _check(load_library().sparvar_block_sparse_attn_q4_form(geom.ref, k, B, H, H_kv, d, form))
+    return tuple(form)
+
+
+# ---------------------------------------------------------------- a cache within a budget
+def _weight_planes(name, t, B, H_kv, n):
+    """Plane stride of fp32 weights [B,H_kv,>= n] with evenly spaced planes."""
+    if t.dtype != _torch().float32:
+        raise SparvarError(ERR_INVALID, f"{name} is {t.dtype}, float32 is required")
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 3 or shape[:2] != (B, H_kv) or shape[2] < n or (shape[2] > 1 and stride[2] != 1):
+        raise SparvarError(ERR_INVALID, f"{name} must be [{B},{H_kv},>= {n}] with rows contiguous")
+    # (an axis of one has no stride of its own)
+    plane = stride[1] if H_kv > 1 else (stride[0] if B > 1 else shape[2])
+    if B > 1 and H_kv > 1 and stride[0] != H_kv * plane:
+        raise SparvarError(ERR_INVALID, f"{name} planes must be evenly spaced")
+    return plane
+
+
+def sparvar_key_weights(q, n_kv, lse, w, w_old=None, n_old=None, decay=1.0, k_cache=None, q4=None, kv_len=None,
+                        softmax_scale=None, stream=None):
+    """Attention weight that the first n_kv keys (kv_len[b] of them, int32, for entry b) of k_cache [B,H_kv,tokens,d] or of a
+    4-bit cache q4 got from queries q [B,H,n_q,d] with softmax denominators lse: w = decay * w_old + it, w_old counting for
+    the first n_old keys (default: all, or none without w_old); see sparvar.h."""
+    lib = load_library()
+    _whole("n_kv", n_kv)
+    B, H, n_q, d = q.shape
+    dt = _dtype_code(q)
+    if n_old is None:
+        n_old = 0 if w_old is None else n_kv
+    _whole("n_old", n_old)
+    _same("lse", lse, (B, H, n_q), _torch().float32)
+    dev = _here(q, lse, w, w_old, k_cache, kv_len)
+    if (k_cache is None) == (q4 is None):
+        raise SparvarError(ERR_INVALID, "either k_cache or a 4-bit cache is required")
+    if q4 is not None:
+        _check_cache(q4, B, q4.H_kv, d, dev)
+        H_kv, ks = q4.H_kv, 0
+    else:
+        H_kv, ks = k_cache.shape[1], _plane_stride(k_cache, "k_cache")
+        if k_cache.dtype != q.dtype or k_cache.shape[0] != B or k_cache.shape[3] != d:
+            raise SparvarError(ERR_INVALID, f"k_cache must be [{B},H_kv,tokens,{d}] of {q.dtype}")
+        if n_kv > k_cache.shape[2]:
+            raise SparvarError(ERR_CAPACITY, f"{n_kv} keys exceed the cache's {k_cache.shape[2]}")
+    if kv_len is not None:
+        _same("kv_len", kv_len, (B,), _torch().int32)
+    ws = _weight_planes("w", w, B, H_kv, n_kv)
+    if w_old is not None and _weight_planes("w_old", w_old, B, H_kv, n_kv) != ws:
+        raise SparvarError(ERR_INVALID, "w and w_old must share their plane stride")
+    _check(lib.sparvar_key_weights(B, H, H_kv, n_q, n_kv, d, dt, _ptr(q), _plane_stride(q, "q"), _ptr(k_cache), ks,
+                                   None if q4 is None else q4.ref, _ptr(lse), _ptr(kv_len), _ptr(w_old), n_old, float(decay),
+                                   _ptr(w), ws, _scale(softmax_scale, d), _stream(stream)))
+    return w
+
+
+def sparvar_kv_evict(w, n, n_keep, n_first, n_last, kept, w_out, k_src=None, v_src=None, k_dst=None, v_dst=None, q4_src=None,
+                     q4_dst=None, kv_len=None, stream=None):
+    """Of the first n tokens (kv_len[b] of them, int32, for entry b) of k_src, v_src [B,H_kv,tokens,d] or of a 4-bit cache,
+    move the n_first first, the n_last last and those of largest weight w [B,H_kv,>= n] to rows [0, n_keep) of k_dst, v_dst
+    or q4_dst; kept int32 [B,H_kv,n_keep] gets their tokens (-1: none), w_out [B,H_kv,>= n_keep] their weights; see
+    sparvar.h."""
+    lib = load_library()
+    _whole("n, n_keep, n_first, n_last", n, n_keep, n_first, n_last)
+    torch = _torch()
+    if len(w.shape) != 3:
+        raise SparvarError(ERR_INVALID, "w must be [B,H_kv,tokens]")
+    B, H_kv = w.shape[:2]
+    dev = _here(w, kept, w_out, k_src, v_src, k_dst, v_dst, kv_len)
+    _same("kept", kept, (B, H_kv, n_keep), torch.int32)
+    if kv_len is not None:
+        _same("kv_len", kv_len, (B,), torch.int32)
+    ws, wo = _weight_planes("w", w, B, H_kv, n), _weight_planes("w_out", w_out, B, H_kv, n_keep)
+    four = [t is not None for t in (q4_src, q4_dst)]
+    if any(four):
+        if not all(four) or any(t is not None for t in (k_src, v_src, k_dst, v_dst)):
+            raise SparvarError(ERR_INVALID, "either k and v or 4-bit caches are required, both ways")
+        d, dt, ss, ds = q4_src.d, BF16, 0, 0
+        _check_cache(q4_src, B, H_kv, d, dev)
+        _check_cache(q4_dst, B, H_kv, d, dev)
+    else:
+        if any(t is None for t in (k_src, v_src, k_dst, v_dst)):
+            raise SparvarError(ERR_INVALID, "either k and v or 4-bit caches are required, both ways")
+        (ss, _), (ds, _) = _kv_planes(k_src, v_src), _kv_planes(k_dst, v_dst)
+        d, dt = k_src.shape[3], _dtype_code(k_src)
+        for name, t, rows in (("k_src", k_src, n), ("k_dst", k_dst, n_keep)):
+            if t.dtype != k_src.dtype or t.shape[:2] != (B, H_kv) or t.shape[3] != d:
+                raise SparvarError(ERR_INVALID, f"{name} must be [{B},{H_kv},tokens,{d}] of {k_src.dtype}")
+            if rows > t.shape[2]:
+                raise SparvarError(ERR_CAPACITY, f"{rows} tokens exceed the {t.shape[2]} of {name}")
+    _check(lib.sparvar_kv_evict(B, H_kv, d, dt, n, n_keep, n_first, n_last, _ptr(kv_len), _ptr(w), ws, _ptr(k_src),
+                                _ptr(v_src), ss, _ptr(k_dst), _ptr(v_dst), ds, None if q4_src is None else q4_src.ref,
+                                None if q4_dst is None else q4_dst.ref, _ptr(kept), _ptr(w_out), wo, _stream(stream)))
+    return kept
