@@ -1,12 +1,14 @@
 // Eviction: of a plane's tokens the first ones, the last ones and those of largest weight move, in
 // order, to a cache of their own.
 //
-// The largest weights are found by their bits: a weight's 32 bits, mapped so that unsigned order is
-// the weights' order, are taken 11, 11 and 10 at a time from the top; a histogram in LDS of those
-// that share the digits found so far tells the next digit of the smallest weight that stays, and how
-// many equal to it do (the first ones). One launch: every workgroup of a plane finds the same
-// threshold and the same places by itself, from the plane's weights, and then copies its own run of
-// kept rows, which is what takes the time: it is bound by memory.
+// The largest weights are found by their bits, mapped so that unsigned order is the weights' order.
+// Of many tokens a sample tells first between which two weights the threshold lies; of those between,
+// a histogram in LDS of the distance to the lower one, its topmost 11 bits, tells those of the
+// smallest weight that stays, a second one of the weights that share them the next, until all are
+// known, and how many equal to it do (the first ones). Where the sample was wrong the same is done
+// between the smallest and the largest weight there is. One launch: every workgroup of a plane finds
+// the same threshold and the same places by itself, from the plane's weights, and then copies its own
+// run of kept rows, which is what takes the time: it is bound by memory.
 #include "device_common.h"
 #include "launch.h"
 
@@ -17,7 +19,8 @@ namespace {
 constexpr int kNT = 1024, kNW = kNT / 64;
 constexpr int kBins = 2048;
 constexpr int kRun = 4096;       // kept rows of a workgroup, at most
-constexpr int kTileRows = 64;    // rows of kNT weights that places are counted over at once
+constexpr int kSpan = 4 * kNT;   // tokens of a row: four neighbouring ones a thread
+constexpr int kTileRows = 16;    // rows that places are counted over at once
 
 struct EvictIO {
   KvEvictArgs a;
@@ -33,39 +36,120 @@ __device__ __forceinline__ uint32_t rank_of(float w) {
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
-// Ranks of a thread's tokens (every kNT-th of the plane, those outside [lo, hi) 0): KPT of them in
-// registers, or read again each time.
-template <int KPT>
+typedef __attribute__((ext_vector_type(4), aligned(4))) float f32x4_any;  // (at any weight)
+
+// Ranks of four weights. Weights are sums of probabilities: none of a wave's is below zero or NaN but
+// for odd inputs, and then their bits need only the topmost set.
+__device__ __forceinline__ u32x4 ranks_of(f32x4_any x) {
+  u32x4 o;
+  bool odd = false;
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    const uint32_t b = __float_as_uint(x[c]);
+    odd |= b > 0x7f800000u;
+    o[c] = b | 0x80000000u;
+  }
+  if (__builtin_amdgcn_ballot_w64(odd)) {
+#pragma unroll
+    for (int c = 0; c < 4; ++c) o[c] = rank_of(x[c]);
+  }
+  return o;
+}
+
+// Ranks of a thread's tokens (four of each row; those outside [lo, hi) 0): ROWS rows in registers, or
+// read again each time.
+template <int ROWS>
 struct Ranks {
   const float* w;
   int32_t lo, hi;
-  uint32_t r[KPT > 0 ? KPT : 1];
-  __device__ __forceinline__ uint32_t read(int32_t at) const {
-    const uint32_t x = rank_of(w[at < hi ? at : hi - 1]);
-    return at >= lo && at < hi ? x : 0u;
+  u32x4 r[ROWS > 0 ? ROWS : 1];
+  __device__ __forceinline__ u32x4 read(int32_t row) const {
+    const int32_t at = row * kSpan + 4 * (int32_t)threadIdx.x;
+    if (row * kSpan >= lo && (row + 1) * kSpan <= hi) return ranks_of(*reinterpret_cast<const f32x4_any*>(w + at));
+    u32x4 o = {0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+      if (at + c >= lo && at + c < hi) o[c] = rank_of(w[at + c]);
+    return o;
   }
   __device__ __forceinline__ void load() {
-    if constexpr (KPT > 0) {
+    if constexpr (ROWS > 0) {
 #pragma unroll
-      for (int i = 0; i < KPT; ++i) r[i] = read(i * kNT + (int32_t)threadIdx.x);
+      for (int i = 0; i < ROWS; ++i) r[i] = read(i);
     }
   }
-  __device__ __forceinline__ uint32_t get(int32_t base, int i) const {
-    if constexpr (KPT > 0) return r[i];
-    else return read(base + i * kNT + (int32_t)threadIdx.x);
+  __device__ __forceinline__ u32x4 get(int32_t first, int i) const {
+    if constexpr (ROWS > 0) return r[i];
+    else return read(first + i);
   }
 };
 
-template <int KPT>
+// x that the compiler takes for a new value: comparisons with it are made where they stand, not held
+// from a pass before as 48 masks.
+__device__ __forceinline__ uint32_t uniform_bits(uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); }
+__device__ __forceinline__ uint32_t fresh(uint32_t x) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile("" : "+s"(x));
+#endif
+  return x;
+}
+
+// Rows in turn: comparisons or LDS reads of all of them ahead would take a register each.
+__device__ __forceinline__ void next_row() { __builtin_amdgcn_sched_barrier(0); }
+
+constexpr int kSample = 128, kLast = 64;
+struct EvictLds {
+  int32_t list[kRun];
+  uint32_t hist[kBins];
+  int2 at[kTileRows * kNW];      // of each row and wave: ranks above the threshold, and equal to it (then those before)
+  int32_t wt[kNW], above[kNW];
+  uint32_t found[3], bound[2];
+  uint32_t last[kLast];
+  int32_t n_last;
+  uint32_t sample[kSample];
+  int32_t place[kSample];
+};
+
+__device__ __forceinline__ int32_t wave_sum(int32_t x) {
+  return __builtin_amdgcn_readlane(wave_incl_scan(x), 63);
+}
+
+// The bin, from the top, in which `need` ranks are reached, and how many of it are needed (false:
+// there are not so many), and how many it holds. Clears the bins. `over`: ranks above those counted,
+// of the wave.
+__device__ __forceinline__ bool pick_digit(EvictLds& s, int32_t over, int32_t& need, uint32_t& digit, int32_t& held) {
+  const int tid = threadIdx.x, top = kBins - 1 - 2 * tid;
+  if ((tid & 63) == 0) s.above[tid >> 6] = over;
+  __syncthreads();
+  const uint2 h = *reinterpret_cast<const uint2*>(&s.hist[top - 1]);
+  *reinterpret_cast<uint2*>(&s.hist[top - 1]) = make_uint2(0u, 0u);
+  int32_t all_over = 0;
+#pragma unroll
+  for (int i = 0; i < kNW; ++i) all_over += s.above[i];
+  const int32_t h1 = (int32_t)h.y, h0 = (int32_t)h.x, left = need - all_over;
+  int32_t all;
+  const int32_t above = block_excl_scan<kNT>(h1 + h0, s.wt, all);
+  if (left <= 0 || left > all) return false;  // (the same for all)
+  if (above < left && left <= above + h1 + h0) {
+    const bool first = left <= above + h1;
+    s.found[0] = (uint32_t)(first ? top : top - 1);
+    s.found[1] = (uint32_t)(left - above - (first ? 0 : h1));
+    s.found[2] = (uint32_t)(first ? h1 : h0);
+  }
+  __syncthreads();
+  digit = s.found[0];
+  need = (int32_t)s.found[1];
+  held = (int32_t)s.found[2];
+  return true;
+}
+
+template <int ROWS>
 __global__ __launch_bounds__(kNT) void kv_evict_kernel(EvictIO io) {
-  __shared__ uint32_t hist[kBins];
-  __shared__ int32_t list[kRun];
-  __shared__ int32_t counts[kTileRows * kNW];
-  __shared__ int32_t wt[kNW];
-  __shared__ uint32_t found[2];
+  __shared__ __attribute__((aligned(16))) EvictLds s;
   const KvEvictArgs& a = io.a;
   const int32_t slice = blockIdx.x % io.slices, plane = blockIdx.x / io.slices;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  int32_t* const list = s.list;
   int32_t len = a.n;
   if (a.kv_len) {
     const int32_t l = a.kv_len[plane / a.H_kv];
@@ -74,93 +158,239 @@ __global__ __launch_bounds__(kNT) void kv_evict_kernel(EvictIO io) {
   const float* w = a.w + (int64_t)plane * a.w_bh_stride;
   const int32_t m = len < a.n_keep ? len : a.n_keep;
   const int32_t s0 = slice * io.run, s1 = s0 + io.run < a.n_keep ? s0 + io.run : a.n_keep;  // places of this workgroup
-  if (len <= a.n_keep) {
+  const int32_t lo = a.n_first, hi = len - a.n_last;  // tokens that compete
+  int32_t need = a.n_keep - a.n_first - a.n_last;     // for so many places
+  if (len <= a.n_keep || s1 <= lo) {  // (nothing to choose, or not in these places)
     for (int32_t i = s0 + tid; i < s1; i += kNT) list[i - s0] = i;
   } else {
-    const int32_t lo = a.n_first, hi = len - a.n_last;  // tokens that compete
-    int32_t need = a.n_keep - a.n_first - a.n_last;     // places that they compete for
-    Ranks<KPT> ranks;
-    ranks.w = w, ranks.lo = lo, ranks.hi = hi;
-    ranks.load();
-    constexpr int R = KPT > 0 ? KPT : kTileRows, kUnroll = KPT > 0 ? KPT : 4;
-    const int32_t tiles = (len + R * kNT - 1) / (R * kNT);  // (one where the ranks are in registers)
-    uint32_t prefix = 0, mask = 0;
-    if (need > 0) {
-      for (int pass = 0; pass < 3; ++pass) {
-        const int shift = pass == 0 ? 21 : (pass == 1 ? 10 : 0);
-        const uint32_t bins = pass == 2 ? 1024 : 2048;
-        hist[tid] = 0;
-        hist[tid + kNT] = 0;
+    // The first tokens, then those of the others that stay, then the last tokens.
+    for (int32_t i = s0 + tid; i < s1; i += kNT) {
+      if (i < lo) list[i - s0] = i;
+      else if (i >= lo + need) list[i - s0] = hi + (i - lo - need);
+    }
+    if (need > 0 && s0 < lo + need) {
+      const int32_t many = hi - lo;
+      uint32_t from = 1u, upto = 0xffffffffu;  // the threshold lies between
+      const bool sampled = many > 2 * kSpan;
+      uint32_t mine = 0;
+      if (sampled && tid < kSample) mine = rank_of(w[lo + (int32_t)((int64_t)tid * many / kSample)]);
+      Ranks<ROWS> ranks;
+      ranks.w = w, ranks.lo = lo, ranks.hi = hi;
+      ranks.load();
+      constexpr int R = ROWS > 0 ? ROWS : kTileRows, kUnroll = ROWS > 0 ? ROWS : 4;
+      const int32_t tiles = ROWS > 0 ? 1 : (hi + R * kSpan - 1) / (R * kSpan);
+      *reinterpret_cast<uint2*>(&s.hist[2 * tid]) = make_uint2(0u, 0u);
+      if (sampled) {
+        // Descending place of each of a sample, by comparison with all of them; the threshold's is
+        // need / many of the way, give or take three and a half standard deviations.
+        if (tid < kSample) {
+          s.sample[tid] = mine;
+          s.place[tid] = 0;
+        }
+        if (tid < 2) s.bound[tid] = tid == 0 ? from : upto;
         __syncthreads();
-        for (int32_t t = 0; t < tiles; ++t) {
-          const int32_t base = t * R * kNT;
+        constexpr int kPer = kSample * kSample / kNT;  // comparisons a thread
+        const int me = tid % kSample, first = tid / kSample * kPer;
+        const uint32_t r = s.sample[me];
+        int32_t before = 0;
+#pragma unroll
+        for (int i = 0; i < kPer; i += 4) {
+          const uint4 o = *reinterpret_cast<const uint4*>(&s.sample[first + i]);
+          before += (o.x > r || (o.x == r && first + i < me)) ? 1 : 0;
+          before += (o.y > r || (o.y == r && first + i + 1 < me)) ? 1 : 0;
+          before += (o.z > r || (o.z == r && first + i + 2 < me)) ? 1 : 0;
+          before += (o.w > r || (o.w == r && first + i + 3 < me)) ? 1 : 0;
+        }
+        atomicAdd(&s.place[me], before);
+        __syncthreads();
+        const float share = (float)need / (float)many, at = share * kSample;
+        const float wide = 1.5f + 3.5f * __builtin_sqrtf(at * (1.f - share));
+        if (tid < kSample) {
+          if (at >= wide && s.place[tid] == (int32_t)(at - wide)) s.bound[1] = mine;
+          if (s.place[tid] == (int32_t)(at + wide)) s.bound[0] = mine;
+        }
+        __syncthreads();
+        from = s.bound[0];
+        upto = s.bound[1];
+      } else {
+        __syncthreads();
+      }
+      // The threshold's distance to the lower end, 11 bits a pass (high: those known, `had` bits left)
+      // until few weights share what is known: then by comparison of those.
+      uint32_t limit = 0;  // the smallest rank that stays, `need` times
+      for (bool again = true; again;) {
+        again = false;
+        const uint32_t range = upto - from;
+        uint32_t high = 0;
+        int had = 32 - __builtin_clz(range | 1u);
+        int32_t held = 0;
+        limit = from;
+        for (bool first = true; first || had > 0; first = false) {
+          const int next = had > 11 ? had - 11 : 0;
+          // ranks that share what is known: `span` from `base` on
+          const uint32_t base = fresh(uniform_bits(first ? from : from + (high << had))), top = fresh(uniform_bits(upto));
+          const uint32_t rest = top - base, width = (1u << (had & 31)) - 1u, span = first || rest < width ? rest : width;
+          int32_t over = 0;
+          if (!first && held <= kLast) {
+            if (tid == 0) s.n_last = 0;
+            __syncthreads();
+            for (int32_t t = 0; t < tiles; ++t) {
 #pragma unroll kUnroll
-          for (int i = 0; i < R; ++i) {
-            const uint32_t r = ranks.get(base, i);
-            if (r != 0u && (r & mask) == prefix) atomicAdd(&hist[(r >> shift) & (bins - 1)], 1u);
+              for (int i = 0; i < R; ++i) {
+                next_row();
+                const u32x4 r = ranks.get(t * R, i);
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                  if (r[c] - base <= span) s.last[atomicAdd(&s.n_last, 1)] = r[c];
+              }
+            }
+            __syncthreads();
+            if (tid < kLast) {  // (one wave)
+              const uint32_t me = lane < held ? s.last[lane] : 0u;
+              int32_t above = 0, equal = 0;
+              for (int32_t i = 0; i < held; ++i) {
+                const uint32_t o = (uint32_t)__builtin_amdgcn_readlane((int)me, i);
+                above += o > me ? 1 : 0;
+                equal += o == me ? 1 : 0;
+              }
+              if (lane < held && above < need && need <= above + equal) {  // (those equal to it write the same)
+                s.found[0] = me;
+                s.found[1] = (uint32_t)(need - above);
+                s.found[2] = (uint32_t)equal;
+              }
+            }
+            __syncthreads();
+            limit = s.found[0];
+            need = (int32_t)s.found[1];
+            held = (int32_t)s.found[2];
+            break;
+          }
+          if (span == 0u) {  // (many equal weights would queue up for one bin)
+            int32_t same = 0;
+            for (int32_t t = 0; t < tiles; ++t) {
+#pragma unroll kUnroll
+              for (int i = 0; i < R; ++i) {
+                next_row();
+                const u32x4 r = ranks.get(t * R, i);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                  over += r[c] > top ? 1 : 0;
+                  same += r[c] == base ? 1 : 0;
+                }
+              }
+            }
+            same = wave_sum(same);
+            if (lane == 0) atomicAdd(&s.hist[0], (uint32_t)same);
+          } else {
+            for (int32_t t = 0; t < tiles; ++t) {
+#pragma unroll kUnroll
+              for (int i = 0; i < R; ++i) {
+                next_row();
+                const u32x4 r = ranks.get(t * R, i);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                  over += r[c] > top ? 1 : 0;
+                  const uint32_t v = r[c] - base;
+                  if (v <= span) atomicAdd(&s.hist[v >> next], 1u);
+                }
+              }
+            }
+          }
+          uint32_t digit;
+          if (!pick_digit(s, first ? wave_sum(over) : 0, need, digit, held)) {  // (the first pass of a sample that was wrong)
+            from = 1u;
+            upto = 0xffffffffu;
+            again = true;
+            break;
+          }
+          high = first ? digit : high << (had - next) | digit;
+          had = next;
+          limit = from + (high << had);
+        }
+        if (!again && need == held) {  // all that are equal to it stay
+          --limit;
+          need = 0;
+        }
+      }
+      limit = uniform_bits(limit);
+      need = uniform(need);
+      // Places of those above it and of the first `need` equal to it
+      int32_t gt0 = 0, eq0 = 0;
+      for (int32_t t = 0; t < tiles; ++t) {
+        __syncthreads();
+        int gts = 0, eqs = 0;  // of row `lane`
+#pragma unroll kUnroll
+        for (int i = 0; i < R; ++i) {
+          next_row();
+          const u32x4 r = ranks.get(t * R, i);
+          const uint32_t lim = fresh(limit);
+          int32_t gt = 0, eq = 0;
+#pragma unroll
+          for (int c = 0; c < 4; ++c) gt += __builtin_popcountll(__builtin_amdgcn_ballot_w64(r[c] > lim));
+          if (need > 0) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c) eq += __builtin_popcountll(__builtin_amdgcn_ballot_w64(r[c] == lim));
+          }
+          gts = lane == i ? gt : gts;
+          eqs = lane == i ? eq : eqs;
+        }
+        if (lane < R) s.at[lane * kNW + wave] = make_int2(gts, eqs);
+        __syncthreads();
+        int2 all = make_int2(0, 0);
+        if (tid < 64) {  // the first wave adds them up, R * kNW / 64 a lane
+          constexpr int kPer = (R * kNW + 63) / 64;
+          int2 v[kPer], sum = make_int2(0, 0);
+#pragma unroll
+          for (int j = 0; j < kPer; ++j) {
+            v[j] = lane * kPer + j < R * kNW ? s.at[lane * kPer + j] : make_int2(0, 0);
+            sum.x += v[j].x;
+            sum.y += v[j].y;
+          }
+          int2 before = make_int2(wave_incl_scan(sum.x) - sum.x + gt0, wave_incl_scan(sum.y) - sum.y + eq0);
+#pragma unroll
+          for (int j = 0; j < kPer; ++j) {
+            if (lane * kPer + j < R * kNW) s.at[lane * kPer + j] = before;
+            before.x += v[j].x;
+            before.y += v[j].y;
+          }
+          if (lane == 63) {
+            s.above[0] = before.x;
+            s.above[1] = before.y;
           }
         }
         __syncthreads();
-        const int top = kBins - 1 - 2 * tid;
-        const int32_t h1 = (int32_t)hist[top], h0 = (int32_t)hist[top - 1];
-        int32_t all;
-        const int32_t above = block_excl_scan<kNT>(h1 + h0, wt, all);
-        if (above < need && need <= above + h1 + h0) {
-          const bool first = need <= above + h1;
-          found[0] = (uint32_t)(first ? top : top - 1);
-          found[1] = (uint32_t)(need - above - (first ? 0 : h1));
-        }
-        __syncthreads();
-        prefix |= found[0] << shift;
-        mask |= (bins - 1) << shift;
-        need = (int32_t)found[1];
-      }
-    }
-    // Places: the first tokens, then of the others those above the threshold and the first `need`
-    // equal to it, then the last tokens.
-    const bool some = mask != 0;
-    for (int32_t i = tid; i < a.n_first; i += kNT)
-      if (i >= s0 && i < s1) list[i - s0] = i;
-    for (int32_t i = tid; i < a.n_last; i += kNT) {
-      const int32_t p = a.n_keep - a.n_last + i;
-      if (p >= s0 && p < s1) list[p - s0] = hi + i;
-    }
-    int32_t gt0 = 0, eq0 = 0;
-    for (int32_t t = 0; some && t < tiles; ++t) {
-      const int32_t base = t * R * kNT;
-      __syncthreads();
+        all = make_int2(s.above[0], s.above[1]);
 #pragma unroll kUnroll
-      for (int i = 0; i < R; ++i) {
-        const uint32_t r = ranks.get(base, i);
-        const uint64_t gt = __builtin_amdgcn_ballot_w64(r > prefix), eq = __builtin_amdgcn_ballot_w64(r == prefix);
-        if (lane == 0) counts[i * kNW + wave] = __builtin_popcountll(gt) | __builtin_popcountll(eq) << 16;
-      }
-      __syncthreads();
-      const int32_t c = tid < R * kNW ? counts[tid] : 0;
-      int32_t gts, eqs;
-      const int32_t gt_before = block_excl_scan<kNT>(c & 0xffff, wt, gts);
-      const int32_t eq_before = block_excl_scan<kNT>(c >> 16, wt, eqs);
-      // (a tile holds at most 65536 of each; those before the tile are added below)
-      __shared__ int32_t gt_at[kTileRows * kNW], eq_at[kTileRows * kNW];
-      if (tid < R * kNW) {
-        gt_at[tid] = gt0 + gt_before;
-        eq_at[tid] = eq0 + eq_before;
-      }
-      __syncthreads();
-#pragma unroll kUnroll
-      for (int i = 0; i < R; ++i) {
-        const uint32_t r = ranks.get(base, i);
-        const uint64_t gt = __builtin_amdgcn_ballot_w64(r > prefix), eq = __builtin_amdgcn_ballot_w64(r == prefix);
-        const uint64_t below = (1ull << lane) - 1;
-        const int32_t g = gt_at[i * kNW + wave] + __builtin_popcountll(gt & below);
-        const int32_t e = eq_at[i * kNW + wave] + __builtin_popcountll(eq & below);
-        if (r > prefix || (r == prefix && e < need)) {
-          const int32_t p = a.n_first + g + (e < need ? e : need);
-          if (p >= s0 && p < s1) list[p - s0] = base + i * kNT + tid;
+        for (int i = 0; i < R; ++i) {
+          next_row();
+          const int2 at = s.at[i * kNW + wave];
+          const int32_t g0 = __builtin_amdgcn_readfirstlane(at.x), e0 = __builtin_amdgcn_readfirstlane(at.y);
+          const int32_t p0 = lo + g0 + (e0 < need ? e0 : need);
+          if (p0 + 256 <= s0 || p0 >= s1) continue;  // (no place of this workgroup's among the wave's)
+          next_row();
+          const u32x4 r = ranks.get(t * R, i);
+          const uint32_t lim = fresh(limit);
+          int32_t n = 0;
+#pragma unroll
+          for (int c = 0; c < 4; ++c) n += r[c] > lim ? 1 : 0;
+          if (need > 0) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c) n += r[c] == lim ? 0x10000 : 0;
+          }
+          n = wave_incl_scan(n) - n;
+          int32_t g = g0 + (n & 0xffff), e = e0 + (n >> 16);
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            const bool gt = r[c] > lim, eq = r[c] == lim;
+            const int32_t p = lo + g + (e < need ? e : need);
+            if ((gt || (eq && e < need)) && p >= s0 && p < s1) list[p - s0] = (t * R + i) * kSpan + 4 * tid + c;
+            g += gt ? 1 : 0;
+            e += eq ? 1 : 0;
+          }
         }
+        gt0 = all.x;
+        eq0 = all.y;
       }
-      gt0 += gts;
-      eq0 += eqs;
     }
   }
   __syncthreads();
@@ -231,8 +461,10 @@ hipError_t launch_kv_evict(const KvEvictArgs& a, hipStream_t stream) {
   io.run = (a.n_keep + slices - 1) / slices;
   io.slices = (a.n_keep + io.run - 1) / io.run;
   const dim3 grid((uint32_t)planes * io.slices);
-  if (a.n <= 8 * kNT) hipLaunchKernelGGL((kv_evict_kernel<8>), grid, dim3(kNT), 0, stream, io);
-  else if (a.n <= 48 * kNT) hipLaunchKernelGGL((kv_evict_kernel<48>), grid, dim3(kNT), 0, stream, io);
+  const int32_t rows = (a.n + kSpan - 1) / kSpan;
+  if (rows <= 2) hipLaunchKernelGGL((kv_evict_kernel<2>), grid, dim3(kNT), 0, stream, io);
+  else if (rows <= 6) hipLaunchKernelGGL((kv_evict_kernel<6>), grid, dim3(kNT), 0, stream, io);
+  else if (rows <= 12) hipLaunchKernelGGL((kv_evict_kernel<12>), grid, dim3(kNT), 0, stream, io);
   else hipLaunchKernelGGL((kv_evict_kernel<0>), grid, dim3(kNT), 0, stream, io);
   return hipGetLastError();
 }
