@@ -1417,6 +1417,7 @@ int sparvar_key_weights(int32_t B, int32_t H, int32_t H_kv, int32_t n_q, int32_t
   a.w_bh_stride = w_bh_stride;
   a.softmax_scale = softmax_scale;
   a.decay = decay;
+  a.swizzle = opt(SPARVAR_OPT_SWIZZLE);
   a.num_cu = device_cus();
   return hip_status(launch_key_weights(a, stream), "key weights launch");
 }

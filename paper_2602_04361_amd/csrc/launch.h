@@ -286,6 +286,7 @@ struct KeyWeightsArgs {
   float* w;
   int64_t w_bh_stride;
   float softmax_scale, decay;
+  int swizzle;
   int num_cu;
 };
 hipError_t launch_key_weights(const KeyWeightsArgs& a, hipStream_t stream);

@@ -30,6 +30,7 @@ struct WeightsIO {
   int64_t q_bh_stride, k_bh_stride, ks_bh_stride, w_bh_stride;  // bytes (w: elements)
   int32_t n_q, rows, group, H_kv;  // rows = group * n_q: those of a key head
   int32_t n_kv, n_old, slabs;      // workgroups a plane
+  int32_t n_items, swizzle;        // workgroups doing work
   int32_t flat;                    // the rows of a group follow one another in memory
   float scale_log2, decay;
 };
@@ -101,25 +102,35 @@ __device__ __forceinline__ f32x16 unit_product(u32x4 a, u32x4 b, f32x16 c) {
   }
 }
 
+// LSEs of the 16 rows of a lane's registers, of a tile's 32 in LDS.
+struct Lse16 {
+  float v[16];
+  __device__ __forceinline__ void load(const float* tile, int half) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float4 x = *reinterpret_cast<const float4*>(tile + 8 * j + 4 * half);
+      v[4 * j] = x.x, v[4 * j + 1] = x.y, v[4 * j + 2] = x.z, v[4 * j + 3] = x.w;
+    }
+  }
+};
+
+// Keeps the computation of x where it stands.
+__device__ __forceinline__ void hold(float& x) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile("" : "+v"(x));
+#endif
+}
+
 // Sum of the 16 probabilities of a lane.
-__device__ __forceinline__ float tile_sum(const f32x16& st, const float (&lse2)[16], float scale_log2) {
+__device__ __forceinline__ float tile_sum(const f32x16& st, const Lse16& lse2, float scale_log2) {
   float p[16];
 #pragma unroll
-  for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[r], scale_log2, -lse2[r]));
+  for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[r], scale_log2, -lse2.v[r]));
 #pragma unroll
   for (int n = 8; n > 0; n >>= 1)
 #pragma unroll
     for (int r = 0; r < n; ++r) p[r] += p[r + n];
   return p[0];
-}
-
-// LSEs of the 16 rows of a lane's registers, of a tile's 32 in LDS.
-__device__ __forceinline__ void load_lse(const float* tile, int half, float (&lse2)[16]) {
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const float4 v = *reinterpret_cast<const float4*>(tile + 8 * j + 4 * half);
-    lse2[4 * j] = v.x, lse2[4 * j + 1] = v.y, lse2[4 * j + 2] = v.z, lse2[4 * j + 3] = v.w;
-  }
 }
 
 __device__ __forceinline__ int32_t length_of(const WeightsIO& io, int32_t plane) {
@@ -128,9 +139,12 @@ __device__ __forceinline__ int32_t length_of(const WeightsIO& io, int32_t plane)
   return len < 0 ? 0 : (len < io.n_kv ? len : io.n_kv);
 }
 
+__device__ __forceinline__ float weight_of(const WeightsIO& io, int32_t key, float old, float sum) {
+  return key < io.n_old ? __builtin_fmaf(io.decay, old, sum) : sum;
+}
 __device__ __forceinline__ void store_weight(const WeightsIO& io, int32_t plane, int32_t key, float sum) {
   const int64_t at = (int64_t)plane * io.w_bh_stride + key;
-  io.w[at] = key < io.n_old ? __builtin_fmaf(io.decay, io.w_old[at], sum) : sum;
+  io.w[at] = weight_of(io, key, key < io.n_old ? io.w_old[at] : 0.f, sum);
 }
 
 // 16-byte unit u of LDS row r at u ^ this.
@@ -142,8 +156,9 @@ __device__ __forceinline__ int row_swizzle(int r) {
 // Many rows: WK waves hold 32 KN keys each, and WR such sets of waves take every WR-th tile of 32
 // rows. The rows stream through LDS, RS at a time, two stages.
 template <Keys KT, int D, int WK, int WR, int KN>
-__global__ __launch_bounds__(WK * WR * 64) __attribute__((amdgpu_waves_per_eu(2))) void key_weights_kernel(WeightsIO io) {
-  constexpr int NT = WK * WR * 64, NW = WK * WR, RS = WR > 2 ? 32 * WR : 64;
+__global__ __launch_bounds__(WK * WR * 64) __attribute__((amdgpu_waves_per_eu(KN == 1 && KT != Keys::kF32 ? 3 : 2))) void key_weights_kernel(WeightsIO io) {
+  // (stages as large as leave the LDS of a CU to as many workgroups as its registers hold)
+  constexpr int NT = WK * WR * 64, NW = WK * WR, RS = KN == 2 || WR == 4 ? 128 : 64;
   constexpr int kElem = Traits<KT>::kElem, kRow = D * kElem, U = kRow / 16;
   constexpr int kLoads = RS * U / NT;
   static_assert(RS * U % NT == 0, "a stage must split evenly over the workgroup");
@@ -152,7 +167,10 @@ __global__ __launch_bounds__(WK * WR * 64) __attribute__((amdgpu_waves_per_eu(2)
   __shared__ __attribute__((aligned(16))) float lses[2][RS];
   __shared__ float sums[WR > 1 ? WR : 1][WK * KN * 32];
 
-  const int32_t slab = blockIdx.x % io.slabs, plane = blockIdx.x / io.slabs;
+  // (the workgroups of a plane on one XCD: its rows are read by all of them)
+  const int32_t item = swizzled_item(blockIdx.x, gridDim.x, io.swizzle);
+  if (item >= io.n_items) return;
+  const int32_t slab = item % io.slabs, plane = item / io.slabs;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, half = lane >> 5, wk = wave % WK, wr = wave / WK;
   const int32_t len = length_of(io, plane);
@@ -189,7 +207,60 @@ __global__ __launch_bounds__(WK * WR * 64) __attribute__((amdgpu_waves_per_eu(2)
 #pragma unroll
   for (int n = 0; n < KN; ++n) sum[n] = 0.f;
 
-  auto step = [&](int32_t s, const char* now, char* then) {
+  // Scores of a tile of rows, and under its products the probabilities of the tile before it, a
+  // share after each unit (two waves of a SIMD left to themselves go through their products side by
+  // side and then through their exponentials side by side); units are read kAhead early.
+  struct Tile {
+    f32x16 st[KN];
+    Lse16 lse2;
+  } even, odd;
+  constexpr int kUnits = U / 2, kShare = (16 + kUnits - 1) / kUnits;  // probabilities of a key after a unit
+  constexpr int kTiles = RS / 32 / WR, kAhead = KN == 1 ? 3 : 4;
+  static_assert(kTiles * 32 * WR == RS, "sets take whole tiles of a stage");
+  auto add_up = [&](const Tile& t) {
+#pragma unroll
+    for (int n = 0; n < KN; ++n) sum[n] += tile_sum(t.st[n], t.lse2, io.scale_log2);
+  };
+  const int l_row = (wr * 32 + l32) * kRow, sw = row_swizzle<U>(l32);
+  auto unit = [&](const char* now, int i) {  // unit i of the wave's tiles of a stage
+    return *reinterpret_cast<const u32x4*>(now + l_row + i / kUnits * (WR * 32 * kRow) + 16 * ((half * kUnits + i % kUnits) ^ sw));
+  };
+  u32x4 ahead[kAhead];
+  auto tile = [&](const char* now, const float* lse, int t, Tile& cur, const Tile& before) {
+    float part[KN][4];
+#pragma unroll
+    for (int n = 0; n < KN; ++n) {
+      cur.st[n] = zero16();
+#pragma unroll
+      for (int j = 0; j < 4; ++j) part[n][j] = 0.f;
+    }
+    cur.lse2.load(lse + (t * WR + wr) * 32, half);
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+      const int i = t * kUnits + u;
+      const u32x4 a = ahead[i % kAhead];
+      if (i + kAhead < kTiles * kUnits) ahead[i % kAhead] = unit(now, i + kAhead);
+#pragma unroll
+      for (int n = 0; n < KN; ++n) cur.st[n] = unit_product<KT>(a, kf[n].u[u], cur.st[n]);
+#pragma unroll
+      for (int n = 0; n < KN; ++n)
+#pragma unroll
+        for (int r = u * kShare; r < (u + 1) * kShare && r < 16; ++r) {
+          part[n][r & 3] += __builtin_amdgcn_exp2f(__builtin_fmaf(before.st[n][r], io.scale_log2, -before.lse2.v[r]));
+          hold(part[n][r & 3]);
+        }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int n = 0; n < KN; ++n) sum[n] += (part[n][0] + part[n][1]) + (part[n][2] + part[n][3]);
+  };
+  // no tile before the first: probabilities of zero
+#pragma unroll
+  for (int n = 0; n < KN; ++n) odd.st[n] = zero16();
+#pragma unroll
+  for (int r = 0; r < 16; ++r) odd.lse2.v[r] = INFINITY;
+
+  auto step = [&](int32_t s, const char* now, char* then, const float* lse, float* lse_then, bool first) {
     __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
     __syncthreads();
     float lse_next = 0.f;
@@ -198,30 +269,25 @@ __global__ __launch_bounds__(WK * WR * 64) __attribute__((amdgpu_waves_per_eu(2)
       if (tid < RS) lse_next = lse2_of(io, lp, (s + 1) * RS + tid);
     }
 #pragma unroll
-    for (int t = 0; t < RS / 32 / WR; ++t) {
-      const int rt = t * WR + wr;
-      const char* row = now + (rt * 32 + l32) * kRow;
-      const int sw = row_swizzle<U>(l32);
-      float lse2[16];
-      load_lse(&lses[s & 1][rt * 32], half, lse2);
-      f32x16 st[KN];
+    for (int i = 0; i < kAhead; ++i) ahead[i] = unit(now, i);
+    if constexpr (kTiles == 1) {
+      if (first) tile(now, lse, 0, even, odd);
+      else tile(now, lse, 0, odd, even);
+    } else {
 #pragma unroll
-      for (int n = 0; n < KN; ++n) st[n] = zero16();
-#pragma unroll
-      for (int u = 0; u < U / 2; ++u) {
-        const u32x4 a = *reinterpret_cast<const u32x4*>(row + 16 * ((half * (U / 2) + u) ^ sw));
-#pragma unroll
-        for (int n = 0; n < KN; ++n) st[n] = unit_product<KT>(a, kf[n].u[u], st[n]);
+      for (int t = 0; t < kTiles; t += 2) {
+        tile(now, lse, t, even, odd);
+        tile(now, lse, t + 1, odd, even);
       }
-#pragma unroll
-      for (int n = 0; n < KN; ++n) sum[n] += tile_sum(st[n], lse2, io.scale_log2);
     }
-    if (s + 1 < stages && tid < RS) lses[(s + 1) & 1][tid] = lse_next;
+    if (s + 1 < stages && tid < RS) lse_then[tid] = lse_next;
   };
   for (int32_t s = 0; s < stages; s += 2) {
-    step(s, stage0, stage1);
-    if (s + 1 < stages) step(s + 1, stage1, stage0);
+    step(s, stage0, stage1, lses[0], lses[1], true);
+    if (s + 1 < stages) step(s + 1, stage1, stage0, lses[1], lses[0], false);
   }
+  if (kTiles == 1 && (stages & 1)) add_up(even);
+  else add_up(odd);
 #pragma unroll
   for (int n = 0; n < KN; ++n) sum[n] = sum_halves(sum[n]);
   if constexpr (WR == 1) {
@@ -273,13 +339,19 @@ void key_weights_few_kernel(WeightsIO io, int32_t tiles) {
   const int32_t row_tiles = (io.rows + 31) / 32;
   float* lses = reinterpret_cast<float*>(smem + row_tiles * 32 * kRow);
 
-  RawKey<KT, D> raw;
-  auto load = [&](int32_t t) {
+  constexpr int kDeep = KT == Keys::kQ4 ? 4 : (KT == Keys::kBf16 ? 2 : 1);  // tiles in flight
+  RawKey<KT, D> raw[kDeep];
+  float old[kDeep];
+  const float* wo = io.w_old + (int64_t)plane * io.w_bh_stride;
+  auto load = [&](int j, int32_t t) {
     const int32_t key = t * 32 + l32;
-    raw.load(kp, ksp, (uint32_t)(key < len ? key : len - 1), half);
+    raw[j].load(kp, ksp, (uint32_t)(key < len ? key : len - 1), half);
+    old[j] = key < io.n_old ? wo[key] : 0.f;
   };
   int32_t t = first + wave;
-  if (t < end) load(t);
+#pragma unroll
+  for (int j = 0; j < kDeep; ++j)
+    if (t + j * kFewWaves < end) load(j, t + j * kFewWaves);
   for (int32_t slot = tid; slot < row_tiles * 32 * U; slot += NT) {
     const int32_t r = slot / U, i = r < io.rows ? r : io.rows - 1;
     const u32x4 v = ldg16(qp + query_at<D, kElem>(io, i) + 16 * (slot % U));
@@ -288,24 +360,39 @@ void key_weights_few_kernel(WeightsIO io, int32_t tiles) {
   if (tid < row_tiles * 32) lses[tid] = lse2_of(io, lp, tid);
   __syncthreads();
   const int sw = row_swizzle<U>(l32);
-  for (; t < end; t += kFewWaves) {
-    KeyFrag<KT, D> kf;
-    kf.take(raw);
-    if (t + kFewWaves < end) load(t + kFewWaves);
-    float sum = 0.f;
-    for (int32_t rt = 0; rt < row_tiles; ++rt) {
-      const char* row = smem + (rt * 32 + l32) * kRow;
-      float lse2[16];
-      load_lse(lses + rt * 32, half, lse2);
-      f32x16 st = zero16();
+  while (t < end) {
 #pragma unroll
-      for (int u = 0; u < U / 2; ++u)
-        st = unit_product<KT>(*reinterpret_cast<const u32x4*>(row + 16 * ((half * (U / 2) + u) ^ sw)), kf.u[u], st);
-      sum += tile_sum(st, lse2, io.scale_log2);
+    for (int j = 0; j < kDeep; ++j) {
+      if (t >= end) break;
+      KeyFrag<KT, D> kf;
+      kf.take(raw[j]);
+      const float had = old[j];
+      if (t + kDeep * kFewWaves < end) load(j, t + kDeep * kFewWaves);
+      float sum = 0.f;
+      for (int32_t rt = 0; rt < row_tiles; ++rt) {
+        const char* row = smem + (rt * 32 + l32) * kRow;
+        f32x16 st = zero16();
+#pragma unroll
+        for (int u = 0; u < U / 2; ++u)
+          st = unit_product<KT>(*reinterpret_cast<const u32x4*>(row + 16 * ((half * (U / 2) + u) ^ sw)), kf.u[u], st);
+        // (eight rows at a time, those that are there)
+        const int32_t eights = (io.rows - rt * 32 + 7) / 8;
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          if (g >= eights) break;
+          const float4 l = *reinterpret_cast<const float4*>(lses + rt * 32 + 8 * g + 4 * half);
+          const float lse2[4] = {l.x, l.y, l.z, l.w};
+          float p[4];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[4 * g + r], io.scale_log2, -lse2[r]));
+          sum += (p[0] + p[1]) + (p[2] + p[3]);
+        }
+      }
+      sum = sum_halves(sum);
+      const int32_t key = t * 32 + l32;
+      if (half == 0 && key < len) io.w[(int64_t)plane * io.w_bh_stride + key] = weight_of(io, key, had, sum);
+      t += kFewWaves;
     }
-    sum = sum_halves(sum);
-    const int32_t key = t * 32 + l32;
-    if (half == 0 && key < len) store_weight(io, plane, key, sum);
   }
 }
 
@@ -313,8 +400,40 @@ template <Keys KT, int D, int WK, int WR, int KN>
 hipError_t launch_many(WeightsIO io, int32_t planes, hipStream_t stream) {
   constexpr int32_t keys = WK * KN * 32;
   io.slabs = (io.n_kv + keys - 1) / keys;
-  hipLaunchKernelGGL((key_weights_kernel<KT, D, WK, WR, KN>), dim3(planes * io.slabs), dim3(WK * WR * 64), 0, stream, io);
+  io.n_items = planes * io.slabs;
+  const int32_t grid = io.swizzle ? (io.n_items + 7) / 8 * 8 : io.n_items;
+  hipLaunchKernelGGL((key_weights_kernel<KT, D, WK, WR, KN>), dim3(grid), dim3(WK * WR * 64), 0, stream, io);
   return hipGetLastError();
+}
+
+// Cost of 32 rows in a form of the kernel of many rows, in us, with m workgroups on the busiest CU: the larger
+// of a + b m and c m. Fits to 4096 rows and 10521 keys, 2304 / 6425, 1600 / 4121, 1024 / 2521 (4 to 32 key
+// heads) and fewer of either, us at d = 128 by workgroups of 256, 128, 64 and 32 keys (the last two with the rows
+// shared out among two and four sets of waves): 2 x 16 heads, 4096 rows 362 / 395 / 456 / 650, 1024 rows 33.6 /
+// 31.6 / 38.3 / 54.1; 8 heads, 1024 rows 20.5 / 17.3 / 16.0 / 19.5; one key head of 8, 200 rows of each, 1000
+// keys 29.4 / 24.3 / 18.1 / 13.4. (fp32 keys in registers leave no room for 256.)
+struct ManyForm {
+  int keys;
+  float a, b, c;
+};
+constexpr ManyForm kManyForms[3][4] = {
+    // d = 64, d = 128, fp32
+    {{256, 0.f, .325f, .325f}, {128, .05f, .175f, 0.f}, {64, .03f, .1f, 0.f}, {32, .02f, .06f, 0.f}},
+    {{256, .1f, .37f, .465f}, {128, .14f, .22f, .277f}, {64, .16f, .075f, .175f}, {32, .07f, .08f, .135f}},
+    {{256, INFINITY, 0.f, 0.f}, {128, 0.f, 2.05f, 0.f}, {64, .1f, 1.1f, 0.f}, {32, 0.f, .78f, 0.f}}};
+
+int many_form(bool f32, int d, int32_t planes, int32_t n_kv, int num_cu) {
+  int best = 128;
+  float least = INFINITY;
+  for (const ManyForm& f : kManyForms[f32 ? 2 : d == 128]) {
+    const int64_t groups = (int64_t)planes * ((n_kv + f.keys - 1) / f.keys);
+    const float m = (float)((groups + num_cu - 1) / num_cu), us = f.a + f.b * m > f.c * m ? f.a + f.b * m : f.c * m;
+    if (us < least) {
+      least = us;
+      best = f.keys;
+    }
+  }
+  return best;
 }
 
 template <Keys KT, int D>
@@ -331,13 +450,14 @@ hipError_t launch_weights(WeightsIO io, int32_t planes, int num_cu, hipStream_t 
                        (int32_t)tiles);
     return hipGetLastError();
   }
-  auto groups = [&](int32_t keys) { return (int64_t)planes * ((io.n_kv + keys - 1) / keys); };
-  if constexpr (KT != Keys::kF32) {
-    if (groups(256) >= 4 * num_cu) return launch_many<KT, D, 4, 1, 2>(io, planes, stream);
+  switch (many_form(KT == Keys::kF32, D, planes, io.n_kv, num_cu)) {
+    case 256:
+      if constexpr (KT != Keys::kF32) return launch_many<KT, D, 4, 1, 2>(io, planes, stream);
+      [[fallthrough]];
+    case 128: return launch_many<KT, D, 4, 1, 1>(io, planes, stream);
+    case 64: return launch_many<KT, D, 2, 2, 1>(io, planes, stream);
+    default: return launch_many<KT, D, 1, 4, 1>(io, planes, stream);
   }
-  if (groups(128) >= 2 * num_cu) return launch_many<KT, D, 4, 1, 1>(io, planes, stream);
-  if (groups(64) >= 2 * num_cu) return launch_many<KT, D, 2, 2, 1>(io, planes, stream);
-  return launch_many<KT, D, 1, 4, 1>(io, planes, stream);
 }
 
 }  // namespace
@@ -362,7 +482,8 @@ hipError_t launch_key_weights(const KeyWeightsArgs& a, hipStream_t stream) {
   io.H_kv = a.H_kv;
   io.n_kv = a.n_kv;
   io.n_old = a.n_old;
-  io.slabs = 0;
+  io.slabs = io.n_items = 0;
+  io.swizzle = a.swizzle;
   io.flat = group == 1 || a.q_bh_stride == (int64_t)a.n_q * a.d;
   io.scale_log2 = a.softmax_scale * kLog2e;
   io.decay = a.decay;

@@ -960,13 +960,21 @@ def _weight_planes(name, t, B, H_kv, n):
     if t.dtype != _torch().float32:
         raise SparvarError(ERR_INVALID, f"{name} is {t.dtype}, float32 is required")
     shape, stride = t.shape, t.stride()
-    if len(shape) != 3 or shape[:2] != (B, H_kv) or shape[2] < n or (shape[2] > 1 and stride[2] != 1):
+    if len(shape) != 3 or shape[0] != B or shape[1] != H_kv or shape[2] < n or (stride[2] != 1 and shape[2] > 1):
         raise SparvarError(ERR_INVALID, f"{name} must be [{B},{H_kv},>= {n}] with rows contiguous")
     # (an axis of one has no stride of its own)
     plane = stride[1] if H_kv > 1 else (stride[0] if B > 1 else shape[2])
     if B > 1 and H_kv > 1 and stride[0] != H_kv * plane:
         raise SparvarError(ERR_INVALID, f"{name} planes must be evenly spaced")
     return plane
+
+
+def _pair(k, v, name):
+    """Shape and plane stride of two [B,H,rows,d] tensors that share them and their dtype."""
+    shape, stride = k.shape, _plane_stride(k, name)
+    if v.shape != shape or v.dtype != k.dtype or (v.stride() != k.stride() and _plane_stride(v, name) != stride):
+        raise SparvarError(ERR_INVALID, f"{name}: k and v must share their shape, dtype and plane stride")
+    return shape, stride
 
 
 def sparvar_key_weights(q, n_kv, lse, w, w_old=None, n_old=None, decay=1.0, k_cache=None, q4=None, kv_len=None,
@@ -1013,32 +1021,32 @@ def sparvar_kv_evict(w, n, n_keep, n_first, n_last, kept, w_out, k_src=None, v_s
     sparvar.h."""
     lib = load_library()
     _whole("n, n_keep, n_first, n_last", n, n_keep, n_first, n_last)
-    torch = _torch()
-    if len(w.shape) != 3:
+    i32 = _torch().int32
+    if w.dim() != 3:
         raise SparvarError(ERR_INVALID, "w must be [B,H_kv,tokens]")
-    B, H_kv = w.shape[:2]
-    dev = _here(w, kept, w_out, k_src, v_src, k_dst, v_dst, kv_len)
-    _same("kept", kept, (B, H_kv, n_keep), torch.int32)
+    B, H_kv, _ = w.shape
+    _same("kept", kept, (B, H_kv, n_keep), i32)
     if kv_len is not None:
-        _same("kv_len", kv_len, (B,), torch.int32)
+        _same("kv_len", kv_len, (B,), i32)
     ws, wo = _weight_planes("w", w, B, H_kv, n), _weight_planes("w_out", w_out, B, H_kv, n_keep)
-    four = [t is not None for t in (q4_src, q4_dst)]
-    if any(four):
-        if not all(four) or any(t is not None for t in (k_src, v_src, k_dst, v_dst)):
+    if q4_src is None and q4_dst is None:
+        if k_src is None or v_src is None or k_dst is None or v_dst is None:
             raise SparvarError(ERR_INVALID, "either k and v or 4-bit caches are required, both ways")
+        _here(w, kept, w_out, k_src, v_src, k_dst, v_dst, kv_len)
+        (sb, sh, sn, d), ss = _pair(k_src, v_src, "the source")
+        (db, dh, dn, dd), ds = _pair(k_dst, v_dst, "the destination")
+        dt = _dtype_code(k_src)
+        if sb != B or sh != H_kv or db != B or dh != H_kv or dd != d or k_dst.dtype != k_src.dtype:
+            raise SparvarError(ERR_INVALID, f"source and destination must be [{B},{H_kv},tokens,{d}] of {k_src.dtype}")
+        if n > sn or n_keep > dn:
+            raise SparvarError(ERR_CAPACITY, f"{n} tokens of {sn}, {n_keep} kept of {dn}")
+    else:
+        if q4_src is None or q4_dst is None or not (k_src is None and v_src is None and k_dst is None and v_dst is None):
+            raise SparvarError(ERR_INVALID, "either k and v or 4-bit caches are required, both ways")
+        dev = _here(w, kept, w_out, kv_len)
         d, dt, ss, ds = q4_src.d, BF16, 0, 0
         _check_cache(q4_src, B, H_kv, d, dev)
         _check_cache(q4_dst, B, H_kv, d, dev)
-    else:
-        if any(t is None for t in (k_src, v_src, k_dst, v_dst)):
-            raise SparvarError(ERR_INVALID, "either k and v or 4-bit caches are required, both ways")
-        (ss, _), (ds, _) = _kv_planes(k_src, v_src), _kv_planes(k_dst, v_dst)
-        d, dt = k_src.shape[3], _dtype_code(k_src)
-        for name, t, rows in (("k_src", k_src, n), ("k_dst", k_dst, n_keep)):
-            if t.dtype != k_src.dtype or t.shape[:2] != (B, H_kv) or t.shape[3] != d:
-                raise SparvarError(ERR_INVALID, f"{name} must be [{B},{H_kv},tokens,{d}] of {k_src.dtype}")
-            if rows > t.shape[2]:
-                raise SparvarError(ERR_CAPACITY, f"{rows} tokens exceed the {t.shape[2]} of {name}")
     _check(lib.sparvar_kv_evict(B, H_kv, d, dt, n, n_keep, n_first, n_last, _ptr(kv_len), _ptr(w), ws, _ptr(k_src),
                                 _ptr(v_src), ss, _ptr(k_dst), _ptr(v_dst), ds, None if q4_src is None else q4_src.ref,
                                 None if q4_dst is None else q4_dst.ref, _ptr(kept), _ptr(w_out), wo, _stream(stream)))
