@@ -688,7 +688,8 @@ int sparvar_kv_dequantize_q4(int32_t B, int32_t H_kv, int32_t d, sparvar_dtype_t
 /*
  * sparvar_dense_attn_q8_fwd and its companions over a 4-bit cache: the same
  * arguments, the same treatment of queries, lengths and workspaces, on the values
- * that the codes stand for.
+ * that the codes stand for. form[1] is 0 for the form of few rows that takes 16 of
+ * them a workgroup, 1 for the one that takes 32.
  */
 int64_t sparvar_dense_attn_q4_workspace(int32_t B, int32_t H, int32_t H_kv, int32_t n_q, int32_t n_kv,
                                         int32_t d); /* bytes, < 0 on error */

@@ -316,7 +316,7 @@ __device__ __forceinline__ void wave_fence() {
 // workgroup) and sets of them that share its keys, slabs of rows, parts of the keys.
 struct DensePlan {
   int waves, sets;
-  int32_t slabs, parts;
+  int32_t slabs, parts, rows;  // rows of a slab
 };
 
 // Cost of a form, in us: with m workgroups on the busiest CU, which share it, f0 + f m for starting
@@ -324,28 +324,31 @@ struct DensePlan {
 struct DenseForm {
   int waves, sets;
   float f0, f, a, c;
+  int32_t rows = 0;  // of a workgroup, where not 32 a wave (few rows: 32)
 };
 constexpr int kMostParts = 128;
 
 template <int N>
-DensePlan plan_dense(const DenseForm (&forms)[N], float token_bytes, int32_t planes, int32_t group, int32_t n_q, int32_t n_kv, int32_t d, int num_cu, bool may_split) {
+DensePlan plan_dense(const DenseForm (&forms)[N], float token_bytes, int32_t planes, int32_t group, int32_t n_q, int32_t n_kv, int32_t d,
+                     int num_cu, bool may_split) {
   const int64_t rows = (int64_t)group * n_q, chunks = ((int64_t)n_kv + 63) / 64;
   const float memory = (float)planes * n_kv * token_bytes * (1.f / 5e6f);
-  DensePlan best{0, 1, 1, 1};
+  DensePlan best{0, 1, 1, 1, 32};
   float best_us = INFINITY;
   for (const DenseForm& f : forms) {
-    const int64_t per = f.waves ? 32 * f.waves : 32, slabs = (rows + per - 1) / per, items = planes * slabs;
+    const int64_t per = f.rows ? f.rows : (f.waves ? 32 * f.waves : 32), slabs = (rows + per - 1) / per, items = planes * slabs;
+    const int64_t sets = f.sets > 1 ? f.sets : 1;
     auto consider = [&](int64_t parts) {
       if (f.sets > 1 && items > num_cu) return;
       if (parts > 1 && (!may_split || f.sets > 1 || parts > chunks || parts > kMostParts)) return;
       const float m = (float)((items * parts + num_cu - 1) / num_cu), even = (float)(items * parts) / (float)num_cu;
-      const float walk = (float)((chunks + parts * f.sets - 1) / (parts * f.sets)) * (f.a + f.c * m);
+      const float walk = (float)((chunks + parts * sets - 1) / (parts * sets)) * (f.a + f.c * m);
       const float read = memory * (m / even) * (1.f + .25f / m);
       float us = f.f0 + f.f * m + (walk > read ? walk : read);
       if (parts > 1) us += 3.f + .08f * parts + (float)parts * planes * rows * d * (8.f / 6e6f);
       if (us < best_us) {
         best_us = us;
-        best = DensePlan{f.waves, f.sets, (int32_t)slabs, (int32_t)parts};
+        best = DensePlan{f.waves, f.sets, (int32_t)slabs, (int32_t)parts, (int32_t)per};
       }
     };
     // one part; growing numbers of parts while there is less than one workgroup a CU; whole

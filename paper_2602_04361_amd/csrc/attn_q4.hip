@@ -20,6 +20,8 @@ namespace sparvar {
 
 namespace {
 
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+
 struct Q4IO : RowsIO {
   Q4View c;
 };
@@ -438,13 +440,205 @@ void attn_q4_rows_kernel(Q4IO io, DenseRowsSrc<32> src) {
   }
 }
 
+// Up to 16 rows a workgroup: the same on 16x16x32 products, half the work of the wider ones on rows
+// that are mostly not there. A lane holds a quarter of a key's channels: 16 bytes of codes of one
+// scale at d = 128, and sixteen neighbouring keys' are 1 KB in a row for a load of the wave.
+__device__ __forceinline__ f32x4 mfma16_bf16(bf16x8 a, bf16x8 b, f32x4 c) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+#else
+  return c;
+#endif
+}
+
+// x of the lanes 16 apart and 32 apart, joined.
+__device__ __forceinline__ HalfPair rows16(float x) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return HalfPair{__uint_as_float(r[0]), __uint_as_float(r[1])};
+#else
+  return HalfPair{x, x};
+#endif
+}
+__device__ __forceinline__ float max_quarters(float x) {
+  const HalfPair p = rows16(x);
+  return max_halves(fmaxf(p.lo, p.hi));
+}
+__device__ __forceinline__ float sum_quarters(float x) {
+  const HalfPair p = rows16(x);
+  return sum_halves(p.lo + p.hi);
+}
+
+template <int D>
+__global__ __launch_bounds__(kRowWaves * 64) __attribute__((amdgpu_waves_per_eu(3)))
+void attn_q4_few_kernel(Q4IO io, DenseRowsSrc<32> src) {
+  constexpr int KC = 32, kRow = D * 2, kTile = KC * kRow;
+  constexpr int kC = D / 16;   // tiles of 16 channels
+  constexpr int kDeep = 2;     // chunks in flight
+  __shared__ __attribute__((aligned(16))) char tiles[kRowWaves][kTile];
+  __shared__ float2 ml[kRowWaves][16];
+
+  const int32_t item = swizzled_item(blockIdx.x, gridDim.x, io.swizzle);
+  if (item >= io.n_items) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int l16 = lane & 15, quarter = lane >> 4;
+
+  const QuerySet qs = src.queries(item, 0);
+  const uint8_t* kp = io.c.k + (int64_t)qs.bh * io.c.bh_stride;
+  const uint8_t* vp = io.c.v + (int64_t)qs.bh * io.c.bh_stride;
+  const uint8_t* ks = io.c.ks + (int64_t)qs.bh * io.c.sc_stride;
+  const uint8_t* vs = io.c.vs + (int64_t)qs.bh * io.c.sc_stride;
+  int vrow, vcol;
+  lane_quarter(lane, vrow, vcol);
+  const int sw = unit_swizzle(vrow) & (D / 8 - 1);
+  const DenseCursor<KC> cur = src.cursor(item, qs);
+
+  VPiece<D> kr[kDeep][2], vr[kDeep][2];
+  auto load = [&](int i, int32_t pos) {
+    const int32_t last = cur.n - 1;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int32_t k = pos + l16 + 16 * j, v = pos + vrow + 16 * j;
+      kr[i][j].load(kp, ks, (uint32_t)(k < last ? k : last), quarter);
+      vr[i][j].load(vp, vs, (uint32_t)(v < last ? v : last), vcol);
+    }
+  };
+  int32_t pos = cur.pos + wave * KC;
+#pragma unroll
+  for (int i = 0; i < kDeep; ++i)
+    if (pos + i * kRowWaves * KC < cur.n) load(i, pos + i * kRowWaves * KC);
+
+  const bool qvalid = qs.q0 + l16 < qs.q1;
+  int32_t plane, qrow;
+  src.place(qs, qvalid ? qs.q0 + l16 : qs.q0, plane, qrow);
+  const bf16_bits* q = io.q + (int64_t)plane * io.q_bh_stride + (int64_t)qrow * D + quarter * (D / 4);
+  bf16x8 qf[D / 32];
+#pragma unroll
+  for (int s = 0; s < D / 32; ++s) qf[s] = as_bf16x8(ldg16(q + 8 * s));
+
+  f32x4 acc[kC];
+#pragma unroll
+  for (int i = 0; i < kC; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m_run = kNoMax, l_run = 0.f;
+
+  // V^T: channels 16 i .. of keys 4 quarter .. + 3, and of those 16 further
+  char* const tile = tiles[wave];
+  const int tr_key = 4 * quarter + (l16 >> 2), tr_q = lane & 3, tr_sw = unit_swizzle(tr_key) & (D / 8 - 1);
+  int v_off[kC];
+#pragma unroll
+  for (int i = 0; i < kC; ++i) v_off[i] = tr_key * kRow + 16 * ((2 * i + (tr_q >> 1)) ^ tr_sw) + (tr_q & 1) * 8;
+
+  while (pos < cur.n) {
+#pragma unroll
+    for (int i = 0; i < kDeep; ++i) {
+      if (pos >= cur.n) break;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) vr[i][j].put(tile + (vrow + 16 * j) * kRow, vcol, sw);
+      wave_fence();
+      f32x4 st[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        st[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        const float f = q4_scale(kr[i][j].byte);
+#pragma unroll
+        for (int s = 0; s < D / 32; ++s) st[j] = mfma16_bf16(as_bf16x8(q4_decode8_bf16(kr[i][j].w[s], f)), qf[s], st[j]);
+      }
+      const int32_t lim = cur.n - pos - 4 * quarter;  // keys from the lane's first on
+      const int32_t next = pos + kDeep * kRowWaves * KC;
+      if (next < cur.n) load(i, next);
+      if (cur.n - pos < KC) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (16 * j + r >= lim) st[j][r] = -INFINITY;
+      }
+      float mx = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) mx = fmaxf(mx, st[j][r]);
+      mx = max_quarters(mx) * io.scale_log2;
+      if (__builtin_amdgcn_ballot_w64(mx > m_run + 8.f)) {
+        const float m_new = fmaxf(m_run, mx), alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+        l_run *= alpha;
+#pragma unroll
+        for (int c = 0; c < kC; ++c) acc[c] *= alpha;
+        m_run = m_new;
+      }
+      u32x4 pw;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        float p[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[j][r], io.scale_log2, -m_run));
+        l_run += (p[0] + p[1]) + (p[2] + p[3]);
+        pw[2 * j] = pack_bf16x2(p[0], p[1]);
+        pw[2 * j + 1] = pack_bf16x2(p[2], p[3]);
+      }
+#pragma unroll
+      for (int c = 0; c < kC; ++c) {
+        const i16x4 lo = lds_read_tr(tile + v_off[c]), hi = lds_read_tr(tile + v_off[c] + 16 * kRow);
+        const uint2 a = __builtin_bit_cast(uint2, lo), b = __builtin_bit_cast(uint2, hi);
+        acc[c] = mfma16_bf16(as_bf16x8(u32x4{a.x, a.y, b.x, b.y}), as_bf16x8(pw), acc[c]);
+      }
+      wave_fence();
+      pos += kRowWaves * KC;
+    }
+  }
+
+  // Join the waves: the row's maximum and sum, then each wave's registers through its tile; wave w
+  // finishes a quarter of the channels, in wave order.
+  const float l_own = sum_quarters(l_run);
+  if (quarter == 0) ml[wave][l16] = make_float2(m_run, l_own);
+  __syncthreads();
+  float m_g = kNoMax, l_g = 0.f;
+#pragma unroll
+  for (int w = 0; w < kRowWaves; ++w) m_g = fmaxf(m_g, ml[w][l16].x);
+#pragma unroll
+  for (int w = 0; w < kRowWaves; ++w) l_g += ml[w][l16].y * __builtin_amdgcn_exp2f(ml[w][l16].x - m_g);
+  const float own = __builtin_amdgcn_exp2f(m_run - m_g);
+  const float inv = io.part_o ? 1.f : (l_g > 0.f ? 1.f / l_g : 0.f);
+  const int64_t orow = (int64_t)plane * io.o_rows + qrow;
+  const int64_t prow = (int64_t)src.part_of(item) * io.rows + orow;
+  static_assert(kC * 4 * 256 == kTile, "a wave's sums fill its tile");
+  float* to = reinterpret_cast<float*>(tile) + lane;
+#pragma unroll
+  for (int c = 0; c < kC; ++c)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) to[(4 * c + r) * 64] = acc[c][r] * own;
+  __syncthreads();
+  if (!qvalid) return;
+#pragma unroll
+  for (int i = 0; i < kC / kRowWaves; ++i) {
+    const int c = wave * (kC / kRowWaves) + i, ch = 16 * c + 4 * quarter;
+    float r[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < kRowWaves; ++w)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) r[e] += reinterpret_cast<const float*>(tiles[w])[(4 * c + e) * 64 + lane];
+    if (io.part_o) {
+      *reinterpret_cast<float4*>(io.part_o + prow * D + ch) = make_float4(r[0], r[1], r[2], r[3]);
+    } else {
+      uint2 w;
+      w.x = pack_bf16x2(r[0] * inv, r[1] * inv);
+      w.y = pack_bf16x2(r[2] * inv, r[3] * inv);
+      *reinterpret_cast<uint2*>(io.o + orow * D + ch) = w;
+    }
+  }
+  if (wave == 0 && quarter == 0) {
+    if (io.part_o) io.part_ml[prow] = make_float2(m_g, l_g);
+    else if (io.lse) io.lse[orow] = lse_of(m_g, l_g);
+  }
+}
+
 // Costs of the forms, as of those over an 8-bit cache.
-constexpr DenseForm kDenseForms[2][5] = {
+constexpr DenseForm kDenseForms[2][6] = {
     // d = 64, d = 128
     {{0, 1, 3.f, .6f, .05f, .20f}, {2, 4, 2.5f, 3.f, 0.f, 1.38f}, {4, 1, 3.f, 1.3f, .2f, .53f}, {4, 2, 4.5f, 4.4f, 0.f, 1.15f},
-     {8, 1, 4.f, 4.4f, 0.f, 1.12f}},
+     {8, 1, 4.f, 4.4f, 0.f, 1.12f}, {0, 0, 2.f, .4f, .03f, .12f, 16}},
     {{0, 1, 2.f, 2.2f, .15f, .35f}, {2, 4, 5.f, 4.5f, 0.f, 1.92f}, {4, 1, 3.5f, 3.f, .3f, .92f}, {4, 2, 5.5f, 6.f, 0.f, 1.8f},
-     {8, 1, 5.f, 6.f, 0.f, 1.77f}}};
+     {8, 1, 5.f, 6.f, 0.f, 1.77f}, {0, 0, 2.f, 1.2f, .1f, .18f, 16}}};
 
 DensePlan dense_plan(int32_t planes, int32_t group, int32_t n_q, int32_t n_kv, int32_t d, int num_cu, bool may_split) {
   return plan_dense(kDenseForms[d == 128], 1.0625f * d, planes, group, n_q, n_kv, d, num_cu, may_split);
@@ -490,7 +684,7 @@ hipError_t launch_dense_attn_q4(const DenseQ4Args& a, hipStream_t stream) {
     src.H_kv = a.H_kv;
     src.group = group;
     src.slabs = p.slabs;
-    src.q_per_wg = p.waves ? 32 * p.waves : 32;
+    src.q_per_wg = p.rows;
     src.parts = p.parts;
     src.kv_len = a.kv_len;
     return src;
@@ -499,7 +693,9 @@ hipError_t launch_dense_attn_q4(const DenseQ4Args& a, hipStream_t stream) {
   if (p.waves == 0) {
     const int32_t grid = padded_grid(io);
     const DenseRowsSrc<32> src = fill(DenseRowsSrc<32>{});
-    if (a.d == 128) hipLaunchKernelGGL((attn_q4_rows_kernel<128>), dim3(grid), dim3(kRowWaves * 64), 0, stream, io, src);
+    if (p.sets == 0 && a.d == 128) hipLaunchKernelGGL((attn_q4_few_kernel<128>), dim3(grid), dim3(kRowWaves * 64), 0, stream, io, src);
+    else if (p.sets == 0) hipLaunchKernelGGL((attn_q4_few_kernel<64>), dim3(grid), dim3(kRowWaves * 64), 0, stream, io, src);
+    else if (a.d == 128) hipLaunchKernelGGL((attn_q4_rows_kernel<128>), dim3(grid), dim3(kRowWaves * 64), 0, stream, io, src);
     else hipLaunchKernelGGL((attn_q4_rows_kernel<64>), dim3(grid), dim3(kRowWaves * 64), 0, stream, io, src);
     e = hipGetLastError();
   } else {
