@@ -632,13 +632,19 @@ void attn_q4_few_kernel(Q4IO io, DenseRowsSrc<32> src) {
   }
 }
 
-// Costs of the forms, as of those over an 8-bit cache.
+// Costs of the forms (plan_dense). Those of the wide forms are the ones over an 8-bit cache, whose walk
+// is the same; those of few rows fit 40 calls of 1 to 4096 rows a head over 85 to 42521 keys, d = 64 and 128,
+// every form forced: the form taken is within 5% of the best in all but two (within 14%). us at d = 128 by 16
+// rows a workgroup, 32, and the best of the others: 12 heads, 160 x 600 8.5 / 9.4 / -; 16 x 4 rows on each of 4
+// heads, 1200 keys 10.6 / 10.6 (in 16 parts) / -; 2 x 16 heads, 256 x 521 10.8 / 9.9 / 15.0, 576 x 1497
+// 32.8 / 29.7 / 30.6, 1024 x 2521 - / 57.8 / 49.3; 8 heads, 1024 x 2521 24.0 / 20.0 / -. One token of 4 x 32 heads
+// on 8, 42521 keys: 40.1 in 16 or 24 parts, 42.6 in 48.
 constexpr DenseForm kDenseForms[2][6] = {
     // d = 64, d = 128
-    {{0, 1, 3.f, .6f, .05f, .20f}, {2, 4, 2.5f, 3.f, 0.f, 1.38f}, {4, 1, 3.f, 1.3f, .2f, .53f}, {4, 2, 4.5f, 4.4f, 0.f, 1.15f},
+    {{0, 1, 3.f, .6f, 0.f, .20f}, {2, 4, 2.5f, 3.f, 0.f, 1.38f}, {4, 1, 3.f, 1.3f, .2f, .53f}, {4, 2, 4.5f, 4.4f, 0.f, 1.15f},
      {8, 1, 4.f, 4.4f, 0.f, 1.12f}, {0, 0, 2.f, .4f, .03f, .12f, 16}},
-    {{0, 1, 2.f, 2.2f, .15f, .35f}, {2, 4, 5.f, 4.5f, 0.f, 1.92f}, {4, 1, 3.5f, 3.f, .3f, .92f}, {4, 2, 5.5f, 6.f, 0.f, 1.8f},
-     {8, 1, 5.f, 6.f, 0.f, 1.77f}, {0, 0, 2.f, 1.2f, .1f, .18f, 16}}};
+    {{0, 1, 2.f, 2.2f, 0.f, .32f}, {2, 4, 5.f, 4.5f, 0.f, 1.92f}, {4, 1, 3.5f, 3.f, .3f, .92f}, {4, 2, 5.5f, 6.f, 0.f, 1.8f},
+     {8, 1, 5.f, 6.f, 0.f, 1.77f}, {0, 0, 2.f, .8f, .1f, .2f, 16}}};
 
 DensePlan dense_plan(int32_t planes, int32_t group, int32_t n_q, int32_t n_kv, int32_t d, int num_cu, bool may_split) {
   return plan_dense(kDenseForms[d == 128], 1.0625f * d, planes, group, n_q, n_kv, d, num_cu, may_split);
