@@ -106,16 +106,22 @@ struct PackedCursor {
   using L = PackedLds<NT>;
   static constexpr int kGroup = NT < 512 ? NT : 511;  // entries of a fill: their count in 9 bits, their tokens in 22
   const int32_t* col;
-  int32_t nb, pos, end;       // ids below nb are blocks; entries of the row not yet decoded
+  int32_t k, pos, end;        // (the queries' scale; blocks are those of scales up to it); entries of the row not yet decoded
   int32_t n, total;           // blocks and tokens of this fill
   int32_t blk, at, stop;      // block of the wave's next position, that position, the end of its part
   char* lds;
 
   __device__ __forceinline__ bool more() const { return pos < end; }
 
+  // The thread's entry of the next kGroup ones: loaded ahead of what is waited for before fill().
+  __device__ __forceinline__ int32_t entry() const {
+    const int tid = fresh_tid();
+    return tid < kGroup && pos + tid < end ? col[pos + tid] : -1;
+  }
+
   // Decodes the next kGroup entries, a thread each (false: none left). Entries that are no blocks
   // are left out, so that no two blocks share a position.
-  __device__ __forceinline__ bool fill() {
+  __device__ __forceinline__ bool fill(int32_t v) {
     int4* info = reinterpret_cast<int4*>(lds + L::kInfo);
     int32_t* start = reinterpret_cast<int32_t*>(lds + L::kStart);
     const GeoTable& G = *reinterpret_cast<const GeoTable*>(lds + L::kGeo);
@@ -123,9 +129,12 @@ struct PackedCursor {
     total = 0;
     while (pos < end && total == 0) {
       __syncthreads();
-      const int32_t v = tid < kGroup && pos + tid < end ? col[pos + tid] : -1;
+      // (a lane holds a scale's bound, so that a search is no chain of reads)
+      const int32_t bound = G.NB[(tid & 63) < kMaxScales ? tid & 63 : kMaxScales];
+      int l = 1;
+      for (int32_t i = 1; i < k; ++i) l += v >= __builtin_amdgcn_readlane(bound, i) ? 1 : 0;
       Tile t{0, 0, 1, 1};
-      if (v >= 0 && v < nb) t = block_tile(G, v);
+      if (v >= 0 && v < __builtin_amdgcn_readlane(bound, k)) t = block_tile_in(G, l, v);
       const int32_t size = t.nr * t.nc;  // at most 4096
       int32_t sum;
       const int32_t before = block_excl_scan<NT>(size > 0 ? 1 << 22 | size : 0, reinterpret_cast<int32_t*>(lds + L::kWt), sum);
@@ -141,6 +150,7 @@ struct PackedCursor {
       if (tid == 0) start[n] = total;
       __syncthreads();
       pos += kGroup;
+      if (total == 0) v = entry();
     }
     blk = 0;
     at = 0;
@@ -209,7 +219,7 @@ struct SparseRowsSrc : SparseSrc<64> {
     const int32_t* from = reinterpret_cast<const int32_t*>(&G);  // (the first fill starts with a barrier)
     for (int i = threadIdx.x; i < kWords; i += NT) reinterpret_cast<int32_t*>(lds + PackedLds<NT>::kGeo)[i] = from[i];
     c.col = col_idx;
-    c.nb = G.NB[k];
+    c.k = k;
     c.pos = row_ptr[r];
     c.end = row_ptr[r + 1];
     c.lds = lds;

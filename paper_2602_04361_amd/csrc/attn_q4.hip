@@ -121,6 +121,12 @@ __global__ __launch_bounds__(QW * KS * 64) __attribute__((amdgpu_waves_per_eu(2)
   const int split = wave_all / QW, wave = wave_all % QW;
 
   const QuerySet qs = src.queries(item, wave);
+  auto cur = [&]() {
+    if constexpr (Src::kSparse) return src.template packed_cursor<NT>(item, tsmem);
+    else return src.cursor(item, qs);
+  }();
+  int32_t entry = 0;
+  if constexpr (Src::kSparse) entry = cur.entry();
   QFragF8<D, true> qf;
   {
     int32_t plane, qrow;
@@ -232,10 +238,6 @@ __global__ __launch_bounds__(QW * KS * 64) __attribute__((amdgpu_waves_per_eu(2)
       for (int dt = 0; dt < D / 32; ++dt) acc[dt] = mfma_bf16(vf[ks][dt], pf[ks], acc[dt]);
   };
 
-  auto cur = [&]() {
-    if constexpr (Src::kSparse) return src.template packed_cursor<NT>(item, tsmem);
-    else return src.cursor(item, qs);
-  }();
   // One pass over what the cursor holds, or over the set's part of it (a block table is filled
   // again between passes, with a barrier, so the tiles are free when a pass starts). Every
   // wave takes the steps of the longest part, and the barriers in them.
@@ -266,9 +268,10 @@ __global__ __launch_bounds__(QW * KS * 64) __attribute__((amdgpu_waves_per_eu(2)
     }
   };
   if constexpr (Src::kSparse) {
-    while (cur.fill()) {
+    while (cur.fill(entry)) {
       walk();
       if (!cur.more()) break;
+      entry = cur.entry();
     }
   } else {
     walk();
@@ -720,6 +723,11 @@ CodesForm sparse_q4_form(const GeoTable& G, int32_t k, int32_t BH, int32_t d, in
   const int32_t tile_q = G.eh[k - 1] * G.ew[k - 1];
   const int nw = waves_for(tile_q);
   const int32_t items = BH * tiles_of(G, k) * ((tile_q + nw * kQPerWave - 1) / (nw * kQPerWave));
+  // Tiles of 33 to 64 queries (8 x 8): launches of few waves a SIMD walk their rows in two parts, up to
+  // one workgroup a CU in four. us in one, two and four, rows of some 1000 tokens: d = 128, 256 workgroups
+  // 32.8 / 24.5 / 23.8, 320 41.7 / 31.4 / 41.7, 512 42.4 / 33.1 / 42.5, 640 45.0 / 47.9 / 61.4; d = 64, 256 24.5 /
+  // 17.9 / 17.2, 768 33.2 / 29.3 / 44.0, 896 34.6 / 37.5 / 54.8. Rows of 1400: 256 39.1 / 28.6 / 26.6 and
+  // 29.2 / 20.6 / 19.1; of some 300: 25.6 / 20.6 / 20.9 and 19.8 / 15.6 / 15.3.
   int32_t sets = 1;
   if (nw == 2 && items <= (d == 64 ? 3 : 2) * num_cu) sets = items <= num_cu && G.C[k] >= 640 ? 4 : 2;
   return CodesForm{nw, sets, 1};

@@ -271,7 +271,7 @@ __global__ __launch_bounds__(QW * KS * 64) __attribute__((amdgpu_waves_per_eu(2)
     }
   };
   if constexpr (Src::kSparse) {
-    while (cur.fill()) {
+    while (cur.fill(cur.entry())) {
       walk();
       if (!cur.more()) break;
     }

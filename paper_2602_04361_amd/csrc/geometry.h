@@ -68,12 +68,13 @@ SV_HD Tile tile_at(const GeoTable& G, int l, int32_t tu, int32_t tv) {
   return t;
 }
 
-SV_HD Tile block_tile(const GeoTable& G, int32_t v) {
-  const int l = block_scale(G, v);
+SV_HD Tile block_tile_in(const GeoTable& G, int l, int32_t v) {  // (l the scale of v)
   const int32_t t = v - G.NB[l - 1];
   const int32_t tu = (int32_t)div_by_magic((uint32_t)t, G.mTw[l - 1]);
   return tile_at(G, l, tu, t - tu * G.Tw[l - 1]);
 }
+
+SV_HD Tile block_tile(const GeoTable& G, int32_t v) { return block_tile_in(G, block_scale(G, v), v); }
 
 // Query Block Homography along one axis (appendix): nearest source tile of the
 // target tile's centre, rounding half up, in exact integers.
