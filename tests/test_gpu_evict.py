@@ -18,6 +18,9 @@ def weights(kind, shape, g):
         return torch.tensor([0.0, -0.0, 1.0, 1.0000001, 2.0, -1.0], device="cuda")[(w * 6).long()]
     if kind == "equal":
         return torch.full(shape, 0.25, device="cuda")
+    if kind.startswith("every"):  # one of 128 far above the others, or far below: a sample of some is like none of them
+        at = torch.arange(shape[-1], device="cuda") * 128 % (shape[-1] - 3) < 128
+        return torch.where(at, w + (9 if kind == "every high" else -9), w)
     if kind == "odd":  # infinities, NaN of both signs, subnormals
         v = torch.tensor([float("inf"), float("-inf"), float("nan"), 1e-42, 2e-42, -1e-42, 0.5], device="cuda")[(w * 7).long()]
         return torch.where(torch.rand(*shape, generator=g, device="cuda") < 0.5, v, -v)
@@ -75,6 +78,37 @@ def test_evict(cache, B, H, n, keep, first, last, d):
 def test_weights_of_any_kind(kind, n, keep, first, last):
     note(f"[evict] {kind} n={n} keep={keep}")
     run("bf16", 1, 2, n, keep, first, last, 64, kind=kind, seed=n)
+
+
+@pytest.mark.parametrize("kind", ["every high", "every low"])
+@pytest.mark.parametrize("n,keep", [(20000, 9000), (20000, 100), (20000, 19900), (50001, 25000), (70000, 35000)])
+def test_samples_that_mislead(kind, n, keep):
+    note(f"[evict] {kind} n={n} keep={keep}")
+    run("bf16", 1, 2, n, keep, 0, 0, 64, kind=kind, seed=n)
+
+
+def test_streams():
+    """Two calls side by side on streams of their own, of few tokens and of many, give what each gives alone."""
+    note("[evict] two streams")
+    jobs = []
+    for n in (700, 30000):
+        g = torch.Generator(device="cuda").manual_seed(n)
+        w = torch.rand(2, 3, n, generator=g, device="cuda")
+        x = torch.randn(2, 2, 3, n, 64, generator=g, device="cuda").bfloat16()
+        m = n // 2
+        outs = [[torch.zeros(2, 3, m, dtype=torch.int32, device="cuda"), torch.zeros(2, 3, m, device="cuda"),
+                 torch.zeros(2, 3, m, 64, device="cuda").bfloat16(), torch.zeros(2, 3, m, 64, device="cuda").bfloat16()]
+                for _ in range(2)]
+        jobs.append((w, n, m, x, torch.cuda.Stream(), *outs))
+    for w, n, m, x, _, alone, _ in jobs:
+        sv.sparvar_kv_evict(w, n, m, 4, 9, alone[0], alone[1], x[0], x[1], alone[2], alone[3])
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for w, n, m, x, stream, _, o in jobs:
+            sv.sparvar_kv_evict(w, n, m, 4, 9, o[0], o[1], x[0], x[1], o[2], o[3], stream=stream)
+    torch.cuda.synchronize()
+    for *_, alone, o in jobs:
+        assert all(torch.equal(a, b) for a, b in zip(alone, o))
 
 
 @pytest.mark.parametrize("cache", ["bf16", "q4"])

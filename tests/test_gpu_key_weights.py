@@ -99,6 +99,14 @@ def test_weights(cache, B, H, Hkv, nq, nkv, d):
     run(cache, B, H, Hkv, nq, nkv, d, seed=nq + nkv, old=nkv // 2, decay=0.75, qpad=2 * (nq % 2), empty=(0, 5, nq))
 
 
+@pytest.mark.parametrize("B,H,nkv,d", [(2, 16, 1800, 128), (2, 16, 1800, 64), (1, 8, 3000, 128), (1, 8, 1800, 64)])
+@pytest.mark.parametrize("cache", CACHES)
+def test_keys_of_a_workgroup(cache, B, H, nkv, d):
+    """As many keys as make the workgroups 256 keys each (bf16, 4 bits), 128 and 64; an odd tile of rows at the end."""
+    note(f"[key weights] forms {cache} B={B} H={H} nkv={nkv} d={d}")
+    run(cache, B, H, H, 161, nkv, d, seed=nkv + d, old=nkv - 100, decay=0.5, empty=(3, 160))
+
+
 @pytest.mark.parametrize("nq,nkv,d", [(1, 3000, 128), (200, 300, 64), (300, 900, 128)])
 @pytest.mark.parametrize("cache", CACHES)
 def test_lengths(cache, nq, nkv, d):
@@ -163,3 +171,23 @@ def test_weights_of_a_whole_attention():
     torch.cuda.synchronize()
     # (the two calls' scores may differ by the bound of attention's LSE, 2e-4)
     assert (w.double().sum(2) - nq * (H // Hkv)).abs().max() <= 2.1e-4 * nq * (H // Hkv)
+
+
+def test_streams():
+    """Two calls side by side on streams of their own, of few rows and of many, give what each gives alone."""
+    note("[key weights] two streams")
+    jobs = []
+    for nq in (1, 200):
+        q4, _, _ = make_cache(2, 2, 3000, 128, 60 + nq)
+        q = torch.randn(2, 8, nq, 128, device="cuda").bfloat16()
+        lse = torch.randn(2, 8, nq, device="cuda") + 9
+        jobs.append((q, lse, q4, torch.cuda.Stream(), torch.empty(2, 2, 3000, device="cuda"), torch.empty(2, 2, 3000, device="cuda")))
+    for q, lse, q4, _, alone, _ in jobs:
+        sv.sparvar_key_weights(q, 3000, lse, alone, q4=q4)
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for q, lse, q4, stream, _, w in jobs:
+            sv.sparvar_key_weights(q, 3000, lse, w, q4=q4, stream=stream)
+    torch.cuda.synchronize()
+    for _, _, _, _, alone, w in jobs:
+        assert torch.equal(alone, w)
