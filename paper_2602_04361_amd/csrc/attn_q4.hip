@@ -12,6 +12,13 @@
 // Scores, maxima, sums and O are held in 32 bits. The probabilities are rounded to bf16 for the
 // product with V, each off by at most 2^-8 of itself, as in the bf16 kernels (the sum that
 // divides them is that of the 32-bit ones).
+//
+// Many rows are bound by the matrix units (busy 48% of the time in the case below) and the exponentials
+// and packing in between (vector units 43%), which hardly overlap, and by the power that both draw: 2 x 16 heads,
+// 4096 x 10521, d = 128, with LSE 581 to 639 us by card (1.22 to 1.11 PFLOP/s; one large bf16 product runs at 1.34),
+// the 8-bit cache on the same cards 571 to 600. Block-sparse, the same heads' 64 x 64 scale with 1355 tokens
+// a row: 124 to 127 us (8 bits: 134 to 139), bound the same way at 37% and 48%, with every second wave's worth of V
+// converted for 64 rows alone. Short rows are bound by what stands before the first product (some 8 us).
 #include "attn_codes.h"
 #include "q4.h"
 #include "q8.h"
@@ -27,8 +34,11 @@ struct Q4IO : RowsIO {
 };
 
 // Which codes of a wave's 16 rows of V a lane loads and converts: four lanes take a row, 32 codes
-// each (16 at D = 64). Eight neighbouring lanes take a row and the one four further: their
-// 16-byte writes meet eight different groups of banks.
+// each (16 at D = 64). Eight neighbouring lanes, whose 16-byte writes go out together, take a row and
+// the one four further, which the swizzle puts in the other of two neighbouring units. At D = 128 that
+// leaves two lanes to a group of banks (14% of the LDS cycles of a dense call); without that, by other
+// rows in a lane's neighbours or by units written in another order, the dense call took as long and the
+// block-sparse one above 127 us against 124.
 __device__ __forceinline__ void lane_quarter(int lane, int& row, int& col) {
   row = ((lane >> 3) & 3) + ((lane >> 2) & 1) * 4 + (lane >> 5) * 8;
   col = lane & 3;
@@ -309,7 +319,8 @@ __global__ __launch_bounds__(QW * KS * 64) __attribute__((amdgpu_waves_per_eu(2)
 // chunk's codes in flight. K goes from registers to the products, converted: a lane holds half of a
 // key's channels, and as a sum over channels may run in any order, step s takes channels 8 s .. of
 // each half. V goes through a piece of LDS of the wave's own, for the transposing read. The four
-// waves of a workgroup take every fourth chunk of a part and join at the end.
+// waves of a workgroup take every fourth chunk of a part and join at the end. (2 x 16 heads, 256 x 521, d = 128:
+// 9.9 us; 1 x 8, 1024 x 2521: 20.)
 constexpr int kRowWaves = 4;
 
 template <int D>
@@ -445,7 +456,9 @@ void attn_q4_rows_kernel(Q4IO io, DenseRowsSrc<32> src) {
 
 // Up to 16 rows a workgroup: the same on 16x16x32 products, half the work of the wider ones on rows
 // that are mostly not there. A lane holds a quarter of a key's channels: 16 bytes of codes of one
-// scale at d = 128, and sixteen neighbouring keys' are 1 KB in a row for a load of the wave.
+// scale at d = 128, and sixteen neighbouring keys' are 1 KB in a row for a load of the wave. Bound by
+// memory: one token of 4 x 32 heads on 8, up to 42521 keys (150 MB) 32 us and 4.7 for the join of 16 parts, where a
+// large copy of as much takes 29.
 __device__ __forceinline__ f32x4 mfma16_bf16(bf16x8 a, bf16x8 b, f32x4 c) {
 #if defined(__HIP_DEVICE_COMPILE__)
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);

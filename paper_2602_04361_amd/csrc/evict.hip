@@ -8,7 +8,11 @@
 // known, and how many equal to it do (the first ones). Where the sample was wrong the same is done
 // between the smallest and the largest weight there is. One launch: every workgroup of a plane finds
 // the same threshold and the same places by itself, from the plane's weights, and then copies its own
-// run of kept rows, which is what takes the time: it is bound by memory.
+// run of kept rows, which is what takes the time: it is bound by memory. 2 x 8 heads of 128, 21260 of 42521 tokens,
+// bf16: 87 us for 354 MB, a large copy of as much 69, the difference the search of the threshold before it (117 with
+// passes over all tokens for every digit, each a histogram of one bin a weight). 460 of 921 tokens of 2 x 12 heads:
+// 11 us, all latency. Ranks stay in registers up to 49152 tokens (12 rows of 4096; 104 registers), past that they are
+// read again in every pass.
 #include "device_common.h"
 #include "launch.h"
 

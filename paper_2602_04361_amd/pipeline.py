@@ -11,7 +11,9 @@ current stream:
   map_all():  the rows of every step in one sparvar_map_index_steps launch
               (they depend only on the selection at S).
 Local rows are geometry-only and built once per step by build_local().
-Q8SparsePath runs the same steps from the projections on, over an 8-bit cache.
+Q8SparsePath runs the same steps from the projections on, over an 8-bit cache,
+Q4SparsePath over a 4-bit one. BudgetPath attends densely over a 4-bit cache of
+bounded length: what its keys got of the attention decides which ones stay.
 All arithmetic runs in libsparvar.so; this module only allocates and calls.
 """
 from __future__ import annotations
