@@ -1378,7 +1378,7 @@ int sparvar_key_weights(int32_t B, int32_t H, int32_t H_kv, int32_t n_q, int32_t
   if (st) return st;
   if ((st = check_heads(B, H, H_kv))) return st;
   if (n_q < 1 || n_kv < 1) return fail(SPARVAR_ERR_INVALID, "n_q and n_kv must be >= 1");
-  if ((int64_t)B * H * n_q >= (int64_t(1) << 31)) return fail(SPARVAR_ERR_INVALID, "B*H*n_q too large");
+  if ((int64_t)B * H * n_q >= 0x7fffff00) return fail(SPARVAR_ERR_INVALID, "B*H*n_q too large");
   if (n_kv >= 0x7fffff00) return fail(SPARVAR_ERR_INVALID, "n_kv = %d too large", n_kv);
   if ((int64_t)B * H_kv * ((n_kv + 31) / 32) >= (int64_t(1) << 31)) return fail(SPARVAR_ERR_INVALID, "too many keys for one launch");
   if ((st = check_softmax_scale(softmax_scale))) return st;

@@ -96,6 +96,7 @@ def test_sparse_arguments(bad, status):
 @pytest.mark.parametrize("bad,status", [
     (dict(d=32), UNS), (dict(dt=5), UNS), (dict(H=3), INV), (dict(B=0), INV), (dict(nq=0), INV), (dict(nkv=0), INV),
     (dict(nkv=0x7fffff00, ks=1 << 40, ws=1 << 32), INV), (dict(B=1 << 15, Hkv=1 << 15, H=1 << 15, nq=2), INV), (dict(sc=0.0), INV),
+    (dict(B=1, H=1, Hkv=1, nq=0x7fffff00, qs=1 << 38), INV),
     (dict(sc=float("nan")), INV), (dict(decay=-0.1), INV), (dict(decay=float("inf")), INV), (dict(q=None), INV), (dict(q=FAKE + 8), INV),
     (dict(qs=63), INV), (dict(k=None), INV), (dict(c=True), INV), (dict(k=FAKE + 4), INV), (dict(ks=6399), INV), (dict(lse=None), INV),
     (dict(w=None), INV), (dict(old=-1), INV), (dict(old=101), INV), (dict(old=5, w0=None), INV), (dict(ws=99), INV),
