@@ -2,7 +2,7 @@
 // order, to a cache of their own.
 //
 // The largest weights are found by their bits, mapped so that unsigned order is the weights' order.
-// Of many tokens a sample tells first between which two weights the threshold lies; of those between,
+// Of more than a few tokens a sample tells first between which two weights the threshold lies; of those between,
 // a histogram in LDS of the distance to the lower one, its topmost 11 bits, tells those of the
 // smallest weight that stays, a second one of the weights that share them the next, until all are
 // known, and how many equal to it do (the first ones). Where the sample was wrong the same is done
@@ -11,7 +11,7 @@
 // run of kept rows, which is what takes the time: it is bound by memory. 2 x 8 heads of 128, 21260 of 42521 tokens,
 // bf16: 87 us for 354 MB, a large copy of as much 69, the difference the search of the threshold before it (117 with
 // passes over all tokens for every digit, each a histogram of one bin a weight). 460 of 921 tokens of 2 x 12 heads:
-// 11 us, all latency. Ranks stay in registers up to 49152 tokens (12 rows of 4096; 104 registers), past that they are
+// 11 us, all latency. 1024 of 42521 tokens of equal weight 29 us, of different ones 27. Ranks stay in registers up to 49152 tokens (12 rows of 4096; 104 registers), past that they are
 // read again in every pass.
 #include "device_common.h"
 #include "launch.h"
@@ -175,7 +175,7 @@ __global__ __launch_bounds__(kNT) void kv_evict_kernel(EvictIO io) {
     if (need > 0 && s0 < lo + need) {
       const int32_t many = hi - lo;
       uint32_t from = 1u, upto = 0xffffffffu;  // the threshold lies between
-      const bool sampled = many > 2 * kSpan;
+      const bool sampled = many > 4 * kSample;
       uint32_t mine = 0;
       if (sampled && tid < kSample) mine = rank_of(w[lo + (int32_t)((int64_t)tid * many / kSample)]);
       Ranks<ROWS> ranks;
@@ -269,37 +269,25 @@ __global__ __launch_bounds__(kNT) void kv_evict_kernel(EvictIO io) {
             held = (int32_t)s.found[2];
             break;
           }
-          if (span == 0u) {  // (many equal weights would queue up for one bin)
-            int32_t same = 0;
-            for (int32_t t = 0; t < tiles; ++t) {
+          // (those equal to the lower end are counted apart: many equal weights, zeros of keys that got nothing
+          // among them, would queue up for one bin)
+          int32_t same = 0;
+          for (int32_t t = 0; t < tiles; ++t) {
 #pragma unroll kUnroll
-              for (int i = 0; i < R; ++i) {
-                next_row();
-                const u32x4 r = ranks.get(t * R, i);
+            for (int i = 0; i < R; ++i) {
+              next_row();
+              const u32x4 r = ranks.get(t * R, i);
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                  over += r[c] > top ? 1 : 0;
-                  same += r[c] == base ? 1 : 0;
-                }
-              }
-            }
-            same = wave_sum(same);
-            if (lane == 0) atomicAdd(&s.hist[0], (uint32_t)same);
-          } else {
-            for (int32_t t = 0; t < tiles; ++t) {
-#pragma unroll kUnroll
-              for (int i = 0; i < R; ++i) {
-                next_row();
-                const u32x4 r = ranks.get(t * R, i);
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                  over += r[c] > top ? 1 : 0;
-                  const uint32_t v = r[c] - base;
-                  if (v <= span) atomicAdd(&s.hist[v >> next], 1u);
-                }
+              for (int c = 0; c < 4; ++c) {
+                over += r[c] > top ? 1 : 0;
+                const uint32_t v = r[c] - base;
+                same += v == 0u ? 1 : 0;
+                if (v - 1u < span) atomicAdd(&s.hist[v >> next], 1u);
               }
             }
           }
+          same = wave_sum(same);
+          if (lane == 0 && same > 0) atomicAdd(&s.hist[0], (uint32_t)same);
           uint32_t digit;
           if (!pick_digit(s, first ? wave_sum(over) : 0, need, digit, held)) {  // (the first pass of a sample that was wrong)
             from = 1u;
