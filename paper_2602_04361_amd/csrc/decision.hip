@@ -149,8 +149,7 @@ __global__ __launch_bounds__(WPT * KS * 64) void decision_kernel(DecisionIO io) 
       constexpr int ST = decltype(st_c)::value;
       char* const stg = ST == 0 ? s0 : s1;
       char* const nstg = ST == 0 ? s1 : s0;
-      __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
-      __syncthreads();
+      sync_copies_and_writes();
       Chunk nxt;
       int32_t nblk = 0;
       bool nlast = false;

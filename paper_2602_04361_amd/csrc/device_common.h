@@ -342,4 +342,14 @@ __device__ __forceinline__ int32_t block_excl_scan(int32_t x, int32_t* wt, int32
 // s_waitcnt immediate for "vmcnt <= n" (gfx9 encoding; expcnt and lgkmcnt left at max).
 __host__ __device__ constexpr int waitcnt_vm(int n) { return (n & 15) | (7 << 4) | (15 << 8) | ((n >> 4) << 14); }
 
+// Barrier that opens a pass of a loop: the wave's direct copies to LDS and its LDS writes of the pass
+// before have arrived. Both waits are spelt out. __syncthreads() brings a wait for LDS writes of its own, but
+// behind a wait for copies at a loop's head the compiler (clang 22 of ROCm 7.2) has left it out where only the way
+// back to the head has writes under way; a wave could then read what another one had not yet written.
+__device__ __forceinline__ void sync_copies_and_writes() {
+  constexpr int kNoneLeft = waitcnt_vm(0) & ~(15 << 8);  // vmcnt and lgkmcnt zero
+  __builtin_amdgcn_s_waitcnt(kNoneLeft);
+  __syncthreads();
+}
+
 }  // namespace sparvar

@@ -265,8 +265,7 @@ __global__ __launch_bounds__(WK * WR * 64) __attribute__((amdgpu_waves_per_eu(KN
   for (int r = 0; r < 16; ++r) odd.lse2.v[r] = INFINITY;
 
   auto step = [&](int32_t s, const char* now, char* then, const float* lse, float* lse_then, bool first) {
-    __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
-    __syncthreads();
+    sync_copies_and_writes();
     float lse_next = 0.f;
     if (s + 1 < stages) {
       issue(s + 1, then);
