@@ -52,11 +52,32 @@ __device__ __forceinline__ int64_t query_at(const WeightsIO& io, int32_t i) {
   return h * io.q_bh_stride + (int64_t)(i - h * io.n_q) * (D * ELEM);
 }
 
-// LSE of row i in the exp2 domain; +inf, which makes every weight zero, for rows that are not there
-// and rows that had no keys.
-__device__ __forceinline__ float lse2_of(const WeightsIO& io, const float* lse, int32_t i) {
-  const float l = i < io.rows ? lse[i] : -INFINITY;
-  return l == -INFINITY ? INFINITY : l * kLog2e;
+// LSE of row i, the last one's of rows that are not there (these hold its query).
+__device__ __forceinline__ float lse_at(const WeightsIO& io, const float* lse, int32_t i) { return lse[i < io.rows ? i : io.rows - 1]; }
+
+// A thread's LSE, of row i, in the exp2 domain to its place in LDS. Rows that had no keys (-inf) add nothing,
+// whatever is in their place: +inf makes the weight of every number zero, and `none`, a word 32 rows and a bit a row,
+// tells which scores must not count even where they are no numbers. Rows that are not there count for nothing
+// beside 2e38 but where the last row's own weight is infinite or NaN and theirs may be; if it had no keys, nor had they.
+__device__ __forceinline__ void put_lse(const WeightsIO& io, float l, int32_t i, float* lses, uint32_t* none) {
+  lses[threadIdx.x] = l == -INFINITY ? INFINITY : (i < io.rows ? l : 2e38f) * kLog2e;
+  const uint64_t b = __builtin_amdgcn_ballot_w64(l == -INFINITY);
+  if ((threadIdx.x & 31) == 0) none[threadIdx.x / 32] = (uint32_t)(b >> (threadIdx.x & 32));
+}
+
+// Those of a stage.
+template <int RS>
+struct alignas(16) RowsLds {
+  float lse2[RS];
+  uint32_t none[RS / 32];
+};
+
+// Zeroes the scores of those among four rows: registers 4 g .. of a lane hold rows 8 g + 4 half .. of a tile (none: the
+// bits from the lane's first row on). Tiles without such rows cost the branch before it: 64 x 64 364 us (363 without it), 377 with
+// one row of a hundred, 390 where all are such.
+__device__ __forceinline__ void leave_out(f32x16& st, int g, uint32_t none) {
+#pragma unroll
+  for (int r = 0; r < 4; ++r) st[4 * g + r] = none & (1u << (8 * g + r)) ? 0.f : st[4 * g + r];
 }
 
 // The units of a lane's half of a key, as they lie in memory.
@@ -168,7 +189,7 @@ __global__ __launch_bounds__(WK * WR * 64) __attribute__((amdgpu_waves_per_eu(KN
   static_assert(RS * U % NT == 0, "a stage must split evenly over the workgroup");
   __shared__ __attribute__((aligned(16))) char stage0[RS * kRow];
   __shared__ __attribute__((aligned(16))) char stage1[RS * kRow];
-  __shared__ __attribute__((aligned(16))) float lses[2][RS];
+  __shared__ RowsLds<RS> lses[2];
   __shared__ float sums[WR > 1 ? WR : 1][WK * KN * 32];
 
   // (the workgroups of a plane on one XCD: its rows are read by all of them)
@@ -195,7 +216,7 @@ __global__ __launch_bounds__(WK * WR * 64) __attribute__((amdgpu_waves_per_eu(KN
     }
   };
   issue(0, stage0);
-  if (tid < RS) lses[0][tid] = lse2_of(io, lp, tid);
+  if (tid < RS) put_lse(io, lse_at(io, lp, tid), tid, lses[0].lse2, lses[0].none);
   KeyFrag<KT, D> kf[KN];
   {
     RawKey<KT, D> raw[KN];
@@ -219,7 +240,7 @@ __global__ __launch_bounds__(WK * WR * 64) __attribute__((amdgpu_waves_per_eu(KN
     Lse16 lse2;
   } even, odd;
   constexpr int kUnits = U / 2, kShare = (16 + kUnits - 1) / kUnits;  // probabilities of a key after a unit
-  constexpr int kTiles = RS / 32 / WR, kAhead = KN == 1 ? 3 : 4;
+  constexpr int kTiles = RS / 32 / WR, kAhead = 3;
   static_assert(kTiles * 32 * WR == RS, "sets take whole tiles of a stage");
   auto add_up = [&](const Tile& t) {
 #pragma unroll
@@ -230,7 +251,9 @@ __global__ __launch_bounds__(WK * WR * 64) __attribute__((amdgpu_waves_per_eu(KN
     return *reinterpret_cast<const u32x4*>(now + l_row + i / kUnits * (WR * 32 * kRow) + 16 * ((half * kUnits + i % kUnits) ^ sw));
   };
   u32x4 ahead[kAhead];
-  auto tile = [&](const char* now, const float* lse, int t, Tile& cur, const Tile& before) {
+  // (inlined by force: eight copies are more than the compiler inlines, and calls would take the tiles to scratch)
+  auto tile = [&](const char* now, const RowsLds<RS>& lse, int t, uint32_t none, Tile& cur, const Tile& before)
+                  __attribute__((always_inline)) {
     float part[KN][4];
 #pragma unroll
     for (int n = 0; n < KN; ++n) {
@@ -238,7 +261,7 @@ __global__ __launch_bounds__(WK * WR * 64) __attribute__((amdgpu_waves_per_eu(KN
 #pragma unroll
       for (int j = 0; j < 4; ++j) part[n][j] = 0.f;
     }
-    cur.lse2.load(lse + (t * WR + wr) * 32, half);
+    cur.lse2.load(lse.lse2 + (t * WR + wr) * 32, half);
 #pragma unroll
     for (int u = 0; u < kUnits; ++u) {
       const int i = t * kUnits + u;
@@ -257,6 +280,12 @@ __global__ __launch_bounds__(WK * WR * 64) __attribute__((amdgpu_waves_per_eu(KN
     }
 #pragma unroll
     for (int n = 0; n < KN; ++n) sum[n] += (part[n][0] + part[n][1]) + (part[n][2] + part[n][3]);
+    if (none) {
+#pragma unroll
+      for (int n = 0; n < KN; ++n)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) leave_out(cur.st[n], g, none >> (4 * half));
+    }
   };
   // no tile before the first: probabilities of zero
 #pragma unroll
@@ -264,26 +293,30 @@ __global__ __launch_bounds__(WK * WR * 64) __attribute__((amdgpu_waves_per_eu(KN
 #pragma unroll
   for (int r = 0; r < 16; ++r) odd.lse2.v[r] = INFINITY;
 
-  auto step = [&](int32_t s, const char* now, char* then, const float* lse, float* lse_then, bool first) {
+  auto step = [&](int32_t s, const char* now, char* then, const RowsLds<RS>& lse, RowsLds<RS>& lse_then, bool first) {
     sync_copies_and_writes();
     float lse_next = 0.f;
     if (s + 1 < stages) {
       issue(s + 1, then);
-      if (tid < RS) lse_next = lse2_of(io, lp, (s + 1) * RS + tid);
+      if (tid < RS) lse_next = lse_at(io, lp, (s + 1) * RS + tid);
     }
+    uint32_t none[kTiles];  // (in scalar registers: held in others, or read at the tiles' ends, 64 x 64 took 382 us for 362)
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) none[t] = (uint32_t)uniform((int32_t)lse.none[t * WR + wr]);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) ahead[i] = unit(now, i);
     if constexpr (kTiles == 1) {
-      if (first) tile(now, lse, 0, even, odd);
-      else tile(now, lse, 0, odd, even);
+      if (first) tile(now, lse, 0, none[0], even, odd);
+      else tile(now, lse, 0, none[0], odd, even);
     } else {
 #pragma unroll
       for (int t = 0; t < kTiles; t += 2) {
-        tile(now, lse, t, even, odd);
-        tile(now, lse, t + 1, odd, even);
+        tile(now, lse, t, none[t], even, odd);
+        tile(now, lse, t + 1, none[t + 1], odd, even);
       }
     }
-    if (s + 1 < stages && tid < RS) lse_then[tid] = lse_next;
+    if (s + 1 < stages && tid < RS) put_lse(io, lse_next, (s + 1) * RS + tid, lse_then.lse2, lse_then.none);
   };
   for (int32_t s = 0; s < stages; s += 2) {
     step(s, stage0, stage1, lses[0], lses[1], true);
@@ -328,7 +361,7 @@ __global__ __launch_bounds__(kFewWaves * 64) __attribute__((amdgpu_waves_per_eu(
 void key_weights_few_kernel(WeightsIO io, int32_t tiles) {
   constexpr int NT = kFewWaves * 64;
   constexpr int kElem = Traits<KT>::kElem, kRow = D * kElem, U = kRow / 16;
-  extern __shared__ __attribute__((aligned(16))) char smem[];  // row tiles, then their LSEs
+  extern __shared__ __attribute__((aligned(16))) char smem[];  // row tiles, then their LSEs and `none`
   const int32_t slab = blockIdx.x % io.slabs, plane = blockIdx.x / io.slabs;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, half = lane >> 5;
@@ -342,6 +375,7 @@ void key_weights_few_kernel(WeightsIO io, int32_t tiles) {
   const float* lp = io.lse + (int64_t)plane * io.rows;
   const int32_t row_tiles = (io.rows + 31) / 32;
   float* lses = reinterpret_cast<float*>(smem + row_tiles * 32 * kRow);
+  uint32_t* nones = reinterpret_cast<uint32_t*>(lses + row_tiles * 32);
 
   constexpr int kDeep = KT == Keys::kQ4 ? 4 : (KT == Keys::kBf16 ? 2 : 1);  // tiles in flight
   RawKey<KT, D> raw[kDeep];
@@ -361,9 +395,10 @@ void key_weights_few_kernel(WeightsIO io, int32_t tiles) {
     const u32x4 v = ldg16(qp + query_at<D, kElem>(io, i) + 16 * (slot % U));
     *reinterpret_cast<u32x4*>(smem + r * kRow + 16 * ((slot % U) ^ row_swizzle<U>(r))) = v;
   }
-  if (tid < row_tiles * 32) lses[tid] = lse2_of(io, lp, tid);
+  if (tid < row_tiles * 32) put_lse(io, lse_at(io, lp, tid), tid, lses, nones);
   __syncthreads();
   const int sw = row_swizzle<U>(l32);
+  const uint32_t none_of = nones[lane < row_tiles ? lane : 0];  // (of row tile `lane`)
   while (t < end) {
 #pragma unroll
     for (int j = 0; j < kDeep; ++j) {
@@ -379,11 +414,13 @@ void key_weights_few_kernel(WeightsIO io, int32_t tiles) {
 #pragma unroll
         for (int u = 0; u < U / 2; ++u)
           st = unit_product<KT>(*reinterpret_cast<const u32x4*>(row + 16 * ((half * (U / 2) + u) ^ sw)), kf.u[u], st);
+        const uint32_t none = (uint32_t)__builtin_amdgcn_readlane((int)none_of, rt);
         // (eight rows at a time, those that are there)
         const int32_t eights = (io.rows - rt * 32 + 7) / 8;
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
           if (g >= eights) break;
+          if (none >> (8 * g) & 0xff) leave_out(st, g, none >> (4 * half));
           const float4 l = *reinterpret_cast<const float4*>(lses + rt * 32 + 8 * g + 4 * half);
           const float lse2[4] = {l.x, l.y, l.z, l.w};
           float p[4];
@@ -449,7 +486,7 @@ hipError_t launch_weights(WeightsIO io, int32_t planes, int num_cu, hipStream_t 
     int64_t tiles = ((int64_t)planes * all + 8 * num_cu - 1) / (8 * num_cu);
     tiles = (tiles + kFewWaves - 1) / kFewWaves * kFewWaves;
     io.slabs = (int32_t)((all + tiles - 1) / tiles);
-    const size_t lds = (size_t)row_tiles * 32 * (kRow + 4);
+    const size_t lds = (size_t)row_tiles * (32 * (kRow + 4) + 4);
     hipLaunchKernelGGL((key_weights_few_kernel<KT, D>), dim3(planes * io.slabs), dim3(kFewWaves * 64), lds, stream, io,
                        (int32_t)tiles);
     return hipGetLastError();
