@@ -728,7 +728,9 @@ int sparvar_block_sparse_attn_q4_form(const sparvar_geometry_t* g, int32_t k, in
  *   kv_len (nullable): device int32 [B]; of entry b the first
  *   min(max(kv_len[b], 0), n_kv) keys are weighed, the others' w is left as it was.
  *   w_old (NULL: n_old = 0), w: fp32 [B,H_kv,>= n_kv], plane stride w_bh_stride
- *   (elements); w_old may be w itself and must not overlap it otherwise.
+ *   (elements); w_old may be w itself and must not overlap it otherwise. n_old is one
+ *   for all entries: with lengths of their own, w_old has to hold something for every
+ *   key of an entry below n_old, zero for one that is new, or the call below is made.
  *   decay: finite, >= 0.
  */
 int sparvar_key_weights(int32_t B, int32_t H, int32_t H_kv, int32_t n_q, int32_t n_kv, int32_t d,
@@ -736,6 +738,18 @@ int sparvar_key_weights(int32_t B, int32_t H, int32_t H_kv, int32_t n_q, int32_t
                         int64_t k_bh_stride, const sparvar_q4_cache_t* q4, const float* lse,
                         const int32_t* kv_len, const float* w_old, int32_t n_old, float decay, float* w,
                         int64_t w_bh_stride, float softmax_scale, hipStream_t stream);
+
+/*
+ * sparvar_key_weights where each entry had a length of its own: old_len (nullable:
+ * n_old keys of each entry) is device int32 [B], and of entry b w_old counts for the
+ * first min(max(old_len[b], 0), n_old) keys; what it holds further on is not used.
+ */
+int sparvar_key_weights_ragged(int32_t B, int32_t H, int32_t H_kv, int32_t n_q, int32_t n_kv, int32_t d,
+                               sparvar_dtype_t dtype, const void* q, int64_t q_bh_stride, const void* k,
+                               int64_t k_bh_stride, const sparvar_q4_cache_t* q4, const float* lse,
+                               const int32_t* kv_len, const float* w_old, int32_t n_old, const int32_t* old_len,
+                               float decay, float* w, int64_t w_bh_stride, float softmax_scale,
+                               hipStream_t stream);
 
 /*
  * Moves the tokens worth keeping to a cache of their own, a plane at a time. Of a

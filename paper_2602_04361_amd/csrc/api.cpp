@@ -1374,6 +1374,16 @@ int sparvar_key_weights(int32_t B, int32_t H, int32_t H_kv, int32_t n_q, int32_t
                         int64_t k_bh_stride, const sparvar_q4_cache_t* q4, const float* lse,
                         const int32_t* kv_len, const float* w_old, int32_t n_old, float decay, float* w,
                         int64_t w_bh_stride, float softmax_scale, hipStream_t stream) {
+  return sparvar_key_weights_ragged(B, H, H_kv, n_q, n_kv, d, dtype, q, q_bh_stride, k, k_bh_stride, q4, lse, kv_len,
+                                    w_old, n_old, nullptr, decay, w, w_bh_stride, softmax_scale, stream);
+}
+
+int sparvar_key_weights_ragged(int32_t B, int32_t H, int32_t H_kv, int32_t n_q, int32_t n_kv, int32_t d,
+                               sparvar_dtype_t dtype, const void* q, int64_t q_bh_stride, const void* k,
+                               int64_t k_bh_stride, const sparvar_q4_cache_t* q4, const float* lse,
+                               const int32_t* kv_len, const float* w_old, int32_t n_old, const int32_t* old_len,
+                               float decay, float* w, int64_t w_bh_stride, float softmax_scale,
+                               hipStream_t stream) {
   int st = check_dtype_d(dtype, d);
   if (st) return st;
   if ((st = check_heads(B, H, H_kv))) return st;
@@ -1412,6 +1422,7 @@ int sparvar_key_weights(int32_t B, int32_t H, int32_t H_kv, int32_t n_q, int32_t
   a.k_bh_stride = k_bh_stride;
   a.lse = lse;
   a.kv_len = kv_len;
+  a.old_len = old_len;
   a.w_old = w_old;
   a.w = w;
   a.w_bh_stride = w_bh_stride;

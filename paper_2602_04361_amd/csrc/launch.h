@@ -281,7 +281,7 @@ struct KeyWeightsArgs {
   int64_t q_bh_stride, k_bh_stride;  // elements
   Q4View c4;
   const float* lse;
-  const int32_t* kv_len;
+  const int32_t *kv_len, *old_len;
   const float* w_old;
   float* w;
   int64_t w_bh_stride;

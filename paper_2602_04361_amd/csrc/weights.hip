@@ -30,7 +30,7 @@ struct WeightsIO {
   const float* lse;
   const float* w_old;
   float* w;
-  const int32_t* kv_len;
+  const int32_t *kv_len, *old_len;
   int64_t q_bh_stride, k_bh_stride, ks_bh_stride, w_bh_stride;  // bytes (w: elements)
   int32_t n_q, rows, group, H_kv;  // rows = group * n_q: those of a key head
   int32_t n_kv, n_old, slabs;      // workgroups a plane
@@ -158,18 +158,21 @@ __device__ __forceinline__ float tile_sum(const f32x16& st, const Lse16& lse2, f
   return p[0];
 }
 
-__device__ __forceinline__ int32_t length_of(const WeightsIO& io, int32_t plane) {
-  if (!io.kv_len) return io.n_kv;
-  const int32_t len = io.kv_len[plane / io.H_kv];
-  return len < 0 ? 0 : (len < io.n_kv ? len : io.n_kv);
+// Keys of a plane that are weighed, and those that have a weight from before: of each entry its own number, or `most`.
+__device__ __forceinline__ int32_t length_of(const WeightsIO& io, const int32_t* lens, int32_t most, int32_t plane) {
+  if (!lens) return most;
+  const int32_t len = lens[plane / io.H_kv];
+  return len < 0 ? 0 : (len < most ? len : most);
 }
+__device__ __forceinline__ int32_t length_of(const WeightsIO& io, int32_t plane) { return length_of(io, io.kv_len, io.n_kv, plane); }
+__device__ __forceinline__ int32_t old_of(const WeightsIO& io, int32_t plane) { return length_of(io, io.old_len, io.n_old, plane); }
 
-__device__ __forceinline__ float weight_of(const WeightsIO& io, int32_t key, float old, float sum) {
-  return key < io.n_old ? __builtin_fmaf(io.decay, old, sum) : sum;
+__device__ __forceinline__ float weight_of(const WeightsIO& io, bool had, float old, float sum) {
+  return had ? __builtin_fmaf(io.decay, old, sum) : sum;
 }
-__device__ __forceinline__ void store_weight(const WeightsIO& io, int32_t plane, int32_t key, float sum) {
+__device__ __forceinline__ void store_weight(const WeightsIO& io, int32_t plane, int32_t key, int32_t n_old, float sum) {
   const int64_t at = (int64_t)plane * io.w_bh_stride + key;
-  io.w[at] = weight_of(io, key, key < io.n_old ? io.w_old[at] : 0.f, sum);
+  io.w[at] = weight_of(io, key < n_old, key < n_old ? io.w_old[at] : 0.f, sum);
 }
 
 // 16-byte unit u of LDS row r at u ^ this.
@@ -326,11 +329,12 @@ __global__ __launch_bounds__(WK * WR * 64) __attribute__((amdgpu_waves_per_eu(KN
   else add_up(odd);
 #pragma unroll
   for (int n = 0; n < KN; ++n) sum[n] = sum_halves(sum[n]);
+  const int32_t n_old = old_of(io, plane);
   if constexpr (WR == 1) {
 #pragma unroll
     for (int n = 0; n < KN; ++n) {
       const int32_t key = key0 + (wk * KN + n) * 32 + l32;
-      if (key < len && half == (n & 1)) store_weight(io, plane, key, sum[n]);
+      if (key < len && half == (n & 1)) store_weight(io, plane, key, n_old, sum[n]);
     }
   } else {
     if (half == 0) {
@@ -343,7 +347,7 @@ __global__ __launch_bounds__(WK * WR * 64) __attribute__((amdgpu_waves_per_eu(KN
       float t = 0.f;
 #pragma unroll
       for (int r = 0; r < WR; ++r) t += sums[r][tid];
-      store_weight(io, plane, key, t);
+      store_weight(io, plane, key, n_old, t);
     }
   }
 }
@@ -381,10 +385,11 @@ void key_weights_few_kernel(WeightsIO io, int32_t tiles) {
   RawKey<KT, D> raw[kDeep];
   float old[kDeep];
   const float* wo = io.w_old + (int64_t)plane * io.w_bh_stride;
+  const int32_t n_old = old_of(io, plane);
   auto load = [&](int j, int32_t t) {
     const int32_t key = t * 32 + l32;
     raw[j].load(kp, ksp, (uint32_t)(key < len ? key : len - 1), half);
-    old[j] = key < io.n_old ? wo[key] : 0.f;
+    old[j] = key < n_old ? wo[key] : 0.f;
   };
   int32_t t = first + wave;
 #pragma unroll
@@ -431,7 +436,7 @@ void key_weights_few_kernel(WeightsIO io, int32_t tiles) {
       }
       sum = sum_halves(sum);
       const int32_t key = t * 32 + l32;
-      if (half == 0 && key < len) io.w[(int64_t)plane * io.w_bh_stride + key] = weight_of(io, key, had, sum);
+      if (half == 0 && key < len) io.w[(int64_t)plane * io.w_bh_stride + key] = weight_of(io, key < n_old, had, sum);
       t += kFewWaves;
     }
   }
@@ -513,6 +518,7 @@ hipError_t launch_key_weights(const KeyWeightsArgs& a, hipStream_t stream) {
   io.w_old = a.w_old;
   io.w = a.w;
   io.kv_len = a.kv_len;
+  io.old_len = a.old_len;
   io.q_bh_stride = a.q_bh_stride * elem;
   io.k_bh_stride = a.k ? a.k_bh_stride * elem : a.c4.bh_stride;
   io.ks_bh_stride = a.k ? 0 : a.c4.sc_stride;

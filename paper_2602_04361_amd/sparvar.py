@@ -59,6 +59,7 @@ EXPORTS = [
     "sparvar_block_sparse_attn_q4_fwd",
     "sparvar_block_sparse_attn_q4_form",
     "sparvar_key_weights",
+    "sparvar_key_weights_ragged",
     "sparvar_kv_evict",
     "sparvar_status_string",
     "sparvar_last_error",
@@ -200,6 +201,8 @@ def load_library(path: str = LIB_PATH):
         "sparvar_block_sparse_attn_q4_form": (ctypes.c_int, [G, i32, i32, i32, i32, i32, ctypes.POINTER(i32)]),
         "sparvar_key_weights": (ctypes.c_int, [i32, i32, i32, i32, i32, i32, ctypes.c_int, vp, i64, vp, i64, Q4, vp, vp, vp,
                                                i32, f32, vp, i64, f32, vp]),
+        "sparvar_key_weights_ragged": (ctypes.c_int, [i32, i32, i32, i32, i32, i32, ctypes.c_int, vp, i64, vp, i64, Q4, vp, vp,
+                                                      vp, i32, vp, f32, vp, i64, f32, vp]),
         "sparvar_kv_evict": (ctypes.c_int, [i32, i32, i32, ctypes.c_int, i32, i32, i32, i32, vp, vp, i64, vp, vp, i64, vp,
                                             vp, i64, Q4, Q4, vp, vp, i64, vp]),
         "sparvar_status_string": (ctypes.c_char_p, [ctypes.c_int]),
@@ -978,10 +981,10 @@ def _pair(k, v, name):
 
 
 def sparvar_key_weights(q, n_kv, lse, w, w_old=None, n_old=None, decay=1.0, k_cache=None, q4=None, kv_len=None,
-                        softmax_scale=None, stream=None):
+                        softmax_scale=None, stream=None, old_len=None):
     """Attention weight that the first n_kv keys (kv_len[b] of them, int32, for entry b) of k_cache [B,H_kv,tokens,d] or of a
     4-bit cache q4 got from queries q [B,H,n_q,d] with softmax denominators lse: w = decay * w_old + it, w_old counting for
-    the first n_old keys (default: all, or none without w_old); see sparvar.h."""
+    the first n_old keys (default: all, or none without w_old), of entry b for old_len[b] of them (int32); see sparvar.h."""
     lib = load_library()
     _whole("n_kv", n_kv)
     B, H, n_q, d = q.shape
@@ -990,7 +993,7 @@ def sparvar_key_weights(q, n_kv, lse, w, w_old=None, n_old=None, decay=1.0, k_ca
         n_old = 0 if w_old is None else n_kv
     _whole("n_old", n_old)
     _same("lse", lse, (B, H, n_q), _torch().float32)
-    dev = _here(q, lse, w, w_old, k_cache, kv_len)
+    dev = _here(q, lse, w, w_old, k_cache, kv_len, old_len)
     if (k_cache is None) == (q4 is None):
         raise SparvarError(ERR_INVALID, "either k_cache or a 4-bit cache is required")
     if q4 is not None:
@@ -1004,12 +1007,14 @@ def sparvar_key_weights(q, n_kv, lse, w, w_old=None, n_old=None, decay=1.0, k_ca
             raise SparvarError(ERR_CAPACITY, f"{n_kv} keys exceed the cache's {k_cache.shape[2]}")
     if kv_len is not None:
         _same("kv_len", kv_len, (B,), _torch().int32)
+    if old_len is not None:
+        _same("old_len", old_len, (B,), _torch().int32)
     ws = _weight_planes("w", w, B, H_kv, n_kv)
     if w_old is not None and _weight_planes("w_old", w_old, B, H_kv, n_kv) != ws:
         raise SparvarError(ERR_INVALID, "w and w_old must share their plane stride")
-    _check(lib.sparvar_key_weights(B, H, H_kv, n_q, n_kv, d, dt, _ptr(q), _plane_stride(q, "q"), _ptr(k_cache), ks,
-                                   None if q4 is None else q4.ref, _ptr(lse), _ptr(kv_len), _ptr(w_old), n_old, float(decay),
-                                   _ptr(w), ws, _scale(softmax_scale, d), _stream(stream)))
+    _check(lib.sparvar_key_weights_ragged(B, H, H_kv, n_q, n_kv, d, dt, _ptr(q), _plane_stride(q, "q"), _ptr(k_cache), ks,
+                                          None if q4 is None else q4.ref, _ptr(lse), _ptr(kv_len), _ptr(w_old), n_old,
+                                          _ptr(old_len), float(decay), _ptr(w), ws, _scale(softmax_scale, d), _stream(stream)))
     return w
 
 
