@@ -752,6 +752,13 @@ int sparvar_key_weights_ragged(int32_t B, int32_t H, int32_t H_kv, int32_t n_q, 
                                hipStream_t stream);
 
 /*
+ * The form that both calls take for these sizes (4-bit caches take that of bf16):
+ * form[0] keys of a workgroup, 256, 128, 64 or 32, or 0 for few queries of a key head.
+ */
+int sparvar_key_weights_form(int32_t B, int32_t H, int32_t H_kv, int32_t n_q, int32_t n_kv, int32_t d,
+                             sparvar_dtype_t dtype, int32_t* form);
+
+/*
  * Moves the tokens worth keeping to a cache of their own, a plane at a time. Of a
  * plane's first len tokens (len = n, or min(max(kv_len[b], 0), n)) all are kept where
  * len <= n_keep; otherwise n_keep: the first n_first, the last n_last, and of those

@@ -387,6 +387,17 @@ int check_rows(const void* p, int64_t batch, int64_t token, int64_t row, int32_t
   return SPARVAR_OK;
 }
 
+int check_weights(int32_t B, int32_t H, int32_t H_kv, int32_t n_q, int32_t n_kv, int32_t d, sparvar_dtype_t dtype) {
+  int st = check_dtype_d(dtype, d);
+  if (st) return st;
+  if ((st = check_heads(B, H, H_kv))) return st;
+  if (n_q < 1 || n_kv < 1) return fail(SPARVAR_ERR_INVALID, "n_q and n_kv must be >= 1");
+  if ((int64_t)B * H * n_q >= 0x7fffff00) return fail(SPARVAR_ERR_INVALID, "B*H*n_q too large");
+  if (n_kv >= 0x7fffff00) return fail(SPARVAR_ERR_INVALID, "n_kv = %d too large", n_kv);
+  if ((int64_t)B * H_kv * ((n_kv + 31) / 32) >= (int64_t(1) << 31)) return fail(SPARVAR_ERR_INVALID, "too many keys for one launch");
+  return SPARVAR_OK;
+}
+
 int check_dense_codes(int32_t B, int32_t H, int32_t H_kv, int32_t n_q, int32_t n_kv, int32_t d) {
   int st = check_dtype_d(SPARVAR_BF16, d);
   if (st) return st;
@@ -1384,13 +1395,8 @@ int sparvar_key_weights_ragged(int32_t B, int32_t H, int32_t H_kv, int32_t n_q, 
                                const int32_t* kv_len, const float* w_old, int32_t n_old, const int32_t* old_len,
                                float decay, float* w, int64_t w_bh_stride, float softmax_scale,
                                hipStream_t stream) {
-  int st = check_dtype_d(dtype, d);
+  int st = check_weights(B, H, H_kv, n_q, n_kv, d, dtype);
   if (st) return st;
-  if ((st = check_heads(B, H, H_kv))) return st;
-  if (n_q < 1 || n_kv < 1) return fail(SPARVAR_ERR_INVALID, "n_q and n_kv must be >= 1");
-  if ((int64_t)B * H * n_q >= 0x7fffff00) return fail(SPARVAR_ERR_INVALID, "B*H*n_q too large");
-  if (n_kv >= 0x7fffff00) return fail(SPARVAR_ERR_INVALID, "n_kv = %d too large", n_kv);
-  if ((int64_t)B * H_kv * ((n_kv + 31) / 32) >= (int64_t(1) << 31)) return fail(SPARVAR_ERR_INVALID, "too many keys for one launch");
   if ((st = check_softmax_scale(softmax_scale))) return st;
   if (!std::isfinite(decay) || decay < 0.f) return fail(SPARVAR_ERR_INVALID, "decay %g is not finite and >= 0", decay);
   const int elem = dtype == SPARVAR_BF16 ? 2 : 4;
@@ -1431,6 +1437,15 @@ int sparvar_key_weights_ragged(int32_t B, int32_t H, int32_t H_kv, int32_t n_q, 
   a.swizzle = opt(SPARVAR_OPT_SWIZZLE);
   a.num_cu = device_cus();
   return hip_status(launch_key_weights(a, stream), "key weights launch");
+}
+
+int sparvar_key_weights_form(int32_t B, int32_t H, int32_t H_kv, int32_t n_q, int32_t n_kv, int32_t d,
+                             sparvar_dtype_t dtype, int32_t* form) {
+  const int st = check_weights(B, H, H_kv, n_q, n_kv, d, dtype);
+  if (st) return st;
+  if (!form) return fail(SPARVAR_ERR_INVALID, "form is NULL");
+  form[0] = key_weights_form(B, H, H_kv, n_q, n_kv, d, dtype == SPARVAR_F32, device_cus());
+  return ok();
 }
 
 int sparvar_kv_evict(int32_t B, int32_t H_kv, int32_t d, sparvar_dtype_t dtype, int32_t n, int32_t n_keep,

@@ -290,6 +290,8 @@ struct KeyWeightsArgs {
   int num_cu;
 };
 hipError_t launch_key_weights(const KeyWeightsArgs& a, hipStream_t stream);
+// Keys of a workgroup of such a call (0: all its rows lie in LDS).
+int32_t key_weights_form(int32_t B, int32_t H, int32_t H_kv, int32_t n_q, int32_t n_kv, int32_t d, bool f32, int num_cu);
 
 // Tokens kept by weight, moved to a cache of their own. A row of the cache is `row` bytes of K and V
 // each and (4-bit caches) `srow` bytes of scales.

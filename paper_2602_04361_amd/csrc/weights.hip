@@ -458,6 +458,12 @@ hipError_t launch_many(WeightsIO io, int32_t planes, hipStream_t stream) {
 // shared out among two and four sets of waves): 2 x 16 heads, 4096 rows 362 / 395 / 456 / 650, 1024 rows 33.6 /
 // 31.6 / 38.3 / 54.1; 8 heads, 1024 rows 20.5 / 17.3 / 16.0 / 19.5; one key head of 8, 200 rows of each, 1000
 // keys 29.4 / 24.3 / 18.1 / 13.4. (fp32 keys in registers leave no room for 256.)
+// d = 64, bf16: 2 x 16 heads, 4096 rows 251 / 260 / 284 / 368; 24 heads, 2102 x 8377 91 / 88 / 95 / 124; 2 x 12 heads,
+// 576 x 1497 11.3 / 10.9 / 10.1 / 12.0. fp32, 128 / 64 / 32: the same at d = 64 1491 / 1493 / 1721, 496 / 485 / 558, 42.8 / 35.3 /
+// 39.1, 8 heads, 1024 x 2521 41.9 / 41.2 / 37.2; d = 128 2861 / 2925 / 3830, 950 / 941 / 1253, 78.4 / 66.6 / 85.5, 74.6 / 74.6 / 76.8.
+// The constants of d = 128 serve fp32 at d = 64 too: of ten sizes the form taken is the best in seven, within 2% in one
+// and 11 to 13% above it in two (8 heads, 1024 x 2521, and 4, 1600 x 4121); bf16 at d = 64 2 to 19% above in three, d = 128
+// fp32 within 1.4% in all.
 struct ManyForm {
   int keys;
   float a, b, c;
@@ -507,6 +513,11 @@ hipError_t launch_weights(WeightsIO io, int32_t planes, int num_cu, hipStream_t 
 }
 
 }  // namespace
+
+int32_t key_weights_form(int32_t B, int32_t H, int32_t H_kv, int32_t n_q, int32_t n_kv, int32_t d, bool f32, int num_cu) {
+  const int32_t most = f32 ? kFewRows<Keys::kF32> : kFewRows<Keys::kBf16>;
+  return H / H_kv * n_q <= most ? 0 : many_form(f32, d, B * H_kv, n_kv, num_cu);
+}
 
 hipError_t launch_key_weights(const KeyWeightsArgs& a, hipStream_t stream) {
   const int32_t elem = a.bf16 ? 2 : 4, group = a.H / a.H_kv;

@@ -60,6 +60,7 @@ EXPORTS = [
     "sparvar_block_sparse_attn_q4_form",
     "sparvar_key_weights",
     "sparvar_key_weights_ragged",
+    "sparvar_key_weights_form",
     "sparvar_kv_evict",
     "sparvar_status_string",
     "sparvar_last_error",
@@ -203,6 +204,7 @@ def load_library(path: str = LIB_PATH):
                                                i32, f32, vp, i64, f32, vp]),
         "sparvar_key_weights_ragged": (ctypes.c_int, [i32, i32, i32, i32, i32, i32, ctypes.c_int, vp, i64, vp, i64, Q4, vp, vp,
                                                       vp, i32, vp, f32, vp, i64, f32, vp]),
+        "sparvar_key_weights_form": (ctypes.c_int, [i32, i32, i32, i32, i32, i32, ctypes.c_int, ctypes.POINTER(i32)]),
         "sparvar_kv_evict": (ctypes.c_int, [i32, i32, i32, ctypes.c_int, i32, i32, i32, i32, vp, vp, i64, vp, vp, i64, vp,
                                             vp, i64, Q4, Q4, vp, vp, i64, vp]),
         "sparvar_status_string": (ctypes.c_char_p, [ctypes.c_int]),
@@ -1016,6 +1018,17 @@ def sparvar_key_weights(q, n_kv, lse, w, w_old=None, n_old=None, decay=1.0, k_ca
                                           None if q4 is None else q4.ref, _ptr(lse), _ptr(kv_len), _ptr(w_old), n_old,
                                           _ptr(old_len), float(decay), _ptr(w), ws, _scale(softmax_scale, d), _stream(stream)))
     return w
+
+
+def sparvar_key_weights_form(B, H, H_kv, n_q, n_kv, d, dtype):
+    """Keys of a workgroup that such a call takes for queries of `dtype` (0: the form of few queries); see sparvar.h."""
+    _whole("sizes", B, H, H_kv, n_q, n_kv, d)
+    torch = _torch()
+    if dtype not in (torch.bfloat16, torch.float32):
+        raise SparvarError(ERR_UNSUPPORTED, f"queries of {dtype}")
+    form = (ctypes.c_int32 * 1)()
+    _check(load_library().sparvar_key_weights_form(B, H, H_kv, n_q, n_kv, d, BF16 if dtype == torch.bfloat16 else F32, form))
+    return form[0]
 
 
 def sparvar_kv_evict(w, n, n_keep, n_first, n_last, kept, w_out, k_src=None, v_src=None, k_dst=None, v_dst=None, q4_src=None,
