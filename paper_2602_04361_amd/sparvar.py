@@ -1012,7 +1012,7 @@ def sparvar_key_weights(q, n_kv, lse, w, w_old=None, n_old=None, decay=1.0, k_ca
     if old_len is not None:
         _same("old_len", old_len, (B,), _torch().int32)
     ws = _weight_planes("w", w, B, H_kv, n_kv)
-    if w_old is not None and _weight_planes("w_old", w_old, B, H_kv, n_kv) != ws:
+    if w_old is not None and _weight_planes("w_old", w_old, B, H_kv, n_kv) != ws and B * H_kv > 1:  # (one plane has no stride)
         raise SparvarError(ERR_INVALID, "w and w_old must share their plane stride")
     _check(lib.sparvar_key_weights_ragged(B, H, H_kv, n_q, n_kv, d, dt, _ptr(q), _plane_stride(q, "q"), _ptr(k_cache), ks,
                                           None if q4 is None else q4.ref, _ptr(lse), _ptr(kv_len), _ptr(w_old), n_old,
