@@ -676,7 +676,10 @@ typedef struct sparvar_q4_cache {
  * Writes rows [0, n) of k_src and v_src ([B,H_kv,n,d] of `dtype`, plane stride
  * src_bh_stride) to tokens [t0, t0 + n) of a 4-bit cache, and reads such tokens back
  * to rows [0, n) of k_dst and v_dst (exact in both types). A step's rows come from
- * sparvar_qkv_append with a 16-bit cache.
+ * sparvar_qkv_append with a 16- or 32-bit cache. Its keys are rounded to that type
+ * first: the half step above holds for the rows given, and a key normed or rotated
+ * on its way into bf16 rows is off by up to 2^-8 of itself more (into fp32 rows, from
+ * fp32 projections, 2^-24).
  */
 int sparvar_kv_quantize_q4(int32_t B, int32_t H_kv, int32_t d, sparvar_dtype_t dtype, int32_t n, int32_t t0,
                            const void* k_src, const void* v_src, int64_t src_bh_stride,

@@ -11,8 +11,11 @@
 // run of kept rows, which is what takes the time: it is bound by memory. 2 x 8 heads of 128, 21260 of 42521 tokens,
 // bf16: 87 us for 354 MB, a large copy of as much 69, the difference the search of the threshold before it (117 with
 // passes over all tokens for every digit, each a histogram of one bin a weight). 460 of 921 tokens of 2 x 12 heads:
-// 11 us, all latency. 1024 of 42521 tokens of equal weight 29 us, of different ones 27. Ranks stay in registers up to 49152 tokens (12 rows of 4096; 104 registers), past that they are
-// read again in every pass.
+// 11 us, all latency. 1024 of 42521 tokens of equal weight 29 us, of different ones 27. Ranks stay in registers up to
+// 49152 tokens (12 rows of 4096; 104 registers), past that they are read again in every pass, by each of a plane's workgroups,
+// of which there is one for every 4096 kept rows: the search then grows with the square of the length. Half of n tokens
+// of 2 x 8 heads of 128 again and again, us (at the copy's rate): 49152 72 (79, partly from the last-level cache), 49153 85,
+// 60000 108 (97), 100000 194 (161), 200000 476 (322); one head, 100000 57 (10), 400000 221 (40).
 #include "device_common.h"
 #include "launch.h"
 

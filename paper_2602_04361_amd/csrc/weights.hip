@@ -10,7 +10,7 @@
 // A sum over channels may run in any order: a lane's fragments are 16-byte units of its half of a
 // row, the same ones of Q (rows in LDS) and K (registers), eight bf16 or four fp32 channels each.
 //
-// Many rows: bound by the matrix units (53% busy) and the exponentials beside them (vector units 71%). 2 x 16 heads,
+// Many rows: bound by the matrix units (55% busy) and the exponentials beside them (vector units 74%). 2 x 16 heads,
 // 4096 x 10521, d = 128, bf16 362 to 382 us by card, 0.98 to 0.92 PFLOP/s; with the exponentials of a tile behind
 // its products, not under the next tile's, 382 where now 362.
 #include "device_common.h"
@@ -354,7 +354,7 @@ __global__ __launch_bounds__(WK * WR * 64) __attribute__((amdgpu_waves_per_eu(KN
 
 // Few rows (up to 128 of a key head; single tokens against a long cache): bound by K's way from
 // memory. All rows lie in LDS; every wave walks tiles of 32 keys by itself, the next ones' in flight: one token
-// of 4 x 32 heads on 8, up to 42521 keys of 4 bits (84 MB) 20.5 us, a large copy of as much 16.3.
+// of 4 x 32 heads on 8, up to 42521 keys of 4 bits (84 MB) 20.9 us, a large copy of as much 16.3.
 constexpr int kFewWaves = 4;
 // (their LDS below 64 KB)
 template <Keys KT>

@@ -14,7 +14,8 @@ Local rows are geometry-only and built once per step by build_local().
 Q8SparsePath runs the same steps from the projections on, over an 8-bit cache,
 Q4SparsePath over a 4-bit one. BudgetPath attends densely over a 4-bit cache of
 bounded length: what its keys got of the attention decides which ones stay.
-All arithmetic runs in libsparvar.so; this module only allocates and calls.
+All arithmetic runs in libsparvar.so; this module only allocates and calls, but for
+the token numbers that BudgetPath keeps beside its cache, which torch writes and gathers.
 """
 from __future__ import annotations
 
@@ -302,7 +303,8 @@ class Q8SparsePath(SparsePath):
 class Q4SparsePath(SparsePath):
     """One layer over a 4-bit cache that grows scale by scale, as C-ABI calls: Q8SparsePath's steps, with a scale's rows
     appended to 16 bits first (sparvar_qkv_append), written from there (sparvar_kv_quantize_q4), and attention by
-    sparvar_dense_attn_q4_fwd and sparvar_block_sparse_attn_q4_fwd. heads as there."""
+    sparvar_dense_attn_q4_fwd and sparvar_block_sparse_attn_q4_fwd. heads as there. Keys are rounded twice, to bf16 and to codes
+    (values once: theirs are bf16 already)."""
 
     def __init__(self, geom: sv.Geometry, S, steps, B, H, d, topk, radius, heads=None, device="cuda", *, prev_dilation=0,
                  softmax_scale=None, projection="point"):
@@ -368,11 +370,13 @@ class BudgetPath:
     """One dense layer whose 4-bit cache is held to a budget of tokens, as C-ABI calls.
 
     step(q, k, v) takes the projections [B, n, heads, d] of the next n tokens (n <= n_max; a scale, or one token):
-      append:  norms and rotation to 16 bits (sparvar_qkv_append), rows to the cache (sparvar_kv_quantize_q4);
+      append:  norms and rotation to 16 bits (sparvar_qkv_append), rows to the cache (sparvar_kv_quantize_q4): keys are
+               rounded twice, to bf16 and to codes;
       attend:  dense attention over the cache (sparvar_dense_attn_q4_fwd);
       weigh:   what each cached key got of it, added to decay times what it had (sparvar_key_weights);
       evict:   where more than `budget` tokens are held, the n_first first, the n_last last and those of largest weight
-               move to the other of two caches (sparvar_kv_evict), which is the cache from then on.
+               move to the other of two caches (sparvar_kv_evict), which is the cache from then on. All that stay
+               move, also where one token goes.
     held: tokens in the cache; tokens [B, H_kv, held]: which of the sequence they are, a row for each key head.
     heads: a NormRope whose table has a row for every token of the sequence, or None.
     """

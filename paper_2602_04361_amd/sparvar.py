@@ -665,7 +665,6 @@ class NormRope:
                             _ptr(q_weight), _ptr(k_weight), _ptr(cos_sin))
         self.ref = ctypes.byref(self.c)
 
-
     def rows(self, t0, n):
         """The same for a cache whose token 0 is token t0 of this one's table: its rows [t0, t0 + n)."""
         cs = self.cos_sin
